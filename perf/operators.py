@@ -1,0 +1,445 @@
+"""The operators of a decoder block that runs in 8 bits, through the public entry points
+(`paper_2602_07899_amd.tlq`), beside the same mathematics in elementary torch operations.
+
+A case is one dict of plain values; `kind` names the operator:
+
+  linear     tokens to 8-bit codes with a step for each token (`row_codes`), times stored 8-bit weights
+             with a step for each output (`linear_i8`):
+               xt = x * f,  step_t = max(max_c |xt|, 1e-5) / 127,  code = clip(rint(xt / step_t)),
+               y[t, o] = step_t * step_o * sum_c code[t, c] * wcode[o, c]
+  rope       queries and keys normalised for each head and rotated by their position (`qk_norm_rope`):
+               u = x / sqrt(mean(x^2) + eps) * w,  (u1, u2) -> (u1 cos - u2 sin, u2 cos + u1 sin),
+               angle = position * inv_freq[i]
+  append     new keys and values into a paged cache of 8-bit codes with a step for each page and head
+             (`kv_append`); a page that was begun earlier keeps the larger of its old and new step
+  attention  causal attention over such a cache (`kv_attention`): single tokens, several, whole prompts
+
+What is held in 8 bits is returned as the values that it stands for.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+_DT = {"f16": torch.float16, "bf16": torch.bfloat16}
+_EPS = 1e-6
+_FLOOR = 1e-5
+_MAX_FLOPS = 1.5e12      # no drawn case costs more than the largest listed one
+_MAX_BYTES = 9e8
+_BASE = 1e6              # of the rotation's frequencies
+
+
+def listed():
+    return [
+        # one generated token through an attention projection of a 7B-class layer: latency counts
+        dict(name="linear_token", kind="linear", n=1, ci=4096, co=4096, bits=8, dt="bf16"),
+        # 48 sequences that each generate a token, a 7B-class down projection: the weights' bytes count
+        dict(name="linear_batch", kind="linear", n=48, ci=11008, co=4096, bits=8, dt="f16"),
+        # one sample of an odd length through a linear of odd sizes, codes of six bits
+        dict(name="linear_ragged", kind="linear", n=613, ci=1096, co=1399, bits=6, dt="bf16"),
+        # prompts of 16 samples x 640 tokens through a 13B-class gate projection: the matrix cores count
+        dict(name="linear_prompt", kind="linear", n=10240, ci=5120, co=13824, bits=8, dt="f16"),
+        # one generated token of each of 16 sequences at far positions, eight key heads for 32 query heads
+        dict(name="rope_token", kind="rope", n=16, heads=32, kv=8, dh=128, rot=128, pairs=0, norm=1, far=1000000, dt="bf16"),
+        # prompts of 34 samples x 1200 tokens, 13B-class heads
+        dict(name="rope_prompt", kind="rope", n=40800, heads=40, kv=40, dh=128, rot=128, pairs=0, norm=1, far=1200, dt="f16"),
+        # one token of each of 64 sequences into pages that were begun earlier
+        dict(name="append_token", kind="append", seqs=64, new=1, ctx=1200, kv=8, dh=128, page=64, dt="bf16"),
+        # whole prompts of a 7B-class layer into fresh pages, the last of each page row partly filled
+        dict(name="append_prompt", kind="append", seqs=16, new=613, ctx=613, kv=32, dh=128, page=32, dt="f16"),
+        # one sequence, one token, a sample's length: latency counts
+        dict(name="attention_token", kind="attention", seqs=1, new=1, ctx=1200, heads=32, kv=32, dh=128, page=64, dt="bf16"),
+        # 64 sequences of 4096 to 8192 tokens that each generate a token, grouped heads: the cache's bytes count
+        dict(name="attention_batch", kind="attention", seqs=64, new=1, ctx=8192, heads=32, kv=8, dh=128, page=16, dt="f16"),
+        # one sequence of 131,072 tokens, seven query heads to a key head: few heads, a long axis
+        dict(name="attention_long", kind="attention", seqs=1, new=1, ctx=131072, heads=28, kv=4, dh=128, page=64, dt="bf16"),
+        # whole prompts of up to 1200 tokens, 13B-class heads: the matrix cores count
+        dict(name="attention_prompt", kind="attention", seqs=16, new=1200, ctx=1200, heads=40, kv=40, dh=128, page=64, dt="bf16"),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _heads(rng):
+    kv = rng.choice([1, 2, 4, 5, 8, 16, 32, 40])
+    return kv * rng.choice([g for g in (1, 2, 4, 6, 7, 8) if kv * g <= 64]), kv
+
+
+def draw(rng):
+    while True:
+        case = _draw(rng)
+        w = work(case)
+        if w["flops"] <= _MAX_FLOPS and w["bytes"] <= _MAX_BYTES:
+            return case
+
+
+def _draw(rng):
+    kind = rng.choice(["linear", "linear", "rope", "append", "attention", "attention", "attention"])
+    dt = rng.choice(["f16", "bf16"])
+    if kind == "linear":
+        return dict(kind=kind, n=_log(rng, 1, 10240), ci=_log(rng, 32, 1728) * 8, co=_log(rng, 100, 13824),
+                    bits=rng.choice([8, 8, 8, 6, 4]), dt=dt)
+    heads, kv = _heads(rng)
+    if kind == "rope":
+        dh = rng.choice([64, 128, 128, 256])
+        return dict(kind=kind, n=_log(rng, 1, 40960), heads=heads, kv=kv, dh=dh, rot=rng.choice([dh, dh, dh // 2]),
+                    pairs=rng.choice([0, 0, 1]), norm=rng.choice([1, 1, 0]), far=_log(rng, 100, 4000000), dt=dt)
+    dh, page = rng.choice([64, 128, 128]), rng.choice([16, 32, 64, 128])
+    if kind == "append":
+        seqs, new = _log(rng, 1, 64), rng.choice([1, 1, _log(rng, 2, 16), _log(rng, 16, 1200)])
+        return dict(kind=kind, seqs=seqs, new=new, ctx=new + rng.choice([0, _log(rng, 1, 4096)]), kv=kv, dh=dh, page=page, dt=dt)
+    form = rng.choice(["token", "token", "several", "chunk", "prompt"])
+    ctx = _log(rng, 1, 131072) if form in ("token", "several") else _log(rng, 16, 4096)
+    new = {"token": 1, "several": rng.randint(2, 9), "chunk": max(1, ctx // rng.randint(2, 9)), "prompt": ctx}[form]
+    return dict(kind=kind, seqs=_log(rng, 1, 64), new=new, ctx=max(new, ctx), heads=heads, kv=kv, dh=dh, page=page, dt=dt)
+
+
+# ------------------------------------------------------------------ sizes that follow from a case
+def _ld8(c):
+    return -(-c // 128) * 128
+
+
+def _new(case):
+    """New tokens of each sequence: all of them for single tokens and appends, a few less from one to the next else."""
+    n = case["new"]
+    return [n - (i * 7) % (n // 8 + 1) for i in range(case["seqs"])]
+
+
+def _lens(case):
+    """Tokens of each sequence, the new ones among them: from the case's most down to about a half of it."""
+    prior = case["ctx"] - case["new"]
+    return [a + prior - (i * 131) % (prior // 2 + 1) for i, a in enumerate(_new(case))]
+
+
+def _pages_of(case):
+    return [-(-n // case["page"]) for n in _lens(case)]
+
+
+def _touched(case):
+    """(sequence, page of it) pairs that an append writes."""
+    out = []
+    for s, (a, n) in enumerate(zip(_new(case), _lens(case))):
+        out += [(s, p) for p in range((n - a) // case["page"], (n - 1) // case["page"] + 1)]
+    return out
+
+
+def work(case):
+    k = case["kind"]
+    if k == "linear":
+        n, ci, co = case["n"], case["ci"], case["co"]
+        return {"bytes": 2 * n * ci + 4 * ci + ci * co + 4 * co + 2 * n * co, "flops": 2 * n * ci * co}
+    if k == "rope":
+        n, e = case["n"], (case["heads"] + case["kv"]) * case["dh"]
+        return {"bytes": 4 * n * e + 4 * n + 8 * case["dh"], "flops": 10 * n * e}
+    row = case["kv"] * case["dh"]
+    if k == "append":
+        fill = sum(_new(case))
+        page_values = len(_touched(case)) * case["page"] * row
+        old = sum((n - a) % case["page"] for a, n in zip(_new(case), _lens(case)))
+        # keys and values: 16-bit rows in, earlier codes of begun pages in, values of the written pages out
+        return {"bytes": 2 * (2 * fill * row + old * row + 4 * page_values), "flops": 8 * fill * row}
+    rows, pairs = sum(_new(case)), 0
+    for a, n in zip(_new(case), _lens(case)):
+        pairs += a * (n - a) + a * (a + 1) // 2
+    cache = sum(_lens(case)) * row * 2 + sum(_pages_of(case)) * case["kv"] * 8
+    return {"bytes": cache + 4 * rows * case["heads"] * case["dh"], "flops": 4 * pairs * case["heads"] * case["dh"]}
+
+
+# ------------------------------------------------------------------ inputs
+def _gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed * 2654435761 % (1 << 62) + 17)
+    return g
+
+
+def _randn(g, *shape):
+    return torch.randn(shape, generator=g, device="cuda", dtype=torch.float32)
+
+
+def prepare(case, seed):
+    g, dt, k = _gen(seed), _DT[case["dt"]], case["kind"]
+    if k == "linear":
+        n, ci, co = case["n"], case["ci"], case["co"]
+        x = _randn(g, n, ci)
+        loud = torch.randperm(ci, generator=g, device="cuda")[:max(1, ci // 100)]
+        x[:, loud] *= 20.0                                  # the few loud channels of a decoder's activations
+        s = x.abs().mean(0).clamp_min(1e-3).sqrt()          # smoothing scales
+        w = _randn(g, co, ci) * 0.02 * s
+        step = w.abs().amax(1).clamp_min(_FLOOR) / 127.0
+        codes = torch.zeros((co, _ld8(ci)), dtype=torch.int8, device="cuda")
+        codes[:, :ci] = torch.round(w / step[:, None]).clamp(-128, 127).to(torch.int8)
+        return dict(case=case, x=x.to(dt), f=1.0 / s, w=codes, wstep=step)
+    if k == "rope":
+        n, e = case["n"], (case["heads"] + case["kv"]) * case["dh"]
+        qkv = _randn(g, n, e + case["kv"] * case["dh"]).to(dt)       # values behind queries and keys, as a projection writes them
+        half = case["rot"] // 2
+        inv = _BASE ** (-torch.arange(half, dtype=torch.float64) / half)
+        pos = torch.randint(0, case["far"], (n,), generator=g, device="cuda", dtype=torch.int32)
+        return dict(case=case, qkv=qkv, pos=pos, inv=inv.cuda(),
+                    wq=1.0 + 0.2 * _randn(g, case["dh"]), wk=1.0 + 0.2 * _randn(g, case["dh"]))
+    # a pool of pages, of which every sequence holds some in no order
+    kv, dh, page = case["kv"], case["dh"], case["page"]
+    new, lens, pages = _new(case), _lens(case), _pages_of(case)
+    total = sum(pages)
+    pool = total + 3
+    order = torch.randperm(pool, generator=g, device="cuda")[:total].to(torch.int32)
+    table = torch.full((case["seqs"], max(pages)), -1, dtype=torch.int32, device="cuda")
+    at = 0
+    for s, m in enumerate(pages):
+        table[s, :m] = order[at:at + m]
+        at += m
+
+    def codes(*shape):
+        return torch.cat([(_randn(g, min(1 << 12, shape[0] - i), *shape[1:]) * 32.0).round_().clamp_(-127, 127).to(torch.int8)
+                          for i in range(0, shape[0], 1 << 12)])
+    state = dict(case=case, table=table, new=new, lens=lens, pool=pool,
+                 cu=torch.tensor([sum(new[:i]) for i in range(len(new) + 1)], dtype=torch.int32, device="cuda"),
+                 dlens=torch.tensor(lens, dtype=torch.int32, device="cuda"),
+                 kc=codes(pool, kv, page, dh), vc=codes(pool, kv, dh, page),
+                 ks=0.03 * torch.exp(0.3 * _randn(g, pool, kv)), vs=0.03 * torch.exp(0.3 * _randn(g, pool, kv)))
+    rows = sum(new)
+    if k == "append":
+        x = _randn(g, rows, 2 * kv * dh)
+        x[:, ::97] *= 4.0
+        x = x.to(dt)
+        where = torch.tensor(_touched(case), device="cuda")
+        state.update(k=x[:, :kv * dh], v=x[:, kv * dh:], hit=table[where[:, 0], where[:, 1]].long())
+    else:
+        state.update(q=(1.3 * _randn(g, rows, case["heads"] * dh)).to(dt))
+        if own:
+            from paper_2602_07899_amd import tlq
+            state["ws"] = torch.empty(max(256, tlq.kv_attention_workspace_bytes(
+                rows, case["heads"], _batch(state), _cache(state))), dtype=torch.uint8, device="cuda")
+    return state
+
+
+# ------------------------------------------------------------------ the framework's calls
+def _params(case):
+    from paper_2602_07899_amd import tlq
+    d = tlq.BF16 if case["dt"] == "bf16" else tlq.F16
+    return tlq.params(x_dtype=d, yref_dtype=d)
+
+
+def _batch(state):
+    from paper_2602_07899_amd import tlq
+    return tlq.kv_batch(state["cu"], state["dlens"], state["table"], max_new=max(state["new"]), max_len=max(state["lens"]))
+
+
+def _cache(state):
+    from paper_2602_07899_amd import tlq
+    return tlq.kv_cache(state["kc"], state["ks"], state["vc"], state["vs"])
+
+
+def _run_own(state):
+    from paper_2602_07899_amd import tlq
+    case = state["case"]
+    p = _params(case)
+    if case["kind"] == "linear":
+        x, n, ci, co = state["x"], case["n"], case["ci"], case["co"]
+        codes = torch.empty((n, _ld8(ci)), dtype=torch.int8, device=x.device)
+        step = torch.empty(n, dtype=torch.float32, device=x.device)
+        y = torch.empty((n, co + -co % 8), dtype=x.dtype, device=x.device)[:, :co]
+        tlq.row_codes(x, case["bits"], p, codes, step, factor=state["f"])
+        tlq.linear_i8(codes, step, state["w"], state["wstep"], ci, p, y)
+        return y
+    if case["kind"] == "rope":
+        nq, nk = case["heads"] * case["dh"], case["kv"] * case["dh"]
+        q, k = state["qkv"][:, :nq], state["qkv"][:, nq:nq + nk]
+        qo = torch.empty((case["n"], nq), dtype=q.dtype, device=q.device)
+        ko = torch.empty((case["n"], nk), dtype=q.dtype, device=q.device)
+        w = dict(wq=state["wq"], wk=state["wk"], eps=_EPS) if case["norm"] else dict(norm=False)
+        tlq.qk_norm_rope(q, k, case["dh"], state["pos"], state["inv"], p, qo, ko, interleaved=bool(case["pairs"]), **w)
+        return qo, ko
+    if case["kind"] == "append":
+        tlq.kv_append(state["k"], state["v"], _batch(state), _cache(state), p)
+        return _values(state)
+    out = torch.empty_like(state["q"])
+    tlq.kv_attention(state["q"], case["heads"], _batch(state), _cache(state), p, out, workspace=state["ws"])
+    return out
+
+
+def _values(state):
+    """What the pages that an append wrote stand for, and their steps."""
+    hit = state["hit"]
+    ks, vs = state["ks"][hit], state["vs"][hit]
+    return state["kc"][hit] * ks[:, :, None, None], state["vc"][hit] * vs[:, :, None, None], ks, vs
+
+
+# ------------------------------------------------------------------ the plain forms
+def run(state):
+    if own:
+        return _run_own(state)
+    return {"linear": _linear, "rope": _rope, "append": _append, "attention": _attention}[state["case"]["kind"]](state)
+
+
+def _step(most, top):
+    """One step of a grid, a true quotient in 32 bits (by a plain number the library multiplies with its reciprocal)."""
+    return most.clamp_min(_FLOOR) / torch.full_like(most, top)
+
+
+def _linear(state):
+    case = state["case"]
+    top = float(2 ** (case["bits"] - 1) - 1)
+    xt = state["x"].float() * state["f"]
+    step = _step(xt.abs().amax(1), top)
+    codes = torch.round(xt / step[:, None]).clamp(-top - 1.0, top)
+    w = state["w"][:, :case["ci"]].float()
+    return ((codes @ w.t()) * state["wstep"] * step[:, None]).to(state["x"].dtype)
+
+
+def _rope(state):
+    case = state["case"]
+    dh, half = case["dh"], case["rot"] // 2
+    angle = state["pos"].double()[:, None] * state["inv"]
+    cos, sin = torch.cos(angle).float()[:, None, :], torch.sin(angle).float()[:, None, :]
+
+    def one(x, w):
+        u = x.float().reshape(x.shape[0], -1, dh)
+        if case["norm"]:
+            u = u / torch.sqrt((u * u).mean(-1, keepdim=True) + _EPS) * w
+        if case["pairs"]:
+            a, b = u[..., 0:2 * half:2], u[..., 1:2 * half:2]
+            turned = torch.stack((a * cos - b * sin, b * cos + a * sin), -1).flatten(-2)
+        else:
+            a, b = u[..., :half], u[..., half:2 * half]
+            turned = torch.cat((a * cos - b * sin, b * cos + a * sin), -1)
+        return torch.cat((turned, u[..., 2 * half:]), -1).reshape(x.shape).to(x.dtype)
+    nq, nk = case["heads"] * dh, case["kv"] * dh
+    return one(state["qkv"][:, :nq], state["wq"]), one(state["qkv"][:, nq:nq + nk], state["wk"])
+
+
+def _append(state):
+    case = state["case"]
+    kv, dh, page = case["kv"], case["dh"], case["page"]
+    at = 0
+    for s, (a, n) in enumerate(zip(state["new"], state["lens"])):
+        rows = slice(at, at + a)
+        at += a
+        first, last = (n - a) // page, (n - 1) // page
+        old = (n - a) % page                         # tokens that the first page holds already
+        ids = state["table"][s, first:last + 1].long()
+        m = last - first + 1
+        for x, codes, steps, turned in ((state["k"], state["kc"], state["ks"], False), (state["v"], state["vc"], state["vs"], True)):
+            fresh = torch.zeros((m * page, kv, dh), dtype=torch.float32, device=x.device)
+            fresh[old:old + a] = x[rows].float().reshape(a, kv, dh)
+            fresh = fresh.reshape(m, page, kv, dh).transpose(1, 2)
+            step = _step(fresh.abs().amax((2, 3)), 127.0)
+            before, was = codes[ids], steps[ids]
+            if turned:
+                before = before.transpose(2, 3)
+            if old:
+                step[0] = torch.maximum(step[0], was[0])
+            q = torch.round(fresh / step[:, :, None, None]).clamp(-127, 127)
+            keep = torch.arange(m * page, device=x.device).reshape(m, 1, page, 1)
+            if old:
+                again = torch.round(before.float() * (was / step)[:, :, None, None])
+                q = torch.where(keep < old, again, q)
+            q = torch.where(keep >= old + a, before.float(), q).to(torch.int8)
+            codes[ids] = q.transpose(2, 3) if turned else q
+            steps[ids] = step
+    return _values(state)
+
+
+def _attention(state):
+    case, q = state["case"], state["q"]
+    heads, kv, dh = case["heads"], case["kv"], case["dh"]
+    group, scale = heads // kv, dh ** -0.5
+    out, at = torch.empty_like(q), 0
+    for s, (a, n) in enumerate(zip(state["new"], state["lens"])):
+        ids = state["table"][s, :-(-n // case["page"])].long()
+        k = (state["kc"][ids].float() * state["ks"][ids][:, :, None, None]).permute(1, 0, 2, 3).reshape(kv, -1, dh)[:, :n]
+        v = (state["vc"][ids].float() * state["vs"][ids][:, :, None, None]).permute(1, 0, 3, 2).reshape(kv, -1, dh)[:, :n]
+        x = q[at:at + a].float().reshape(a, kv, group, dh).permute(1, 0, 2, 3).reshape(kv, a * group, dh)
+        sc = torch.bmm(x, k.transpose(1, 2).contiguous()).reshape(kv, a, group, n) * scale
+        if a > 1:
+            ahead = torch.arange(n, device=q.device)[None, :] > torch.arange(n - a, n, device=q.device)[:, None]
+            sc.masked_fill_(ahead[None, :, None, :], -math.inf)
+        e = torch.exp(sc - sc.amax(-1, keepdim=True))
+        o = torch.bmm(e.reshape(kv, a * group, n), v.contiguous()).reshape(kv, a, group, dh) / e.sum(-1, keepdim=True)
+        out[at:at + a] = o.permute(1, 0, 2, 3).reshape(a, heads * dh).to(q.dtype)
+        at += a
+    return out
+
+
+# ------------------------------------------------------------------ the definitions in 64 bits
+def exact(case, seed):
+    state = prepare(case, seed)
+    k = case["kind"]
+    if k == "linear":
+        top = 2.0 ** (case["bits"] - 1) - 1.0
+        # (the product with the factors is rounded to 32 bits by definition: whole codes hang on it)
+        xt = (state["x"].float() * state["f"]).double()
+        step = torch.maximum(xt.abs().max(dim=1, keepdim=True).values, torch.tensor(_FLOOR, dtype=torch.float64, device="cuda")) / top
+        codes = torch.clamp(torch.round(xt / step), -(top + 1.0), top)
+        y = torch.empty((case["n"], case["co"]), dtype=torch.float64, device="cuda")
+        for o in range(0, case["co"], 2048):
+            wd = state["w"][o:o + 2048, :case["ci"]].double() * state["wstep"][o:o + 2048, None].double()
+            y[:, o:o + 2048] = torch.matmul(codes * step, wd.t().contiguous())
+        return y
+    if k == "rope":
+        dh, half, res = case["dh"], case["rot"] // 2, []
+        theta = torch.outer(state["pos"].double(), state["inv"])
+        turn = torch.polar(torch.ones_like(theta), theta)[:, None]          # e^(i theta)
+        first = 0
+        for count, w in ((case["heads"], state["wq"]), (case["kv"], state["wk"])):
+            u = state["qkv"][:, first:first + count * dh].double().view(-1, count, dh)
+            first += count * dh
+            if case["norm"]:
+                u = u * torch.rsqrt(u.pow(2).sum(-1, keepdim=True) / dh + _EPS) * w.double()
+            o = u.clone()
+            low, high = (slice(0, 2 * half, 2), slice(1, 2 * half, 2)) if case["pairs"] else (slice(0, half), slice(half, 2 * half))
+            z = torch.complex(u[..., low].contiguous(), u[..., high].contiguous()) * turn
+            o[..., low], o[..., high] = z.real, z.imag
+            res.append(o.reshape(-1, count * dh))
+        return tuple(res)
+    page, table = case["page"], state["table"].cpu()
+    if k == "append":
+        kv, dh = case["kv"], case["dh"]
+        kvals, vvals, ksteps, vsteps = [], [], [], []
+        start = [sum(state["new"][:i]) for i in range(case["seqs"])]
+        for s, p in _touched(case):
+            a, n, pg = state["new"][s], state["lens"][s], int(table[s, p])
+            begin = n - a                                     # position of the first new token
+            lo, hi = max(begin, p * page), min(n, (p + 1) * page)
+            for x, c, st, vals, steps, axis in ((state["k"], state["kc"], state["ks"], kvals, ksteps, 1),
+                                                (state["v"], state["vc"], state["vs"], vvals, vsteps, 2)):
+                # (steps, quotients and their products are numbers of 32 bits by definition, as in every quantiser of
+                # the library: whole codes hang on them)
+                fresh = x[start[s] + lo - begin:start[s] + hi - begin].float().view(hi - lo, kv, dh).permute(1, 0, 2)
+                most = torch.clamp(fresh.abs().flatten(1).max(dim=1).values, min=_FLOOR)
+                step = torch.div(most, torch.tensor([127.0], device="cuda"))
+                code = c[pg].double() if axis == 1 else c[pg].double().mT.contiguous()
+                held = lo - p * page
+                if held:
+                    was = st[pg]
+                    step = torch.where(was > step, was, step)
+                    code[:, :held] = torch.round(code[:, :held].float() * torch.div(was, step).view(kv, 1, 1)).double()
+                code[:, held:hi - p * page] = torch.round(torch.div(fresh, step.view(kv, 1, 1))).double()
+                step = step.double()
+                val = code * step[:, None, None]
+                vals.append(val if axis == 1 else val.mT)
+                steps.append(step)
+        return torch.stack(kvals), torch.stack(vvals), torch.stack(ksteps), torch.stack(vsteps)
+    heads, dh = case["heads"], case["dh"]
+    group = heads // case["kv"]
+    out, at = torch.empty(tuple(state["q"].shape), dtype=torch.float64, device="cuda"), 0
+    for s, (a, n) in enumerate(zip(state["new"], state["lens"])):
+        ids = table[s, :-(-n // page)].long().cuda()
+        q = state["q"][at:at + a].double().view(a, heads, dh)
+        seen = torch.tril(torch.ones((a, n), dtype=torch.bool, device="cuda"), diagonal=n - a)
+        for h in range(case["kv"]):
+            key = (state["kc"][ids, h].double() * state["ks"][ids, h].double()[:, None, None]).reshape(-1, dh)[:n]
+            val = (state["vc"][ids, h].double() * state["vs"][ids, h].double()[:, None, None]).mT.reshape(-1, dh)[:n]
+            for j in range(group):
+                z = torch.matmul(q[:, h * group + j], key.mT.contiguous()) / math.sqrt(dh)
+                z = torch.where(seen, z, torch.full_like(z, -math.inf))
+                w = torch.exp(z - torch.logsumexp(z, dim=1, keepdim=True))
+                c = (h * group + j) * dh
+                out[at:at + a, c:c + dh] = torch.matmul(w, val)
+        at += a
+    return out
