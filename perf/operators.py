@@ -3,8 +3,8 @@
 
 A case is one dict of plain values; `kind` names the operator:
 
-  linear     tokens to 8-bit codes with a step for each token (`row_codes`), times stored 8-bit weights
-             with a step for each output (`linear_i8`):
+  linear     tokens to codes of up to 8 bits with a step for each token, times stored 8-bit weights with a
+             step for each output (`linear_i8`; the weights come from `row_codes`):
                xt = x * f,  step_t = max(max_c |xt|, 1e-5) / 127,  code = clip(rint(xt / step_t)),
                y[t, o] = step_t * step_o * sum_c code[t, c] * wcode[o, c]
   rope       queries and keys normalised for each head and rotated by their position (`qk_norm_rope`):
@@ -173,7 +173,11 @@ def prepare(case, seed):
         step = w.abs().amax(1).clamp_min(_FLOOR) / 127.0
         codes = torch.zeros((co, _ld8(ci)), dtype=torch.int8, device="cuda")
         codes[:, :ci] = torch.round(w / step[:, None]).clamp(-128, 127).to(torch.int8)
-        return dict(case=case, x=x.to(dt), f=1.0 / s, w=codes, wstep=step)
+        state = dict(case=case, x=x.to(dt), f=1.0 / s, w=codes, wstep=step)
+        if own:
+            from paper_2602_07899_amd import tlq
+            state["ws"] = torch.empty(max(256, tlq.linear_i8_workspace_bytes(n, ci)), dtype=torch.uint8, device="cuda")
+        return state
     if k == "rope":
         n, e = case["n"], (case["heads"] + case["kv"]) * case["dh"]
         qkv = _randn(g, n, e + case["kv"] * case["dh"]).to(dt)       # values behind queries and keys, as a projection writes them
@@ -222,7 +226,7 @@ def prepare(case, seed):
 def _params(case):
     from paper_2602_07899_amd import tlq
     d = tlq.BF16 if case["dt"] == "bf16" else tlq.F16
-    return tlq.params(x_dtype=d, yref_dtype=d)
+    return tlq.params(act_bits=case.get("bits", 0), x_dtype=d, yref_dtype=d)
 
 
 def _batch(state):
@@ -240,12 +244,9 @@ def _run_own(state):
     case = state["case"]
     p = _params(case)
     if case["kind"] == "linear":
-        x, n, ci, co = state["x"], case["n"], case["ci"], case["co"]
-        codes = torch.empty((n, _ld8(ci)), dtype=torch.int8, device=x.device)
-        step = torch.empty(n, dtype=torch.float32, device=x.device)
-        y = torch.empty((n, co + -co % 8), dtype=x.dtype, device=x.device)[:, :co]
-        tlq.row_codes(x, case["bits"], p, codes, step, factor=state["f"])
-        tlq.linear_i8(codes, step, state["w"], state["wstep"], ci, p, y)
+        x, co = state["x"], case["co"]
+        y = torch.empty((case["n"], co + -co % 8), dtype=x.dtype, device=x.device)[:, :co]
+        tlq.linear_i8(x, state["w"], state["wstep"], p, y, factor=state["f"], workspace=state["ws"])
         return y
     if case["kind"] == "rope":
         nq, nk = case["heads"] * case["dh"], case["kv"] * case["dh"]
