@@ -329,6 +329,92 @@ tlq_status tlq_silu_mul(const void* G, int64_t ldg, const void* U, int64_t ldu, 
 tlq_status tlq_residual_add(const void* H, int64_t ldh, const void* Z, int64_t ldz, int64_t n_tok,
                             int64_t c, const tlq_params* p, void* Out, int64_t ldo, void* stream);
 
+/* ---- a decoder block that runs in 8 bits: what the searched setting act_bits <= 8, group = 0, symmetric = 1
+ * (Sec. 4.1: per-token activations, per-channel symmetric weights) is searched for.  Forward only; forms for single
+ * tokens and for whole prompts; no call synchronises, allocates or keeps anything, all can be captured into a graph.
+ *
+ * tlq_row_codes: rows to signed codes with one step a row, the quantiser of Q_a above and of Q_w with group = 0,
+ * symmetric = 1 alike (float arithmetic, one rounding an operation, half to even):
+ *   xt = x * factor[c];  step_r = max(max_c |xt|, 1e-5) / (2^(bits-1) - 1);
+ *   code = clip(rint(xt / step_r), -2^(bits-1), 2^(bits-1) - 1).
+ * X [n, c] x_dtype; factor: float [c], 16-byte aligned, or NULL (ones) - the searched scales for weight rows, their
+ * reciprocals for tokens; bits 2..8; codes: out int8 [n, ldc], ldc (bytes) a multiple of 16 and at least c rounded up
+ * to 128 (zeros are written behind c up to there, nothing beyond); 16-byte aligned; steps: out float [n].  A NaN has the lowest code and no
+ * part in the step; an infinity makes the step infinite. */
+tlq_status tlq_row_codes(const void* X, int64_t n, int64_t c, int64_t ldx, const float* factor, int32_t bits,
+                         const tlq_params* p, int8_t* codes, int64_t ldc, float* steps, void* stream);
+/* tlq_linear_i8: Y[t,o] = step_t * w_step[o] * sum_c code[t,c] * w_codes[o,c], with the codes and steps that
+ * tlq_row_codes gives X (factor as there, bits = p->act_bits, TLQ_ERR_UNSUPPORTED if that is 0); the sums are exact.
+ * w_codes int8 [c_out, ldw] and w_steps float [c_out] as tlq_row_codes writes them (the zeros behind c_in up to the next
+ * multiple of 128 are read; w_steps 16-byte aligned); c_in a multiple of 8, at most 65536; ldw < 2^22.
+ * Y [n_tok, c_out] yref_dtype, 16-byte aligned, ldy a multiple of 8 (4 for float).  Workspace from the query. */
+size_t tlq_linear_i8_workspace_bytes(int64_t n_tok, int64_t c_in);
+tlq_status tlq_linear_i8(const void* X, int64_t n_tok, int64_t c_in, int64_t ldx, const float* factor,
+                         const int8_t* w_codes, int64_t c_out, int64_t ldw, const float* w_steps, const tlq_params* p,
+                         void* Y, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
+
+/* tlq_qk_norm_rope: queries and keys normalised for each head (norm = 1; 0: not) and rotated by their position:
+ *   u = x / sqrt(mean_d x^2 + eps) * w[d];  angle = pos[t] * inv_freq[i] (in double), i < rot / 2;
+ *   (u_a, u_b) -> (u_a cos - u_b sin, u_b cos + u_a sin), (a, b) = (i, i + rot/2), or (2i, 2i+1) with interleaved = 1;
+ * d >= rot is not rotated.  Float arithmetic, one rounding to x_dtype at the end.
+ * Q [n_tok, n_heads * head_dim], K [n_tok, n_kv_heads * head_dim] x_dtype, 16-byte aligned, strides multiples of 8
+ * (both may be column slices of one matrix); head_dim 64, 128 or 256 (TLQ_ERR_UNSUPPORTED otherwise); rot a multiple
+ * of 16, 0 <= rot <= head_dim; pos int32 [n_tok] (any sign), inv_freq double [rot/2]; wq, wk float [head_dim], 16-byte
+ * aligned, or NULL (ones; both have to be NULL without norm).  Q_out may be Q with the same stride, K_out likewise K; no
+ * other overlap. */
+tlq_status tlq_qk_norm_rope(const void* Q, int64_t ldq, int32_t n_heads, const void* K, int64_t ldk, int32_t n_kv_heads,
+                            int64_t n_tok, int32_t head_dim, int32_t rot, int32_t interleaved, int32_t norm, float eps,
+                            const float* wq, const float* wk, const int32_t* pos, const double* inv_freq,
+                            const tlq_params* p, void* Q_out, int64_t ldqo, void* K_out, int64_t ldko, void* stream);
+
+/* ---- keys and values of earlier tokens in 8 bits, in pages of `page` tokens with one step for each page and head.
+ * A cache is a pool of n_pages pages for n_kv_heads heads:
+ *   k int8 [n_pages, n_kv_heads, page, head_dim], k_step float [n_pages, n_kv_heads]: key = code * step;
+ *   v int8 [n_pages, n_kv_heads, head_dim, page] (the tokens of a channel are contiguous), v_step likewise.
+ * k and v 16-byte aligned; head_dim 64 or 128, page 16, 32, 64, 128 or 256 (TLQ_ERR_UNSUPPORTED otherwise).
+ * A batch is n_seq sequences whose lengths live on the device: sequence s has lens[s] tokens, the newest of which are the
+ * rows cu_new[s] .. cu_new[s+1]-1 of the call's matrices (cu_new int32 [n_seq + 1], ascending from 0; rows behind the last
+ * sequence are neither read nor written); token j of it lives in page table[s * ld_table + j / page], j < max_pages * page.
+ * max_new and max_len are upper bounds of a sequence's new tokens and of its length; launches are sized by them.
+ * Device values are never trusted with an address: an entry of the table outside [0, n_pages) stands for a page of tokens
+ * that do not exist (nothing is written, no query sees them), cu_new is held to [0, n_tok], new tokens beyond lens[s],
+ * beyond the table or beyond the bounds are left out. */
+typedef struct tlq_kv_cache {
+  uint32_t struct_size; /* = sizeof(tlq_kv_cache) */
+  int32_t n_kv_heads, head_dim, page;
+  int64_t n_pages;
+  int8_t* k; float* k_step;
+  int8_t* v; float* v_step;
+} tlq_kv_cache;
+typedef struct tlq_kv_batch {
+  uint32_t struct_size; /* = sizeof(tlq_kv_batch) */
+  int32_t n_seq;        /* 1 .. 65535 */
+  const int32_t* cu_new; const int32_t* lens; const int32_t* table;
+  int64_t ld_table;     /* entries between the table's rows, >= max_pages */
+  int32_t max_pages, max_new, max_len;
+  int32_t reserved;     /* 0 */
+} tlq_kv_batch;
+/* tlq_kv_append: the new tokens' keys and values as codes.  For a page and head, over its new tokens (float arithmetic):
+ *   step = max(max |x|, 1e-5) / 127, and at least the page's step if it held tokens of the sequence before;
+ *   code = clip(rint(x / step), -127, 127); codes held before: rint(code * (old step / step)).
+ * Infinities count as +-127 and NaN as 0, neither has a part in the step.  Codes behind a sequence's last token stay
+ * as they were.  K, V [n_tok, n_kv_heads * head_dim] x_dtype, 16-byte aligned, strides multiples of 8.  Two sequences may
+ * share pages that the call does not write; a page in which two sequences of one call have new tokens ends up undefined. */
+tlq_status tlq_kv_append(const void* K, int64_t ldk, const void* V, int64_t ldv, int64_t n_tok, const tlq_kv_batch* b,
+                         const tlq_kv_cache* c, const tlq_params* p, void* stream);
+/* tlq_kv_attention: Out[r, h] = sum_{j <= pos(r)} softmax_j(scale * q_r . key_j) value_j, head h with the keys of head
+ * h / (n_heads / n_kv_heads); row r of sequence s is its token pos(r) = lens[s] - (cu_new[s+1] - cu_new[s]) + r - cu_new[s].
+ * scale: any finite number, 0 = 1 / sqrt(head_dim).  A row that sees no token gives zeros; a query that is not finite
+ * makes its own row undefined and no other.  Scores, softmax and sums are
+ * float; the matrix products take codes as they are, queries exactly (bf16 ones times a power of two of their row) and
+ * probabilities times the page's step in fp16 with the largest at 2^15; Out is rounded to x_dtype.
+ * Q, Out [n_tok, n_heads * head_dim] x_dtype, 16-byte aligned, strides multiples of 8; n_heads a multiple of n_kv_heads.
+ * The workspace query reads sizes only, no pointer; the result does not depend on the workspace's contents. */
+size_t tlq_kv_attention_workspace_bytes(int64_t n_tok, int32_t n_heads, const tlq_kv_batch* b, const tlq_kv_cache* c);
+tlq_status tlq_kv_attention(const void* Q, int64_t ldq, int64_t n_tok, int32_t n_heads, float scale, const tlq_kv_batch* b,
+                            const tlq_kv_cache* c, const tlq_params* p, void* Out, int64_t ldo, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
 /* ---- host-side self check (no GPU work, no device memory): walks the block -> tile map that
  * the contraction kernels (S3/S4, f_fp, S6) would use for this problem shape, in both of its
  * orders (candidates inside every patch row / candidate-outermost), both patch shapes and all tile

@@ -85,6 +85,8 @@ bool use_int8(const tlq_params* p, int64_t c_in) {
   return p->act_bits != 0 && (p->group == 0 || p->group == c_in) && c_in >= 72 && c_in <= 16384 &&
          (p->symmetric || p->bits <= 7);
 }
+// tlq_linear_i8: rows of at most this many codes (the sums stay below 2^31), and tokens up to which the kernels for few are taken
+constexpr int64_t kMaxLinearI8 = 65536, kLinearFew = 64;
 int64_t int8_row(int64_t c_in) { return (int64_t)align_up((size_t)c_in, 128); }
 
 struct SearchPlan {
@@ -853,6 +855,136 @@ tlq_status tlq_silu_mul(const void* G, int64_t ldg, const void* U, int64_t ldu, 
 tlq_status tlq_residual_add(const void* H, int64_t ldh, const void* Z, int64_t ldz, int64_t n_tok,
                             int64_t c, const tlq_params* p, void* Out, int64_t ldo, void* stream) {
   return pairwise(1, H, ldh, Z, ldz, n_tok, c, p, Out, ldo, stream);
+}
+
+
+// ------------------------------------------------------------ a decoder block in 8 bits
+tlq_status tlq_row_codes(const void* X, int64_t n, int64_t c, int64_t ldx, const float* factor, int32_t bits,
+                         const tlq_params* p, int8_t* codes, int64_t ldc, float* steps, void* stream) {
+  if (!X || !codes || !steps) return TLQ_ERR_NULL;
+  TLQ_TRY(check_params(p));
+  if (bits < 2 || bits > 8) return TLQ_ERR_UNSUPPORTED;
+  if (!dims_ok(n, c, ldx) || (c % 8) != 0 || ldc < int8_row(c) || ldc >= (1LL << 31)) return TLQ_ERR_SHAPE;
+  if (!mat16_aligned(X, ldx) || !aligned(codes, 16) || (ldc % 16) != 0 || (factor && !aligned(factor, 16)) || !aligned(steps, 4))
+    return TLQ_ERR_ALIGN;
+  return hip_status(launch_act_quant(X, n, c, ldx, p->x_dtype == TLQ_BF16, factor, 0, 1, bits, codes, steps,
+                                     (hipStream_t)stream, ldc));
+}
+
+size_t tlq_linear_i8_workspace_bytes(int64_t n_tok, int64_t c_in) {
+  if (n_tok <= 0 || c_in <= 0 || n_tok >= (1LL << 31) || c_in > kMaxLinearI8) return 0;
+  return align_up((size_t)n_tok * int8_row(c_in), 256) + align_up((size_t)n_tok * sizeof(float), 256);
+}
+
+tlq_status tlq_linear_i8(const void* X, int64_t n_tok, int64_t c_in, int64_t ldx, const float* factor,
+                         const int8_t* w_codes, int64_t c_out, int64_t ldw, const float* w_steps, const tlq_params* p,
+                         void* Y, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!X || !w_codes || !w_steps || !Y) return TLQ_ERR_NULL;
+  TLQ_TRY(check_params(p));
+  if (p->act_bits == 0 || c_in > kMaxLinearI8) return TLQ_ERR_UNSUPPORTED;
+  if (!dims_ok(n_tok, c_in, ldx) || (c_in % 8) != 0 || !dims_ok(c_out, int8_row(c_in), ldw) || ldw >= (1LL << 22) ||
+      !dims_ok(n_tok, c_out, ldy))
+    return TLQ_ERR_SHAPE;
+  if (!mat16_aligned(X, ldx) || !aligned(w_codes, 16) || (ldw % 16) != 0 || !aligned(w_steps, 16) ||
+      (factor && !aligned(factor, 16)) || !mat_aligned(Y, ldy, p->yref_dtype))
+    return TLQ_ERR_ALIGN;
+  TLQ_TRY(check_ws(workspace, workspace_bytes, tlq_linear_i8_workspace_bytes(n_tok, c_in)));
+  hipStream_t st = (hipStream_t)stream;
+  Carver c(workspace);
+  const int64_t ld8 = int8_row(c_in);
+  int8_t* codes = c.take<int8_t>((size_t)n_tok * ld8);
+  float* steps = c.take<float>((size_t)n_tok);
+  TLQ_HIP(launch_act_quant(X, n_tok, c_in, ldx, p->x_dtype == TLQ_BF16, factor, 0, 1, p->act_bits, codes, steps, st, ld8));
+  if (n_tok <= kLinearFew)
+    return hip_status(launch_linear_few({codes, n_tok, ld8, steps, w_codes, c_out, ldw, ld8, w_steps, Y, ldy, p->yref_dtype}, st));
+  GemmArgs g{};
+  g.X = codes; g.n_tok = n_tok; g.tok_scale = steps; g.Wh = w_codes; g.c_out = c_out; g.n_cand = 1; g.row_scale = w_steps;
+  g.i8_k = c_in; g.c_in = g.ldx = ld8 / 2; g.ldw = ldw / 2;      // (in units of 16 bits)
+  g.Yout = Y; g.ldo = ldy; g.yout_dtype = p->yref_dtype;
+  g.wide_patch = true;
+  g.tile() = gemm_tile(g, kTileAll, INT64_MAX);
+  return hip_status(launch_gemm_store(g, st));
+}
+
+tlq_status tlq_qk_norm_rope(const void* Q, int64_t ldq, int32_t n_heads, const void* K, int64_t ldk, int32_t n_kv_heads,
+                            int64_t n_tok, int32_t head_dim, int32_t rot, int32_t interleaved, int32_t norm, float eps,
+                            const float* wq, const float* wk, const int32_t* pos, const double* inv_freq,
+                            const tlq_params* p, void* Q_out, int64_t ldqo, void* K_out, int64_t ldko, void* stream) {
+  if (!Q || !K || !Q_out || !K_out || !pos || (!inv_freq && rot > 0)) return TLQ_ERR_NULL;
+  TLQ_TRY(check_params(p));
+  if ((head_dim != 64 && head_dim != 128 && head_dim != 256) || (interleaved != 0 && interleaved != 1) ||
+      (norm != 0 && norm != 1) || (norm == 0 && (wq || wk)) || !(eps >= 0.0f) || eps > 3.0e38f)
+    return TLQ_ERR_UNSUPPORTED;
+  if (n_tok <= 0 || n_tok >= (1LL << 31) || n_heads <= 0 || n_heads > 65535 || n_kv_heads <= 0 || n_kv_heads > 65535 || rot < 0 ||
+      rot > head_dim || (rot % 16) != 0)
+    return TLQ_ERR_SHAPE;
+  const int64_t wide = (int64_t)n_heads * head_dim, narrow = (int64_t)n_kv_heads * head_dim;
+  if (ldq < wide || ldqo < wide || ldk < narrow || ldko < narrow) return TLQ_ERR_SHAPE;
+  if (!mat16_aligned(Q, ldq) || !mat16_aligned(K, ldk) || !mat16_aligned(Q_out, ldqo) || !mat16_aligned(K_out, ldko) ||
+      (wq && !aligned(wq, 16)) || (wk && !aligned(wk, 16)) || !aligned(pos, 4) || !aligned(inv_freq, 8))
+    return TLQ_ERR_ALIGN;
+  return hip_status(launch_qk_norm_rope({Q, K, ldq, ldk, n_heads, n_kv_heads, n_tok, head_dim, rot, interleaved != 0, norm != 0,
+                                         p->x_dtype == TLQ_BF16, eps, wq, wk, pos, inv_freq, Q_out, K_out, ldqo, ldko},
+                                        (hipStream_t)stream));
+}
+
+// sizes of a cache and a batch (no pointer); then the rest
+static tlq_status check_kv_sizes(const tlq_kv_batch* b, const tlq_kv_cache* c) {
+  if (!b || !c) return TLQ_ERR_NULL;
+  if (b->struct_size != sizeof(tlq_kv_batch) || c->struct_size != sizeof(tlq_kv_cache) || b->reserved != 0) return TLQ_ERR_UNSUPPORTED;
+  if (c->head_dim != 64 && c->head_dim != 128) return TLQ_ERR_UNSUPPORTED;
+  if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128 && c->page != 256) return TLQ_ERR_UNSUPPORTED;
+  if (c->n_kv_heads <= 0 || c->n_kv_heads > 65535 || c->n_pages <= 0 || c->n_pages >= (1LL << 31) || b->n_seq <= 0 ||
+      b->n_seq > 65535 || b->max_pages <= 0 || b->ld_table < b->max_pages || b->max_new <= 0 || b->max_len < b->max_new ||
+      b->max_len > (1 << 30))
+    return TLQ_ERR_SHAPE;
+  return TLQ_OK;
+}
+static tlq_status check_kv(const tlq_kv_batch* b, const tlq_kv_cache* c) {
+  TLQ_TRY(check_kv_sizes(b, c));
+  if (!b->cu_new || !b->lens || !b->table || !c->k || !c->k_step || !c->v || !c->v_step) return TLQ_ERR_NULL;
+  if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->k_step, 4) || !aligned(c->v_step, 4) || !aligned(b->cu_new, 4) ||
+      !aligned(b->lens, 4) || !aligned(b->table, 4))
+    return TLQ_ERR_ALIGN;
+  return TLQ_OK;
+}
+
+tlq_status tlq_kv_append(const void* K, int64_t ldk, const void* V, int64_t ldv, int64_t n_tok, const tlq_kv_batch* b,
+                         const tlq_kv_cache* c, const tlq_params* p, void* stream) {
+  if (!K || !V) return TLQ_ERR_NULL;
+  TLQ_TRY(check_params(p));
+  TLQ_TRY(check_kv(b, c));
+  const int64_t width = (int64_t)c->n_kv_heads * c->head_dim;
+  if (n_tok <= 0 || n_tok >= (1LL << 31) || ldk < width || ldv < width) return TLQ_ERR_SHAPE;
+  if (!mat16_aligned(K, ldk) || !mat16_aligned(V, ldv)) return TLQ_ERR_ALIGN;
+  return hip_status(launch_kv_append(K, ldk, V, ldv, n_tok, *b, *c, p->x_dtype == TLQ_BF16, (hipStream_t)stream));
+}
+
+static tlq_status check_kv_heads(int64_t n_tok, int32_t n_heads, const tlq_kv_cache* c) {
+  if (n_tok <= 0 || n_tok >= (1LL << 31) || n_heads <= 0 || n_heads > 65535 || (n_heads % c->n_kv_heads) != 0) return TLQ_ERR_SHAPE;
+  return TLQ_OK;
+}
+
+size_t tlq_kv_attention_workspace_bytes(int64_t n_tok, int32_t n_heads, const tlq_kv_batch* b, const tlq_kv_cache* c) {
+  if (check_kv_sizes(b, c) != TLQ_OK || check_kv_heads(n_tok, n_heads, c) != TLQ_OK) return 0;
+  return kv_attention_workspace(n_tok, n_heads, *b, *c);
+}
+
+tlq_status tlq_kv_attention(const void* Q, int64_t ldq, int64_t n_tok, int32_t n_heads, float scale, const tlq_kv_batch* b,
+                            const tlq_kv_cache* c, const tlq_params* p, void* Out, int64_t ldo, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+  if (!Q || !Out) return TLQ_ERR_NULL;
+  TLQ_TRY(check_params(p));
+  TLQ_TRY(check_kv(b, c));
+  TLQ_TRY(check_kv_heads(n_tok, n_heads, c));
+  if (!(scale - scale == 0.0f)) return TLQ_ERR_UNSUPPORTED;
+  const int64_t width = (int64_t)n_heads * c->head_dim;
+  if (ldq < width || ldo < width) return TLQ_ERR_SHAPE;
+  if (!mat16_aligned(Q, ldq) || !mat16_aligned(Out, ldo)) return TLQ_ERR_ALIGN;
+  TLQ_TRY(check_ws(workspace, workspace_bytes, kv_attention_workspace(n_tok, n_heads, *b, *c)));
+  if (scale == 0.0f) scale = c->head_dim == 128 ? 0.08838834764831845f : 0.125f;
+  return hip_status(launch_kv_attention(Q, ldq, n_tok, n_heads, scale, *b, *c, p->x_dtype == TLQ_BF16, Out, ldo, workspace,
+                                        (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -254,6 +254,30 @@ hipError_t launch_rmsnorm_mul(const void* Z, int64_t ldz, const void* Zb, int64_
                               int64_t c, bool bf16, const float* m_a, const float* m_b, int period,
                               int split, void* out, int64_t ldo, hipStream_t stream);
 
+// products of few tokens' codes with stored codes (linear.hip); launch_gemm_store has the others.  K = row length in codes, a multiple of 128
+struct LinearI8Args {
+  const int8_t* xc; int64_t n_tok, ldx; const float* xs;    // token codes and steps
+  const int8_t* wc; int64_t c_out, ldw, K; const float* ws;
+  void* Y; int64_t ldy; int ydt;
+};
+hipError_t launch_linear_few(const LinearI8Args& a, hipStream_t stream);
+
+// queries and keys of a decoder block (rope.hip)
+struct QkRopeArgs {
+  const void *Q, *K; int64_t ldq, ldk; int n_heads, n_kv_heads; int64_t n_tok;
+  int head_dim, rot; bool interleaved, norm, bf16; float eps;
+  const float *wq, *wk; const int32_t* pos; const double* inv_freq;
+  void *Qo, *Ko; int64_t ldqo, ldko;
+};
+hipError_t launch_qk_norm_rope(const QkRopeArgs& a, hipStream_t stream);
+
+// the 8-bit cache (kv_append.hip, kv_attention.hip)
+hipError_t launch_kv_append(const void* K, int64_t ldk, const void* V, int64_t ldv, int64_t n_tok, const tlq_kv_batch& b,
+                            const tlq_kv_cache& c, bool bf16, hipStream_t stream);
+size_t kv_attention_workspace(int64_t n_tok, int n_heads, const tlq_kv_batch& b, const tlq_kv_cache& c);
+hipError_t launch_kv_attention(const void* Q, int64_t ldq, int64_t n_tok, int n_heads, float scale, const tlq_kv_batch& b,
+                               const tlq_kv_cache& c, bool bf16, void* Out, int64_t ldo, void* workspace, hipStream_t stream);
+
 // decoder-block glue (block.hip): head width 128, rows in blocks of seq_len
 hipError_t launch_causal_attention(const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V,
                                    int64_t ldv, int64_t n_tok, int n_heads, int seq_len, bool bf16, void* O,

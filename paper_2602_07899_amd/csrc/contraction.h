@@ -931,9 +931,16 @@ __device__ __forceinline__ void gemm_dma_body(const GemmDev& a) {
     const float* rsc = a.row_scale + (int64_t)cand * a.row_scale_stride;
 #pragma unroll
     for (int i = 0; i < IA; ++i) {
-      const int64_t o = o0 + wo * WO + i * 16 + fq * 4;       // (the table's rows are whole groups of four)
-      const float4 rs = o < a.c_out ? *reinterpret_cast<const float4*>(rsc + o) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      const float r[4] = {rs.x, rs.y, rs.z, rs.w};
+      const int64_t o = o0 + wo * WO + i * 16 + fq * 4;
+      float r[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (o + 3 < a.c_out) {
+        const float4 rs = *reinterpret_cast<const float4*>(rsc + o);
+        r[0] = rs.x; r[1] = rs.y; r[2] = rs.z; r[3] = rs.w;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+          if (o + e < a.c_out) r[e] = rsc[o + e];
+      }
 #pragma unroll
       for (int j = 0; j < JB; ++j) {
         const i32x4 v = __builtin_bit_cast(i32x4, acc[i][j]);

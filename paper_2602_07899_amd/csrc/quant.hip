@@ -572,7 +572,7 @@ __device__ __forceinline__ void aq_load_tile(const uint16_t* __restrict__ X, int
   }
 }
 
-// INT: int8 codes in rows of ldc bytes (zeros behind c_in) instead of fp16 ones in rows of c_in.
+// INT: int8 codes in rows of ldc bytes (zeros behind c_in up to the next multiple of 128) instead of fp16 ones in rows of c_in.
 template <typename T, bool INT>
 __global__ __launch_bounds__(kAqWaves * 64) void act_quant_kernel(const uint16_t* __restrict__ X, int64_t n_tok, int64_t c_in,
                                                                   int64_t ldx, const float* __restrict__ inv_table,
@@ -635,12 +635,14 @@ __global__ __launch_bounds__(kAqWaves * 64) void act_quant_kernel(const uint16_t
   __syncthreads();
   for (int strip = wave; strip < strips; strip += nw) {
     const int64_t c = (int64_t)strip * kAqCols + lane * 8;
-    if (c >= (INT ? ldc : c_in)) continue;
+    if (c >= (INT ? (c_in + 127) / 128 * 128 : c_in)) continue;
     aq_load_tile<T>(X, n_tok, c_in, ldx, r0, c, x);
     for (int k = 0; k < nk; ++k) {
       if (inv_table && (!INT || c < c_in)) load8(inv_table + (int64_t)(k0 + k) * c_in + c, iv);
-      // (behind c_in any code will do, the weights are zeros there: a zero gives the code zero, unless the lane's last
-      // factor was infinite)
+      else if (INT && inv_table) {      // (behind c_in the codes are zeros whatever the lane's last factors were)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) iv[j] = 1.0f;
+      }
       const int64_t at = ((int64_t)(k0 + k) * n_tok + r0) * ldc + c;
 #pragma unroll
       for (int r = 0; r < kAqRows; ++r) {

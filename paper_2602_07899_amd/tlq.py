@@ -29,6 +29,19 @@ def params(bits=4, group=128, symmetric=0, act_bits=0, xstat_kind=0, x_dtype=F16
     return Params(C.sizeof(Params), bits, group, symmetric, act_bits, xstat_kind, x_dtype, yref_dtype)
 
 
+class KvCache(C.Structure):
+    """tlq_kv_cache; made by kv_cache()."""
+    _fields_ = [("struct_size", C.c_uint32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page", C.c_int32),
+                ("n_pages", C.c_int64), ("k", C.c_void_p), ("k_step", C.c_void_p), ("v", C.c_void_p), ("v_step", C.c_void_p)]
+
+
+class KvBatch(C.Structure):
+    """tlq_kv_batch; made by kv_batch()."""
+    _fields_ = [("struct_size", C.c_uint32), ("n_seq", C.c_int32), ("cu_new", C.c_void_p), ("lens", C.c_void_p),
+                ("table", C.c_void_p), ("ld_table", C.c_int64), ("max_pages", C.c_int32), ("max_new", C.c_int32),
+                ("max_len", C.c_int32), ("reserved", C.c_int32)]
+
+
 class TlqError(RuntimeError):
     def __init__(self, status, where):
         self.status = status
@@ -42,6 +55,9 @@ _I64 = C.c_int64
 _I32 = C.c_int32
 _SZ = C.c_size_t
 _PP = C.POINTER(Params)
+_F = C.c_float
+_PB = C.POINTER(KvBatch)
+_PC = C.POINTER(KvCache)
 
 _SIGNATURES = {
     "tlq_status_string": (C.c_char_p, [C.c_int]),
@@ -79,6 +95,14 @@ _SIGNATURES = {
     "tlq_causal_attention": (C.c_int, [_P, _I64, _P, _I64, _P, _I64, _I64, _I32, _I32, _I32, _PP, _P, _I64, _P]),
     "tlq_silu_mul": (C.c_int, [_P, _I64, _P, _I64, _I64, _I64, _PP, _P, _I64, _P]),
     "tlq_residual_add": (C.c_int, [_P, _I64, _P, _I64, _I64, _I64, _PP, _P, _I64, _P]),
+    "tlq_row_codes": (C.c_int, [_P, _I64, _I64, _I64, _P, _I32, _PP, _P, _I64, _P, _P]),
+    "tlq_linear_i8_workspace_bytes": (_SZ, [_I64, _I64]),
+    "tlq_linear_i8": (C.c_int, [_P, _I64, _I64, _I64, _P, _P, _I64, _I64, _P, _PP, _P, _I64, _P, _SZ, _P]),
+    "tlq_qk_norm_rope": (C.c_int, [_P, _I64, _I32, _P, _I64, _I32, _I64, _I32, _I32, _I32, _I32, _F, _P, _P, _P, _P, _PP,
+                                   _P, _I64, _P, _I64, _P]),
+    "tlq_kv_append": (C.c_int, [_P, _I64, _P, _I64, _I64, _PB, _PC, _PP, _P]),
+    "tlq_kv_attention_workspace_bytes": (_SZ, [_I64, _I32, _PB, _PC]),
+    "tlq_kv_attention": (C.c_int, [_P, _I64, _I64, _I32, _F, _PB, _PC, _PP, _P, _I64, _P, _SZ, _P]),
     "tlq_selftest_tile_map": (C.c_int64, [_I64, _I64, _I64, _I32, C.POINTER(C.c_int64)]),
     "tlq_profile_enable": (C.c_int, [C.c_int]),
     "tlq_profile_enabled": (C.c_int, []),
@@ -364,6 +388,134 @@ def residual_add(H, Z, p, Out):
     n, c = H.shape
     _check(lib().tlq_residual_add(_ptr(H), _ld(H), _ptr(Z), _ld(Z), n, c, C.byref(p), _ptr(Out), _ld(Out),
                                   _stream()), "tlq_residual_add")
+    return Out
+
+
+# ------------------------------------------------------------------ a decoder block in 8 bits
+def _expect(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _here(p, types, *tensors):
+    """The tensors are of the types that the call reads them as, and on the device whose stream it takes."""
+    import torch
+    here = None
+    for t, dt in zip(tensors, types):
+        if t is None:
+            continue
+        want = dt if not isinstance(dt, str) else (torch.float16, torch.bfloat16, torch.float32)[p.x_dtype if dt == "x" else p.yref_dtype]
+        if t.dtype != want:
+            raise ValueError(f"a tensor of {t.dtype} where {want} is read")
+        if here is None and t.is_cuda:
+            here = torch._C._cuda_getDevice()
+        if not t.is_cuda or t.get_device() != here:
+            raise ValueError("tensors have to be on the current device")
+
+
+def row_codes(X, bits, p, codes, steps, factor=None):
+    """Rows of X * factor as signed codes of `bits` bits (int8 [n, >= c rounded up to 128]) and steps (float [n])."""
+    import torch
+    n, c = X.shape
+    f32 = torch.float32
+    _here(p, ("x", torch.int8, f32, f32), X, codes, steps, factor)
+    _expect(codes.shape[0] == n and _ld(codes) >= codes.shape[1] >= -(-c // 128) * 128, "codes: n rows, zeros behind c up to a multiple of 128")
+    _expect(steps.numel() == n and steps.is_contiguous(), "one step a row")
+    _expect(factor is None or factor.numel() == c and factor.is_contiguous(), "one factor a channel")
+    _check(lib().tlq_row_codes(_ptr(X), n, c, _ld(X), _ptr(factor), bits, C.byref(p), _ptr(codes), _ld(codes), _ptr(steps),
+                               _stream()), "tlq_row_codes")
+
+
+def linear_i8_workspace_bytes(n_tok, c_in):
+    return int(lib().tlq_linear_i8_workspace_bytes(n_tok, c_in))
+
+
+def linear_i8(X, w_codes, w_steps, p, Y, factor=None, workspace=None):
+    """Y = step_t * step_o * codes(X * factor) . w_codes^T; the tokens' codes have p.act_bits bits."""
+    import torch
+    n, ci = X.shape
+    co = w_codes.shape[0]
+    f32 = torch.float32
+    _here(p, ("x", torch.int8, f32, "y", f32), X, w_codes, w_steps, Y, factor)
+    _expect(w_codes.shape[1] >= -(-ci // 128) * 128, "w_codes: rows with zeros behind c_in up to a multiple of 128")
+    _expect(w_steps.numel() == co and w_steps.is_contiguous(), "one step an output")
+    _expect(Y.shape == (n, co), "Y: [n_tok, c_out]")
+    _expect(factor is None or factor.numel() == ci and factor.is_contiguous(), "one factor a channel")
+    ws = workspace if workspace is not None else _ws(linear_i8_workspace_bytes(n, ci), X)
+    _check(lib().tlq_linear_i8(_ptr(X), n, ci, _ld(X), _ptr(factor), _ptr(w_codes), co, _ld(w_codes), _ptr(w_steps), C.byref(p),
+                               _ptr(Y), _ld(Y), _ptr(ws), ws.numel(), _stream()), "tlq_linear_i8")
+    return Y
+
+
+def qk_norm_rope(Q, K, head_dim, pos, inv_freq, p, Q_out, K_out, wq=None, wk=None, eps=1e-6, norm=True, interleaved=False):
+    """Heads of Q [n, heads * head_dim] and K normalised (unless norm is False) and the first 2 * len(inv_freq) channels of
+    each turned by pos * inv_freq."""
+    import torch
+    n = Q.shape[0]
+    f32 = torch.float32
+    _here(p, ("x", "x", "x", "x", torch.int32, torch.float64, f32, f32), Q, K, Q_out, K_out, pos, inv_freq, wq, wk)
+    _expect(K.shape[0] == n and Q_out.shape == Q.shape and K_out.shape == K.shape, "outputs of the inputs' shapes")
+    _expect(Q.shape[1] % head_dim == 0 and K.shape[1] % head_dim == 0, "whole heads")
+    _expect(pos.numel() == n and pos.is_contiguous() and (inv_freq is None or inv_freq.is_contiguous()), "one position a row")
+    _expect(all(w is None or (w.numel() == head_dim and w.is_contiguous()) for w in (wq, wk)), "one weight a channel of a head")
+    rot = 0 if inv_freq is None else 2 * inv_freq.numel()
+    _check(lib().tlq_qk_norm_rope(_ptr(Q), _ld(Q), Q.shape[1] // head_dim, _ptr(K), _ld(K), K.shape[1] // head_dim, n, head_dim,
+                                  rot, 1 if interleaved else 0, 1 if norm else 0, eps, _ptr(wq), _ptr(wk), _ptr(pos),
+                                  _ptr(inv_freq), C.byref(p), _ptr(Q_out), _ld(Q_out), _ptr(K_out), _ld(K_out), _stream()),
+           "tlq_qk_norm_rope")
+    return Q_out, K_out
+
+
+def kv_cache(k, k_step, v, v_step):
+    """The cache made of k int8 [n_pages, n_kv_heads, page, head_dim], v int8 [n_pages, n_kv_heads, head_dim, page] and
+    their steps float [n_pages, n_kv_heads]."""
+    import torch
+    n, h, page, dh = k.shape
+    _expect(tuple(v.shape) == (n, h, dh, page) and tuple(k_step.shape) == (n, h) == tuple(v_step.shape), "the shapes of a cache's parts differ")
+    _expect(all(t.is_contiguous() for t in (k, k_step, v, v_step)), "a cache's parts are dense")
+    c = KvCache(C.sizeof(KvCache), h, dh, page, n, _ptr(k), _ptr(k_step), _ptr(v), _ptr(v_step))
+    c.parts = (k, v, k_step, v_step)       # (they live as long as the structure that points to them)
+    return c
+
+
+def kv_batch(cu_new, lens, table, max_new, max_len):
+    """Sequences of a call: their rows (int32 [n + 1]), lengths with the new tokens (int32 [n]), pages (int32 [n, max_pages])
+    and the host's bounds of new tokens and of lengths."""
+    n = lens.numel()
+    _expect(cu_new.numel() == n + 1 and table.dim() == 2 and table.shape[0] == n and (table.stride(1) == 1 or table.shape[1] == 1),
+            "cu_new [n + 1], lens [n], table [n, pages]")
+    _expect(cu_new.is_contiguous() and lens.is_contiguous(), "cu_new and lens are dense")
+    ld = max(table.stride(0), table.shape[1])
+    b = KvBatch(C.sizeof(KvBatch), n, _ptr(cu_new), _ptr(lens), _ptr(table), ld, table.shape[1], max_new, max_len, 0)
+    b.parts = (cu_new, lens, table)
+    return b
+
+
+def _kv_here(p, b, c, *xs):
+    import torch
+    i8, f32, i32 = torch.int8, torch.float32, torch.int32
+    _here(p, ("x",) * len(xs) + (i32,) * 3 + (i8, i8, f32, f32), *xs, *b.parts, *c.parts)
+
+
+def kv_append(K, V, batch, cache, p):
+    """New rows of keys and values [n_tok, n_kv_heads * head_dim] into the cache's pages."""
+    _kv_here(p, batch, cache, K, V)
+    _expect(K.shape == V.shape and K.shape[1] == cache.n_kv_heads * cache.head_dim, "K, V: [n_tok, n_kv_heads * head_dim]")
+    _check(lib().tlq_kv_append(_ptr(K), _ld(K), _ptr(V), _ld(V), K.shape[0], C.byref(batch), C.byref(cache), C.byref(p),
+                               _stream()), "tlq_kv_append")
+
+
+def kv_attention_workspace_bytes(n_tok, n_heads, batch, cache):
+    return int(lib().tlq_kv_attention_workspace_bytes(n_tok, n_heads, C.byref(batch), C.byref(cache)))
+
+
+def kv_attention(Q, n_heads, batch, cache, p, Out, scale=0.0, workspace=None):
+    """Causal attention of the new rows Q [n_tok, n_heads * head_dim] over the cache, their own tokens among it."""
+    _kv_here(p, batch, cache, Q, Out)
+    _expect(Q.shape == Out.shape and Q.shape[1] == n_heads * cache.head_dim, "Q, Out: [n_tok, n_heads * head_dim]")
+    ws = workspace if workspace is not None else _ws(kv_attention_workspace_bytes(Q.shape[0], n_heads, batch, cache), Q)
+    _check(lib().tlq_kv_attention(_ptr(Q), _ld(Q), Q.shape[0], n_heads, scale, C.byref(batch), C.byref(cache), C.byref(p),
+                                  _ptr(Out), _ld(Out), _ptr(ws), ws.numel(), _stream()), "tlq_kv_attention")
     return Out
 
 

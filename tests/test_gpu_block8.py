@@ -1,0 +1,597 @@
+"""A decoder block in 8 bits on the GPU against the 64-bit oracle: codes of rows, the integer linear, normalised and rotated
+queries and keys, appends to the paged cache, attention over it, a run of them together, captured graphs, streams."""
+import numpy as np
+import pytest
+
+from oracle import block8 as ob
+from oracle import tlq_oracle as orc
+from paper_2602_07899_amd import tlq
+
+pytestmark = pytest.mark.gpu
+
+HALF = {"f16": 2.0 ** -11, "bf16": 2.0 ** -8, "f32": 2.0 ** -24}     # half a step, relative
+TINY = {"f16": 2.0 ** -25, "bf16": 2.0 ** -134, "f32": 2.0 ** -150}    # half of the smallest step
+U = 2.0 ** -24
+CODE = {"f16": tlq.F16, "bf16": tlq.BF16, "f32": tlq.F32}
+
+
+def tt(dt):
+    import torch
+    return {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}[dt]
+
+
+def rnd(a, dt):
+    """float32 values that dt holds exactly."""
+    a = np.asarray(a, np.float32)
+    return a.astype(np.float16).astype(np.float32) if dt == "f16" else np.asarray(orc.round_to_bf16(a), np.float32)
+
+
+def dev(a, gpu, dt=None):
+    import torch
+    t = torch.from_numpy(np.ascontiguousarray(a)).to(gpu)
+    return t if dt is None else t.to(tt(dt))
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def spread(a, gpu, dt, left=8, right=16):
+    """A column slice of a wider matrix that holds `a`, and the matrix."""
+    import torch
+    wide = torch.full((a.shape[0], left + -(-a.shape[1] // 8) * 8 + right), 3.0, dtype=tt(dt), device=gpu)
+    part = wide[:, left:left + a.shape[1]]
+    part.copy_(dev(a, gpu, dt))
+    return part, wide
+
+
+def within(got, want, bound):
+    bad = ~(np.abs(got - want) <= bound)
+    assert not bad.any(), (int(bad.sum()), float(np.nanmax(np.abs(got - want) / bound)), np.argwhere(bad)[:4].tolist())
+
+
+# ------------------------------------------------------------------ row codes, integer linear
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("n,c,bits,scaled", [(1, 8, 8, True), (3, 72, 8, False), (17, 128, 4, True), (9, 1096, 2, True),
+                                             (130, 520, 6, False), (2, 13824, 8, True)])
+def test_row_codes_are_exact(gpu, dt, n, c, bits, scaled):
+    import torch
+    g = np.random.default_rng([21, n, c])
+    x = rnd(g.standard_normal((n, c)) * np.exp(g.standard_normal((n, 1)) * 3), dt)
+    x[0, :] = 0.0 if n > 1 else x[0, :]                       # a row of zeros: the floor
+    f = np.exp(g.standard_normal(c)).astype(np.float32) if scaled else None
+    p = tlq.params(x_dtype=CODE[dt])
+    c8 = -(-c // 128) * 128
+    wide = torch.full((n, c8 + 32), 77, dtype=torch.int8, device=gpu)
+    steps = torch.empty(n, dtype=torch.float32, device=gpu)
+    xt, _ = spread(x, gpu, dt)
+    tlq.row_codes(xt, bits, p, wide[:, 16:16 + c8], steps, factor=None if f is None else dev(f, gpu))
+    want, wsteps = ob.row_codes(x, bits, f)
+    got = wide.cpu().numpy()
+    assert np.array_equal(got[:, 16:16 + c], want) and np.array_equal(steps.cpu().numpy(), wsteps)
+    assert np.all(got[:, 16 + c:16 + c8] == 0)                    # zeros behind the row,
+    assert np.all(got[:, :16] == 77) and np.all(got[:, 16 + c8:] == 77)      # nothing beyond
+
+
+def test_row_codes_zeros_behind_infinite_factors(gpu):
+    """The zeros behind a row's channels are zeros whatever the factors are."""
+    import torch
+    f = np.full(136, np.inf, np.float32)
+    codes = torch.full((2, 256), 5, dtype=torch.int8, device=gpu)
+    tlq.row_codes(dev(np.ones((2, 136)), gpu, "f16"), 8, tlq.params(), codes, torch.empty(2, device=gpu), factor=dev(f, gpu))
+    assert bool((codes[:, 136:] == 0).all())
+
+
+def test_row_codes_of_weights_are_the_channel_quantiser(gpu):
+    """The codes are those of fake_quant with symmetric rows."""
+    import torch
+    g = np.random.default_rng(22)
+    W = rnd(g.standard_normal((37, 648)) * 0.02, "f16")
+    s = np.exp(g.standard_normal(648)).astype(np.float32)
+    p = tlq.params(bits=8, group=0, symmetric=1)
+    codes, steps = torch.empty((37, 768), dtype=torch.int8, device=gpu), torch.empty(37, device=gpu)
+    tlq.row_codes(dev(W, gpu, "f16"), 8, p, codes, steps, factor=dev(s, gpu))
+    stored, delta = torch.empty((37, 648), dtype=torch.uint8, device=gpu), torch.empty((37, 1), device=gpu)
+    tlq.fake_quant(dev(W, gpu, "f16"), dev(s, gpu), p, codes=stored, delta=delta)
+    assert torch.equal(codes[:, :648].int(), stored.int() - 128) and torch.equal(steps, delta[:, 0])
+
+
+def _linear_case(g, n, ci, co, dt, bits, wbits=8):
+    x = rnd(g.standard_normal((n, ci)) * 2.0, dt)
+    x[:, g.integers(0, ci, max(1, ci // 50))] *= 16
+    x = rnd(x, dt)
+    f = np.exp(0.5 * g.standard_normal(ci)).astype(np.float32)
+    wc, ws = ob.row_codes(rnd(g.standard_normal((co, ci)) * 0.03, dt), wbits)
+    return x, f, wc, ws
+
+
+def _padded(wc, gpu, extra=0):
+    import torch
+    co, ci = wc.shape
+    t = torch.zeros((co, -(-ci // 128) * 128 + extra), dtype=torch.int8, device=gpu)
+    if extra:
+        t[:, -extra:] = 99
+    t[:, :ci] = dev(wc, gpu)
+    return t
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("out", ["x", "f32"])
+@pytest.mark.parametrize("n,ci,co,bits", [
+    (1, 8, 1, 8), (1, 4096, 16, 8), (2, 72, 3, 8), (4, 1096, 33, 6), (5, 264, 17, 8), (16, 640, 100, 8), (17, 136, 31, 4),
+    (32, 128, 16, 8), (33, 2056, 50, 8), (64, 384, 130, 8), (65, 256, 20, 8), (129, 72, 129, 8), (300, 1096, 263, 6),
+    (1, 13824, 24, 8), (3, 11008, 70, 2), (257, 512, 257, 8)])
+def test_linear_i8(gpu, dt, out, n, ci, co, bits):
+    import torch
+    g = np.random.default_rng([23, n, ci, co])
+    x, f, wc, ws = _linear_case(g, n, ci, co, dt, bits)
+    od = dt if out == "x" else "f32"
+    p = tlq.params(act_bits=bits, x_dtype=CODE[dt], yref_dtype=CODE[od])
+    xt, _ = spread(x, gpu, dt)
+    y, wide = spread(np.zeros((n, co), np.float32), gpu, od)
+    work = torch.full((tlq.linear_i8_workspace_bytes(n, ci),), 0xAB, dtype=torch.uint8, device=gpu)
+    tlq.linear_i8(xt, _padded(wc, gpu, 16), dev(ws, gpu), p, y, factor=dev(f, gpu), workspace=work)
+    want = ob.linear_i8(x, bits, wc, ws, f)
+    # the sum as a float, two products, the output: each a rounding
+    within(host(y), want, np.abs(want) * (HALF[od] + 3.1 * U) + TINY[od] + 1e-44)
+    keep = torch.ones(wide.shape[1], dtype=torch.bool)
+    keep[8:8 + co] = False
+    assert bool((wide[:, keep.to(gpu)] == 3.0).all())
+
+
+def test_linear_i8_is_the_propagation_of_the_search(gpu):
+    """Stored weights and per-token codes give what apply_best gives in the searched setting."""
+    import torch
+    g = np.random.default_rng(24)
+    n, ci, co = 90, 384, 200
+    x, W = rnd(g.standard_normal((n, ci)), "bf16"), rnd(g.standard_normal((co, ci)) * 0.02, "bf16")
+    s = np.exp(0.5 * g.standard_normal(ci)).astype(np.float32)
+    p = tlq.params(bits=8, group=0, symmetric=1, act_bits=8, x_dtype=tlq.BF16, yref_dtype=tlq.BF16)
+    X, Wt, st = dev(x, gpu, "bf16"), dev(W, gpu, "bf16"), dev(s, gpu)
+    a, y = (torch.empty((n, co), dtype=torch.bfloat16, device=gpu) for _ in range(2))
+    tlq.apply_best(X, Wt, st, p, a)
+    codes, steps = torch.empty((co, 384), dtype=torch.int8, device=gpu), torch.empty(co, device=gpu)
+    tlq.row_codes(Wt, 8, p, codes, steps, factor=st)
+    for rows in (n, 20):                                       # large tiles, the kernel for few tokens
+        tlq.linear_i8(X[:rows], codes, steps, p, y[:rows], factor=dev(np.float32(1) / s, gpu))
+        d = (y[:rows].float() - a[:rows].float()).abs()
+        assert bool((d <= 2 * HALF["bf16"] * a[:rows].float().abs() * 1.01).all())    # (either may round the last bit the other way)
+
+
+def test_linear_i8_extreme_sums(gpu):
+    """The largest sums that the codes allow: exact in 32 bits."""
+    import torch
+    n, ci, co = 2, 65536, 5
+    x = np.ones((n, ci), np.float32)
+    x[1] = -1.0
+    wc, ws = np.full((co, ci), -128, np.int8), np.ones(co, np.float32)
+    p = tlq.params(act_bits=8, yref_dtype=tlq.F32)
+    for rows in (n, 66):
+        X = dev(np.repeat(x, 33, 0)[:rows] if rows > n else x, gpu, "f16")
+        y = torch.empty((rows, 8), device=gpu)[:, :co]
+        tlq.linear_i8(X, dev(wc, gpu), dev(ws, gpu), p, y)
+        want = ob.linear_i8(X.float().cpu().numpy(), 8, wc, ws)
+        within(host(y), want, np.abs(want) * 4 * U)
+
+
+# ------------------------------------------------------------------ queries and keys
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("n,h,kv,dh,rot,pairs,norm,far", [
+    (1, 1, 1, 64, 64, False, True, 10), (5, 3, 1, 128, 128, False, True, 5000), (16, 32, 8, 128, 128, False, True, 2 ** 31 - 1),
+    (7, 7, 1, 128, 64, False, False, 1000), (33, 5, 5, 256, 256, True, True, 100000), (4, 2, 2, 64, 48, False, True, 77),
+    (9, 4, 2, 64, 16, True, False, 3000), (3, 9, 3, 256, 80, False, True, 10 ** 6), (6, 2, 1, 128, 0, False, True, 9),
+    (8200, 1, 1, 64, 64, False, True, 9000)])
+def test_qk_norm_rope(gpu, dt, n, h, kv, dh, rot, pairs, norm, far):
+    import torch
+    g = np.random.default_rng([31, n, h, dh, rot])
+    q, k = (rnd(g.standard_normal((n, m * dh)) * np.exp(g.standard_normal((n, 1))), dt) for m in (h, kv))
+    q[0] = 0.0                                                # a head of zeros stays zeros
+    pos = g.integers(0, far, n).astype(np.int32)
+    pos[-1] = far if far < 2 ** 31 - 1 else -(2 ** 31)
+    inv = 1e6 ** (-np.arange(rot // 2) / max(1, rot // 2))
+    w = [np.exp(0.3 * g.standard_normal(dh)).astype(np.float32) if norm else None for _ in range(2)]
+    p = tlq.params(x_dtype=CODE[dt])
+    qk = np.concatenate([q, k], 1)
+    both, _ = spread(qk, gpu, dt)
+    qo, qw = spread(np.zeros_like(q), gpu, dt)
+    ko, kw = spread(np.zeros_like(k), gpu, dt)
+    inv_t = dev(inv, gpu) if rot else None
+    tlq.qk_norm_rope(both[:, :h * dh], both[:, h * dh:], dh, dev(pos, gpu), inv_t, p, qo, ko,
+                     wq=None if w[0] is None else dev(w[0], gpu), wk=None if w[1] is None else dev(w[1], gpu), norm=norm,
+                     interleaved=pairs)
+    for x, got, wt in ((q, qo, w[0]), (k, ko, w[1])):
+        want = ob.qk_norm_rope(x, dh, pos, inv, wt, 1e-6, norm, pairs)
+        u = np.abs(ob.qk_norm_rope(x, dh, pos, inv[:0], wt, 1e-6, norm, pairs)).reshape(n, -1, dh)
+        both_of = u.copy()                                    # |u_a| + |u_b| of each pair
+        for i in range(rot // 2):
+            a, b = (2 * i, 2 * i + 1) if pairs else (i, i + rot // 2)
+            both_of[:, :, a] = both_of[:, :, b] = u[:, :, a] + u[:, :, b]
+        # the norm: dh products summed in any order, a root, a quotient, two products; cosine and sine: a fraction of a turn
+        # as a float (2 pi 2^-26), the function's own error (two ulp of 1), the angle in double
+        delta = (dh + 8) * U + 2 * np.pi * 2.0 ** -26 + 4 * U + np.abs(pos.astype(np.float64))[:, None, None] * 2.0 ** -51
+        within(host(got).reshape(n, -1, dh), want.reshape(n, -1, dh), both_of * delta + np.abs(want).reshape(n, -1, dh) * HALF[dt] * 1.001 + TINY[dt] * 1.01)
+    assert bool((qw[:, :8] == 3.0).all()) and bool((kw[:, 8 + kv * dh:] == 3.0).all())
+    # in place: the same bits
+    tlq.qk_norm_rope(both[:, :h * dh], both[:, h * dh:], dh, dev(pos, gpu), inv_t, p, both[:, :h * dh], both[:, h * dh:],
+                     wq=None if w[0] is None else dev(w[0], gpu), wk=None if w[1] is None else dev(w[1], gpu), norm=norm,
+                     interleaved=pairs)
+    assert torch.equal(both[:, :h * dh], qo) and torch.equal(both[:, h * dh:], ko)
+
+
+# ------------------------------------------------------------------ the cache
+class Pool:
+    """A pool of pages with sequences in it, on the host and on the device."""
+
+    def __init__(self, g, gpu, lens, new, kv, dh, page, dt, spare=2, wild=False):
+        self.g, self.gpu, self.dt = g, gpu, dt
+        self.new, self.lens, self.kv, self.dh, self.page = list(new), list(lens), kv, dh, page
+        need = [-(-max(n, 0) // page) for n in lens]
+        self.n = sum(need) + spare
+        order = g.permutation(self.n)
+        self.table = np.full((len(lens), max(max(need), 1) + 1), -1, np.int32)
+        at = 0
+        for s, m in enumerate(need):
+            self.table[s, :m] = order[at:at + m]
+            at += m
+        self.kc = np.clip(np.rint(g.standard_normal((self.n, kv, page, dh)) * 40), -127, 127).astype(np.int8)
+        self.vc = np.clip(np.rint(g.standard_normal((self.n, kv, dh, page)) * 40), -127, 127).astype(np.int8)
+        w = 3.0 if wild else 0.4
+        self.ks = (0.02 * np.exp(0.4 * g.standard_normal((self.n, kv)))).astype(np.float32)
+        self.vs = (0.02 * np.exp(w * g.standard_normal((self.n, kv)))).astype(np.float32)
+        self.cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+        self.rows = int(self.cu[-1])
+        self.max_new, self.max_len = max(max(new), 1), max(max(lens), max(new), 1)
+
+    def load(self):
+        d = lambda a: dev(a, self.gpu)
+        self.t = (d(self.kc), d(self.ks), d(self.vc), d(self.vs))
+        self.l = np.array(self.lens, np.int32)
+        return tlq.kv_batch(d(self.cu), d(self.l), d(self.table), self.max_new, self.max_len), tlq.kv_cache(*self.t)
+
+
+APPENDS = [
+    ([1], [1], 1, 64, 16), ([16, 17, 33], [16, 1, 33], 2, 128, 16), ([100, 64, 65, 1], [37, 64, 1, 1], 3, 128, 64),
+    ([200, 0, 5], [90, 0, 5], 2, 64, 128), ([300, 299], [3, 299], 1, 128, 256), ([48, 40, 47], [9, 40, 2], 5, 128, 32),
+    ([2, 130], [5, 2], 2, 64, 32),           # more new rows than the sequence has tokens
+]
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("lens,new,kv,dh,page", APPENDS)
+def test_kv_append(gpu, dt, lens, new, kv, dh, page):
+    """Codes and steps are those of the definition, bit for bit; what is not written stays as it was."""
+    g = np.random.default_rng([41, sum(lens), page, dh])
+    c = Pool(g, gpu, lens, new, kv, dh, page, dt)
+    rows = c.rows + 3                                         # rows behind the last sequence: no part in anything
+    x = rnd(g.standard_normal((rows, 2 * kv * dh)) * np.exp(1.5 * g.standard_normal((rows, 1))), dt)
+    x[c.rows:] = np.nan
+    x[0, :dh] = 0.0
+    b, cache = c.load()
+    wide, _ = spread(x, gpu, dt)
+    tlq.kv_append(wide[:, :kv * dh], wide[:, kv * dh:], b, cache, tlq.params(x_dtype=CODE[dt]))
+    ob.kv_append(x[:, :kv * dh], c.kc, c.ks, c.cu, c.lens, c.table, c.max_len, False)
+    ob.kv_append(x[:, kv * dh:], c.vc, c.vs, c.cu, c.lens, c.table, c.max_len, True)
+    for got, want in zip(c.t, (c.kc, c.ks, c.vc, c.vs)):
+        assert np.array_equal(got.cpu().numpy(), want)
+
+
+def test_kv_append_one_by_one_grows_the_step(gpu):
+    """Tokens one at a time, each louder or quieter than the last: earlier codes follow the page's step."""
+    g = np.random.default_rng(42)
+    kv, dh, page, dt = 2, 64, 16, "bf16"
+    c = Pool(g, gpu, [20], [20], kv, dh, page, dt)
+    x = rnd(g.standard_normal((20, kv * dh)) * np.array([1, 3, 0.1, 50, 2] * 4)[:, None], dt)
+    b, cache = c.load()
+    X = dev(x, gpu, dt)
+    one = np.array([0, 1], np.int32)
+    for t in range(20):
+        lens = np.array([t + 1], np.int32)
+        tlq.kv_append(X[t:t + 1], X[t:t + 1], tlq.kv_batch(dev(one, gpu), dev(lens, gpu), b.parts[2], 1, 32), cache, tlq.params(x_dtype=tlq.BF16))
+        ob.kv_append(x[t:t + 1], c.kc, c.ks, one, lens, c.table, 32, False)
+        ob.kv_append(x[t:t + 1], c.vc, c.vs, one, lens, c.table, 32, True)
+    for got, want in zip(c.t, (c.kc, c.ks, c.vc, c.vs)):
+        assert np.array_equal(got.cpu().numpy(), want)
+
+
+def test_kv_append_of_infinities_and_nan(gpu):
+    g = np.random.default_rng(43)
+    c = Pool(g, gpu, [24], [20], 1, 64, 16, "f16")
+    x = rnd(g.standard_normal((20, 64)), "f16")
+    x[3, 5], x[4, 6], x[5, 7], x[19, :] = np.inf, -np.inf, np.nan, np.nan
+    b, cache = c.load()
+    X = dev(x, gpu, "f16")
+    tlq.kv_append(X, X, b, cache, tlq.params())
+    ob.kv_append(x, c.kc, c.ks, c.cu, c.lens, c.table, c.max_len, False)
+    ob.kv_append(x, c.vc, c.vs, c.cu, c.lens, c.table, c.max_len, True)
+    for got, want in zip(c.t, (c.kc, c.ks, c.vc, c.vs)):
+        assert np.array_equal(got.cpu().numpy(), want)
+
+
+def _attend(gpu, c, heads, dt, q, scale=0.0, rows=None, poison=True):
+    import torch
+    b, cache = c.load()
+    wide_q, _ = spread(q, gpu, dt)
+    out, wide = spread(np.zeros_like(q), gpu, dt)
+    wide.fill_(3.0)
+    p = tlq.params(x_dtype=CODE[dt])
+    work = torch.full((max(256, tlq.kv_attention_workspace_bytes(q.shape[0], heads, b, cache)),), 0xFF, dtype=torch.uint8, device=gpu)
+    tlq.kv_attention(wide_q, heads, b, cache, p, out, scale=scale, workspace=work)
+    torch.cuda.synchronize()
+    got = host(wide)
+    assert np.all(got[:, :8] == 3.0) and np.all(got[:, 8 + q.shape[1]:] == 3.0)
+    return got[:, 8:8 + q.shape[1]]
+
+
+def _check_attention(gpu, c, heads, dt, q, scale=0.0):
+    got = _attend(gpu, c, heads, dt, q, scale)
+    want, mag, sens = ob.kv_attention(q, heads, c.kc, c.ks, c.vc, c.vs, c.cu, c.lens, c.table, c.max_len, scale or None)
+    none = np.isnan(want[:, 0])
+    assert np.all(got[none] == 3.0)                            # rows behind the last sequence stay as they were
+    got, want, mag, sens = got[~none], want[~none], mag[~none], np.repeat(sens[~none], c.dh, 1)
+    # weights in 16 bits (2^-11; those below 2^-29 of the largest: 2^-40 of it), scores as sums of dh products (a relative
+    # error of e^(2 ds) in p and in the sum of p), sums over the keys in 32 bits, the output
+    n = c.max_len
+    ds = ((c.dh + 6) * sens + 64) * U
+    bound = mag * (2.0 ** -11 + 2.1 * ds + (n / 4 + 64) * U) + n * 2.0 ** -40 * 127 * c.vs.max() + np.abs(want) * HALF[dt] * 1.001 + TINY[dt] * 1.01
+    within(got, want, bound)
+    # well inside on average: the weights' roundings do not line up
+    assert np.abs(got - want).mean() <= 0.6 * bound.mean()
+
+
+ATTENTION = [   # lens, new, kv heads, group, dh, page
+    ([1], [1], 1, 1, 64, 16), ([1, 2, 3], [1, 1, 1], 2, 2, 128, 16), ([70, 16, 129], [1, 1, 1], 2, 7, 128, 16),
+    ([300, 255, 256, 257], [1, 1, 1, 1], 1, 8, 128, 64), ([1000], [1], 3, 4, 64, 32), ([2600, 40], [1, 1], 2, 4, 128, 256),
+    ([40, 41, 64], [3, 9, 2], 2, 3, 128, 32), ([65, 130], [65, 130], 2, 1, 128, 64), ([33, 100], [33, 50], 1, 4, 64, 16),
+    ([500], [129], 2, 1, 128, 64), ([700, 300, 5], [200, 300, 5], 1, 2, 64, 128), ([150, 0, 20], [150, 0, 20], 2, 6, 128, 16),
+    ([1500], [17], 1, 1, 128, 64), ([20], [20], 1, 40, 64, 16),
+]
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("lens,new,kv,group,dh,page", ATTENTION)
+def test_kv_attention(gpu, dt, lens, new, kv, group, dh, page):
+    g = np.random.default_rng([51, sum(lens), group, dh])
+    c = Pool(g, gpu, lens, new, kv, dh, page, dt)
+    q = rnd(1.5 * g.standard_normal((c.rows + 2, kv * group * dh)), dt)
+    q[c.rows:] = np.nan
+    _check_attention(gpu, c, kv * group, dt, q)
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+def test_kv_attention_of_wild_steps_and_loud_queries(gpu, dt):
+    """Pages whose steps lie five orders of magnitude apart; queries of very different size, zeros among them; scores large
+    enough that one key has nearly all of the weight; a scale of the caller's."""
+    g = np.random.default_rng(52)
+    c = Pool(g, gpu, [400, 333, 90], [1, 6, 90], 2, 128, 16, dt, wild=True)
+    q = rnd(g.standard_normal((c.rows, 4 * 128)) * np.exp(2 * g.standard_normal((c.rows, 1))), dt)
+    q[2] = 0.0
+    if dt == "bf16":
+        q[3] = rnd(q[3] * 2.0 ** -100, dt)
+    _check_attention(gpu, c, 4, dt, q)
+    _check_attention(gpu, c, 4, dt, q, scale=-0.31)
+    c.ks[:] *= 20
+    _check_attention(gpu, c, 4, dt, q)
+
+
+def test_kv_attention_of_pages_that_are_not_there(gpu):
+    """Entries outside the pool stand for tokens that do not exist, wherever they are; a row that sees none gives zeros; steps and
+    codes of pages that no sequence names are never used."""
+    g = np.random.default_rng(53)
+    for dt, new in (("f16", [1, 3, 1, 2, 70]), ("bf16", [70, 40, 20, 30, 64])):
+        c = Pool(g, gpu, [130, 100, 20, 40, 70], new, 2, 128, 16, dt)
+        c.table[0, 2], c.table[0, 5], c.table[1, 6], c.table[2, :], c.table[3, 0], c.table[4, :4] = -1, c.n, 2 ** 31 - 1, -5, -(2 ** 31), -1
+        named = {int(i) for i in c.table.ravel() if 0 <= i < c.n}
+        for i in set(range(c.n)) - named:
+            c.ks[i], c.vs[i] = np.nan, np.inf
+        q = rnd(g.standard_normal((c.rows, 4 * 128)), dt)
+        keep = c.vs.copy()
+        c.vs[~np.isfinite(c.vs)] = 0.0                        # (the bound takes the largest step; put back below)
+        top = c.vs.max()
+        c.vs = keep
+        got = _attend(gpu, c, 4, dt, q)
+        want, mag, sens = ob.kv_attention(q, 4, c.kc, c.ks, c.vc, c.vs, c.cu, c.lens, c.table, c.max_len)
+        ds = ((128 + 6) * np.repeat(sens, 128, 1) + 64) * U
+        within(got, want, mag * (2.0 ** -11 + 2.1 * ds + 200 * U) + 200 * 2.0 ** -40 * 127 * top + np.abs(want) * HALF[dt] * 1.001 + TINY[dt] * 1.01)
+        assert (want == 0).all(axis=1).any()
+
+
+def test_kv_lengths_that_no_batch_should_have(gpu):
+    """Lengths beyond the table, beyond the host's bound, negative ones and new rows beyond a length: held to what is there."""
+    g = np.random.default_rng(54)
+    dt = "bf16"
+    c = Pool(g, gpu, [40, 40, 40, 40], [2, 40, 3, 2], 1, 64, 16, dt)
+    c.table = c.table[:, :3].copy()                           # 48 tokens a sequence at most
+    c.lens = [1000, 25, -7, 40]
+    c.max_len = 47
+    q = rnd(g.standard_normal((c.rows, 128)), dt)
+    _check_attention(gpu, c, 2, dt, q)
+    x = rnd(g.standard_normal((c.rows, 64)), dt)
+    b, cache = c.load()
+    tlq.kv_append(dev(x, gpu, dt), dev(x, gpu, dt), b, cache, tlq.params(x_dtype=tlq.BF16))
+    ob.kv_append(x, c.kc, c.ks, c.cu, c.lens, c.table, c.max_len, False)
+    ob.kv_append(x, c.vc, c.vs, c.cu, c.lens, c.table, c.max_len, True)
+    for got, want in zip(c.t, (c.kc, c.ks, c.vc, c.vs)):
+        assert np.array_equal(got.cpu().numpy(), want)
+
+
+def test_kv_attention_of_a_shared_prefix(gpu):
+    """Two sequences that hold the same first pages give what they give alone."""
+    import torch
+    g = np.random.default_rng(55)
+    c = Pool(g, gpu, [100, 90], [1, 1], 2, 128, 32, "f16")
+    c.table[1, :2] = c.table[0, :2]
+    q = rnd(g.standard_normal((2, 4 * 128)), "f16")
+    _check_attention(gpu, c, 4, "f16", q)
+
+
+def test_kv_attention_of_a_long_sequence(gpu):
+    """40,000 keys of which a few have most of the weight: what lies far below them still counts."""
+    g = np.random.default_rng(56)
+    c = Pool(g, gpu, [40001], [1], 1, 64, 64, "f16")
+    q = rnd(2.0 * g.standard_normal((1, 2 * 64)), "f16")
+    _check_attention(gpu, c, 2, "f16", q)
+    # one key 2^17 times as heavy as each of the others: together they have a quarter of the weight
+    c.kc[:] = 0
+    c.kc[c.table[0, 300], 0, 5, :] = 127
+    c.ks[:] = np.float32(17 * np.log(2) / (127 * 8))
+    _check_attention(gpu, c, 2, "f16", np.ones((1, 128), np.float32))
+
+
+# ------------------------------------------------------------------ together
+def _block(gpu, g, d, heads, kv, dh, ffn, dt):
+    """Weights of a block as stored codes and steps, and its vectors."""
+    import torch
+    out = {}
+    for name, co, ci in (("qkv", (heads + 2 * kv) * dh, d), ("o", d, heads * dh), ("gate_up", 2 * ffn, d), ("down", d, ffn)):
+        W = dev(rnd(g.standard_normal((co, ci)) * ci ** -0.5, dt), gpu, dt)
+        s = np.exp(0.3 * g.standard_normal(ci)).astype(np.float32)
+        codes = torch.empty((co, -(-ci // 128) * 128), dtype=torch.int8, device=gpu)
+        steps = torch.empty(co, device=gpu)
+        tlq.row_codes(W, 8, tlq.params(x_dtype=CODE[dt]), codes, steps, factor=dev(s, gpu))
+        out[name] = (codes, steps, dev(np.float32(1) / s, gpu))
+    return out
+
+
+@pytest.mark.parametrize("dt,heads,kv,dh", [("bf16", 4, 2, 128), ("f16", 6, 1, 64)])
+def test_a_block_in_eight_bits(gpu, dt, heads, kv, dh):
+    """Prompts of three sequences and four steps of single tokens through a whole block, as a program runs it; every operator
+    is held to the oracle on the inputs that it met."""
+    import torch
+    g = np.random.default_rng([61, heads])
+    d, ffn, page = 256, 384, 16
+    w = _block(gpu, g, d, heads, kv, dh, ffn, dt)
+    p = tlq.params(bits=8, group=0, symmetric=1, act_bits=8, x_dtype=CODE[dt], yref_dtype=CODE[dt])
+    inv = 1e4 ** (-np.arange(dh // 2) / (dh // 2))
+    wq, wk = (np.exp(0.2 * g.standard_normal(dh)).astype(np.float32) for _ in range(2))
+    prompt = [19, 33, 7]
+    c = Pool(g, gpu, [n + 4 for n in prompt], prompt, kv, dh, page, dt)
+    c.load()
+    cache = tlq.kv_cache(*c.t)
+    table = dev(c.table, gpu)
+    lens = np.zeros(3, np.int32)
+    new = lambda n, m: torch.empty((n, m), dtype=tt(dt), device=gpu)
+
+    def linear(x, name):
+        codes, steps, f = w[name]
+        y = tlq.linear_i8(x, codes, steps, p, new(x.shape[0], codes.shape[0]), factor=f)
+        want = ob.linear_i8(host(x), 8, codes[:, :x.shape[1]].cpu().numpy(), steps.cpu().numpy(), f.cpu().numpy())
+        within(host(y), want, np.abs(want) * (HALF[dt] + 3.1 * U) + TINY[dt])
+        return y
+
+    for counts in [prompt] + [[1, 1, 1]] * 4:
+        n = sum(counts)
+        lens = lens + np.array(counts, np.int32)
+        cu = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+        pos = np.concatenate([np.arange(l - m, l) for l, m in zip(lens, counts)]).astype(np.int32)
+        batch = tlq.kv_batch(dev(cu, gpu), dev(lens.astype(np.int32), gpu), table, max(counts), 64)
+        h = dev(rnd(g.standard_normal((n, d)), dt), gpu, dt)
+        qkv = linear(tlq.rmsnorm_mul(h, p, new(n, d)), "qkv")
+        q, k, v = qkv[:, :heads * dh], qkv[:, heads * dh:(heads + kv) * dh], qkv[:, (heads + kv) * dh:]
+        before = host(q)
+        tlq.qk_norm_rope(q, k, dh, dev(pos, gpu), dev(inv, gpu), p, q, k, wq=dev(wq, gpu), wk=dev(wk, gpu))
+        want = ob.qk_norm_rope(before, dh, pos, inv, wq)
+        within(host(q), want, np.abs(want) * HALF[dt] * 1.001 + 2e-5 * np.abs(want).max())
+        tlq.kv_append(k, v, batch, cache, p)
+        ob.kv_append(host(k), c.kc, c.ks, cu, lens, c.table, 64, False)
+        ob.kv_append(host(v), c.vc, c.vs, cu, lens, c.table, 64, True)
+        for got, code in zip(c.t, (c.kc, c.ks, c.vc, c.vs)):
+            assert np.array_equal(got.cpu().numpy(), code)
+        a = tlq.kv_attention(q, heads, batch, cache, p, new(n, heads * dh))
+        want, mag, sens = ob.kv_attention(host(q), heads, c.kc, c.ks, c.vc, c.vs, cu, lens, c.table, 64)
+        ds = ((dh + 6) * np.repeat(sens, dh, 1) + 64) * U
+        within(host(a), want, mag * (2.0 ** -11 + 2.1 * ds + 100 * U) + np.abs(want) * HALF[dt] * 1.001 + TINY[dt] + 1e-7)
+        h = tlq.residual_add(h, linear(a, "o"), p, h)
+        gu = linear(tlq.rmsnorm_mul(h, p, new(n, d)), "gate_up")
+        m = tlq.silu_mul(gu[:, :ffn], gu[:, ffn:], p, new(n, ffn))
+        h = tlq.residual_add(h, linear(m, "down"), p, h)
+        assert bool(torch.isfinite(h).all())
+
+
+def test_a_step_as_a_graph(gpu):
+    """One step of single tokens captured; lengths and inputs change between replays, eager work lies between them, and a second
+    graph shares the workspace."""
+    import torch
+    g = np.random.default_rng(62)
+    heads, kv, dh, page, dt = 8, 2, 128, 64, "bf16"
+    d = heads * dh
+    p = tlq.params(act_bits=8, x_dtype=tlq.BF16, yref_dtype=tlq.BF16)
+    c = Pool(g, gpu, [900, 700], [1, 1], kv, dh, page, dt)
+    c.load()
+    cache = tlq.kv_cache(*c.t)
+    w = _block(gpu, g, d, heads, kv, dh, 128, dt)
+    cu, lens, table = dev(c.cu, gpu), dev(np.array([700, 500], np.int32), gpu), dev(c.table, gpu)
+    pos = torch.zeros(2, dtype=torch.int32, device=gpu)
+    inv = dev(1e4 ** (-np.arange(64) / 64.0), gpu)
+    batch = tlq.kv_batch(cu, lens, table, 1, 900)
+    h = torch.empty((2, d), dtype=tt(dt), device=gpu)
+    qkv = torch.empty((2, (heads + 2 * kv) * dh), dtype=tt(dt), device=gpu)
+    a, y = torch.empty_like(h), torch.empty_like(h)
+    ws = torch.empty(max(tlq.linear_i8_workspace_bytes(2, d), tlq.kv_attention_workspace_bytes(2, heads, batch, cache)), dtype=torch.uint8, device=gpu)
+
+    def step(out):
+        codes, steps, f = w["qkv"]
+        tlq.linear_i8(h, codes, steps, p, qkv, factor=f, workspace=ws)
+        q, k, v = qkv[:, :d], qkv[:, d:d + kv * dh], qkv[:, d + kv * dh:]
+        tlq.qk_norm_rope(q, k, dh, pos, inv, p, q, k)
+        tlq.kv_append(k, v, batch, cache, p)
+        tlq.kv_attention(q, heads, batch, cache, p, a, workspace=ws)
+        codes, steps, f = w["o"]
+        tlq.linear_i8(a, codes, steps, p, out, factor=f, workspace=ws)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        h.copy_(dev(rnd(g.standard_normal((2, d)), dt), gpu, dt))
+        step(y)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    y2 = torch.empty_like(y)
+    graphs = []
+    for out in (y, y2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=side):
+            step(out)
+    saved = [t.clone() for t in c.t]
+    for i in range(4):
+        h.copy_(dev(rnd(g.standard_normal((2, d)), dt), gpu, dt))
+        lens.copy_(dev(np.array([701 + 60 * i, 501 + i], np.int32), gpu))
+        pos.copy_(lens - 1)
+        for t, o in zip(c.t, saved):
+            t.copy_(o)
+        step(y)
+        torch.cuda.synchronize()
+        want = [t.clone() for t in (y, a, *c.t)]
+        for graph, out in zip(graphs, (y, y2)):
+            for t, o in zip(c.t, saved):
+                t.copy_(o)
+            ws.fill_(0xFF)
+            out.fill_(float("nan"))
+            graph.replay()
+            torch.cuda.synchronize()
+            for got, e in zip((out, a, *c.t), want):
+                assert torch.equal(got, e)
+
+
+def test_calls_on_another_stream(gpu):
+    """The calls run on the current stream, in its order."""
+    import torch
+    g = np.random.default_rng(63)
+    c = Pool(g, gpu, [200], [1], 2, 128, 16, "f16")
+    b, cache = c.load()
+    q = dev(rnd(g.standard_normal((1, 512)), "f16"), gpu, "f16")
+    k = dev(rnd(g.standard_normal((1, 256)), "f16"), gpu, "f16")
+    p = tlq.params()
+    saved = [t.clone() for t in c.t]
+    tlq.kv_append(k, k, b, cache, p)
+    want = tlq.kv_attention(q, 4, b, cache, p, torch.empty_like(q)).clone()
+    for t, o in zip(c.t, saved):
+        t.copy_(o)
+    out, late = torch.zeros_like(q), torch.zeros_like(k)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        late.copy_(k)
+        tlq.kv_append(late, late, b, cache, p)
+        tlq.kv_attention(q, 4, b, cache, p, out)
+    side.synchronize()
+    assert torch.equal(out, want)
