@@ -27,6 +27,7 @@ struct KvAttnDev {
   tlq_kv_batch b; tlq_kv_cache c; int page_bits;
   uint16_t* Out; int64_t ldo;
   int n_splits, chunk;          // keys of a split
+  int tiles; unsigned ways, members; int64_t n_pairs;      // kv_prompt_kernel: row tiles, and the order of its blocks
   float2* ml; float* acc;       // per (row, head, split): reference and sum; [head_dim] sums of codes
 };
 
@@ -50,13 +51,14 @@ __device__ __forceinline__ f16x8 widen_codes8(uint32_t a, uint32_t b) {
 }
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// N queries' channels of a lane as halves; the factor that undoes their prescale.  `rows`: lanes (lane ^ 16, lane ^ 32)
-// that hold the other channels of the same query.
-template <typename T, int N>
-__device__ __forceinline__ float load_queries(const uint16_t* p, f16x8 (&qf)[N]) {
+// A lane's channels of its query as halves, eight at a time and STEP apart (negated if asked); the factor that undoes their
+// prescale.  Lanes lane ^ 16 and lane ^ 32 hold the other channels of the same query.
+template <typename T, int N, int STEP>
+__device__ __forceinline__ float load_queries(const uint16_t* p, f16x8 (&qf)[N], bool negate) {
   u16x8 raw[N];
+  const unsigned short sign = negate ? 0x8000 : 0;
 #pragma unroll
-  for (int i = 0; i < N; ++i) raw[i] = *reinterpret_cast<const u16x8*>(p + 8 * i);
+  for (int i = 0; i < N; ++i) raw[i] = *reinterpret_cast<const u16x8*>(p + STEP * i) ^ sign;
   if constexpr (std::is_same<T, F16>::value) {
 #pragma unroll
     for (int i = 0; i < N; ++i) qf[i] = __builtin_bit_cast(f16x8, raw[i]);
@@ -91,7 +93,7 @@ __device__ __forceinline__ float load_queries(const uint16_t* p, f16x8 (&qf)[N])
 // where they are widened: no LDS, no barrier in the loop, the next 64 keys in flight while these are worked on.
 // For few rows, bound by the bytes of the cache.
 template <typename T, int DH>
-__global__ __launch_bounds__(256, 2) void kv_few_kernel(KvAttnDev a) {
+__global__ __launch_bounds__(256, 3) void kv_few_kernel(KvAttnDev a) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int NS = DH / 32, ND = DH / 16, LW = DH / 64;    // k32 steps of a score, channel tiles, 16-byte pieces of a lane's key
   constexpr int RS = DH + 4;
@@ -116,9 +118,8 @@ __global__ __launch_bounds__(256, 2) void kv_few_kernel(KvAttnDev a) {
   const int k1 = end - k0 < a.chunk ? end : k0 + a.chunk;
 
   f16x8 qf[NS];
-  const float unscale = load_queries<T, NS>(
-      a.Q + (q.row0 + qi) * a.ldq + ((int64_t)hk * a.group + g) * DH + fq * (DH / 4), qf);
-  const float fac = a.scale2 * unscale;
+  const float fac = a.scale2 * load_queries<T, NS, 8>(
+      a.Q + (q.row0 + qi) * a.ldq + ((int64_t)hk * a.group + g) * DH + fq * (DH / 4), qf, false);
 
   f32x4 acc[ND];
 #pragma unroll
@@ -251,15 +252,225 @@ __global__ __launch_bounds__(256, 2) void kv_few_kernel(KvAttnDev a) {
 #endif
 }
 
+// 128 rows of a sequence and key head against one split of the keys, 32 rows a wave, 64 keys a step.  The keys and values of
+// a step are widened once for the block on their way into LDS: what comes from memory during one step is written during
+// the next into the stage that nobody reads (one barrier a step).  A lane has 16 neighbouring keys of two queries: they lie
+// in one page, so its steps are two numbers, and the largest exponent is found on the bare products.
+// All row tiles of a sequence and key head run on one XCD, up to eight of those together with the longest tiles first (as
+// in block.hip).
+template <typename T, int DH>
+__global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int NS = DH / 32, ND = DH / 16, CPK = DH / 8;   // k32 steps of a score, channel tiles, 16-byte chunks of a key
+  constexpr int KB = DH * 2, VB = 128;                      // bytes of a row of K, of V^T in LDS
+  constexpr int STAGE = 64 * KB + DH * VB, LR = DH / 64;    // LR: 16-byte loads of a thread for K, and for V
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * STAGE];
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, fq = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // blockIdx.x = ways * (members * (split, tile) + member) + pair
+  unsigned pair = blockIdx.x % a.ways, rest = blockIdx.x / a.ways;
+  const unsigned which = rest / a.members, member = rest - which * a.members;
+  const int64_t sh = (((int64_t)blockIdx.z * gridDim.y + blockIdx.y) * a.members + member) * a.ways + pair;
+  if (sh >= a.n_pairs) return;
+  const int tile = a.tiles - 1 - (int)which / a.n_splits, split = (int)which % a.n_splits;
+  const int s = (int)(sh / a.c.n_kv_heads), hk = (int)(sh % a.c.n_kv_heads);
+  const KvSeq q = kv_sequence(a.b, a.c.page, a.n_tok, s);
+  const int64_t rows = (int64_t)q.n_new * a.group, first_row = (int64_t)tile * 128;
+  if (first_row >= rows) return;
+  auto last_key = [&](int64_t r) {      // number of keys that rows up to r see
+    const int p = q.first + (int)((r < rows - 1 ? r : rows - 1) / a.group);
+    return p + 1 < q.len ? p + 1 : q.len;
+  };
+  const int end = last_key(first_row + 127);
+  const int k0 = split * a.chunk;
+  if (k0 >= end && a.n_splits > 1) return;
+  const int k1 = end - k0 < a.chunk ? end : k0 + a.chunk;
+  const int64_t wrow = first_row + wave * 32;
+  const int wend = wrow < rows ? (last_key(wrow + 31) < k1 ? last_key(wrow + 31) : k1) : 0;    // keys of this wave
+  const int wfull = wrow < rows ? last_key(wrow) : 0;                                          // keys that all of its rows see
+
+  f16x8 qf[2][NS];
+  float fac[2];
+  int pos[2];
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    const int64_t r = wrow + n * 16 + l16 < rows ? wrow + n * 16 + l16 : rows - 1;
+    const int qi = (int)(r / a.group), g = (int)(r % a.group);
+    pos[n] = q.first + qi;
+    const uint16_t* p = a.Q + (q.row0 + qi) * a.ldq + ((int64_t)hk * a.group + g) * DH + fq * 8;
+    fac[n] = fabsf(a.scale2) * load_queries<T, NS, 32>(p, qf[n], a.scale2 < 0.0f);
+  }
+  f32x4 acc[ND][2];
+#pragma unroll
+  for (int d = 0; d < ND; ++d) acc[d][0] = acc[d][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  float m_run[2] = {-INFINITY, -INFINITY}, ref[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.0f, 0.0f};
+
+  // what a thread moves: K rows tid / (CPK / 2) and further ones, 16 codes; V channels tid / 4 and 64 further, 16 keys
+  const int krow = tid / (CPK / 2), kch = tid % (CPK / 2) * 2, vrow = tid >> 2, vgr = tid & 3;
+  constexpr int KSTEP = 512 / CPK;                          // rows between a thread's loads of K
+  const int64_t head_bytes = (int64_t)a.c.page * DH;
+  uint4 kr[LR], vr[LR];
+  bool seen = false, seen_next = false;
+  float ks = 0.0f, vs = 1.0f, ks_next = 0.0f, vs_next = 1.0f;
+  auto slot_of = [&](int key, bool& ok) {
+    const int id = key < k1 ? kv_page(a.b, a.c, s, key >> a.page_bits) : -1;
+    ok = id >= 0;
+    return (int64_t)(ok ? id : 0) * a.c.n_kv_heads + hk;
+  };
+  auto load = [&](int unit) {
+    bool ok;
+#pragma unroll
+    for (int i = 0; i < LR; ++i) {
+      const int key = unit + krow + i * KSTEP;
+      kr[i] = *reinterpret_cast<const uint4*>(a.c.k + slot_of(key, ok) * head_bytes + (int64_t)(key & (a.c.page - 1)) * DH + kch * 8);
+    }
+    const int key = unit + vgr * 16;
+    const int8_t* p = a.c.v + slot_of(key, ok) * head_bytes + (int64_t)vrow * a.c.page + (key & (a.c.page - 1));
+#pragma unroll
+    for (int i = 0; i < LR; ++i) vr[i] = *reinterpret_cast<const uint4*>(p + (int64_t)i * 64 * a.c.page);
+    const int64_t slot = slot_of(unit + fq * 16, seen_next);
+    ks_next = seen_next ? a.c.k_step[slot] : 0.0f;
+    vs_next = seen_next ? fmaxf(a.c.v_step[slot], kSmallStep) : 1.0f;
+  };
+  // 16-byte chunks lie at chunk ^ key of their row: the rows that the 16 lanes of a fragment read name have different ones
+  auto kkey = [](int row) { return DH == 128 ? (row >> 4 & 3) * 4 + (row & 3) : (row >> 4 & 3) * 2 + (row >> 1 & 1); };
+  auto stage = [&](unsigned char* at) {
+#pragma unroll
+    for (int i = 0; i < LR; ++i) {
+      const int row = krow + i * KSTEP;
+      *reinterpret_cast<f16x8*>(at + row * KB + ((kch ^ kkey(row)) << 4)) = widen_codes8(kr[i].x, kr[i].y);
+      *reinterpret_cast<f16x8*>(at + row * KB + (((kch + 1) ^ kkey(row)) << 4)) = widen_codes8(kr[i].z, kr[i].w);
+    }
+    at += 64 * KB;
+#pragma unroll
+    for (int i = 0; i < LR; ++i) {
+      const int row = vrow + i * 64;
+      *reinterpret_cast<f16x8*>(at + row * VB + (((vgr * 2) ^ (row >> 1 & 7)) << 4)) = widen_codes8(vr[i].x, vr[i].y);
+      *reinterpret_cast<f16x8*>(at + row * VB + (((vgr * 2 + 1) ^ (row >> 1 & 7)) << 4)) = widen_codes8(vr[i].z, vr[i].w);
+    }
+  };
+  const int my_row = (l16 >> 2) * 16 + (l16 & 3);           // row of K of score tile 0 (tile j: 4 j further, the same key)
+  const int kbase = my_row * KB, kx = kkey(my_row);
+  const int vbase = 64 * KB + l16 * VB, vx = l16 >> 1;      // (row of V^T: 16 d + l16, the same key for all d)
+
+  if (k0 < k1) {
+    load(k0);
+    stage(lds);
+    seen = seen_next; ks = ks_next; vs = vs_next;
+    if (k0 + 64 < k1) load(k0 + 64);
+  }
+  int cur = 0;
+  for (int unit = k0; unit < k1; unit += 64, cur ^= 1) {
+    __syncthreads();
+    const unsigned char* kv = lds + cur * STAGE;
+    const bool work = unit < wend;
+    f32x4 sc[4][2];
+    if (work) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        sc[j][0] = sc[j][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+          const f16x8 kf = *reinterpret_cast<const f16x8*>(kv + kbase + j * 4 * KB + (((i * 4 + fq) ^ kx) << 4));
+          sc[j][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[0][i], sc[j][0], 0, 0, 0);
+          sc[j][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[1][i], sc[j][1], 0, 0, 0);
+        }
+      }
+    }
+    const bool now_seen = seen;
+    const float kst = ks, vst = vs;
+    if (unit + 64 < k1) {
+      stage(lds + (cur ^ 1) * STAGE);
+      seen = seen_next; ks = ks_next; vs = vs_next;
+      if (unit + 128 < k1) load(unit + 128);
+    }
+    if (!work) continue;
+    const float lg = __log2f(vst), rv = 1.0f / vst;
+    if (unit + 64 > wfull || unit + 64 > wend || __any(!now_seen)) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const int limit = now_seen ? (pos[n] < k1 - 1 ? pos[n] : k1 - 1) - (unit + fq * 16) : -1;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) sc[j][n][r] = 4 * j + r <= limit ? sc[j][n][r] : -INFINITY;
+      }
+    }
+    f16x8 pf[2][2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      float mx = sc[0][n][0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, sc[e >> 2][n][e & 3]);
+      const float f = fmaxf(fac[n] * kst, 1e-37f);       // (zero times a masked product would not be -inf)
+      mx = mx == -INFINITY ? mx : __builtin_fmaf(mx, f, lg);
+      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      if (mx > m_run[n]) {
+        const float next = weight_ref(mx), alpha = exp2_fast(ref[n] - next);
+        m_run[n] = mx;
+        ref[n] = next;
+        l_run[n] *= alpha;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) acc[d][n] *= alpha;
+      }
+      const float off = ref[n] != -INFINITY ? lg - ref[n] : 0.0f;
+      float ps = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float w = exp2_fast(__builtin_fmaf(sc[e >> 2][n][e & 3], f, off));
+        ps += w;
+        pf[n][e >> 3][e & 7] = (_Float16)w;
+      }
+      l_run[n] = __builtin_fmaf(ps, rv, l_run[n]);
+    }
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const f16x8 vf = *reinterpret_cast<const f16x8*>(kv + vbase + d * 16 * VB + (((fq * 2 + u) ^ vx) << 4));
+        acc[d][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[0][u], acc[d][0], 0, 0, 0);
+        acc[d][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[1][u], acc[d][1], 0, 0, 0);
+      }
+  }
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    float l = l_run[n];
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    const int64_t r = wrow + n * 16 + l16;
+    if (r >= rows) continue;
+    const int64_t token = q.row0 + r / a.group, head = (int64_t)hk * a.group + r % a.group;
+    if (a.n_splits > 1) {
+      const int64_t at = (token * a.n_heads + head) * a.n_splits + split;
+      if (fq == 0) a.ml[at] = make_float2(ref[n], l);
+#pragma unroll
+      for (int d = 0; d < ND; ++d) *reinterpret_cast<f32x4*>(a.acc + at * DH + d * 16 + fq * 4) = acc[d][n];
+      continue;
+    }
+    const float inv = ref[n] == -INFINITY ? 0.0f : 1.0f / l;
+    uint16_t* to = a.Out + token * a.ldo + head * DH + fq * 4;
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+      uint16_t w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = T::from_float(acc[d][n][e] * inv);
+      *reinterpret_cast<uint2*>(to + d * 16) = make_uint2((uint32_t)w[0] | (uint32_t)w[1] << 16, (uint32_t)w[2] | (uint32_t)w[3] << 16);
+    }
+  }
+#endif
+}
+
 // The splits of a row: sums joined with the largest of their references.  A block has one row; DH / 4 lanes read the sums of a
 // split, 1024 / DH splits side by side.
+constexpr int kMaxSplits = 1024;
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnDev a, int tile_rows) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int LPR = DH / 4, SIDE = 256 / LPR;
   __shared__ __attribute__((aligned(16))) float4 sum[SIDE][LPR];
-  __shared__ float lsum[SIDE];
-  const int tid = threadIdx.x, side = tid / LPR, d = tid % LPR;
+  __shared__ float factor[kMaxSplits], red[2][4];
+  const int tid = threadIdx.x, side = tid / LPR, d = tid % LPR, wave = tid >> 6;
   const int s = blockIdx.z, head = blockIdx.y, qi = blockIdx.x;
   const KvSeq q = kv_sequence(a.b, a.c.page, a.n_tok, s);
   if (qi >= q.n_new) return;
@@ -271,26 +482,44 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnDev a, int tile_rows
   const int end = last + 1 < q.len ? last + 1 : q.len;
   const int n = end <= 0 ? 0 : (end + a.chunk - 1) / a.chunk;
   const int64_t at = ((q.row0 + qi) * a.n_heads + head) * a.n_splits;
-  float m = -INFINITY;
-  for (int i = 0; i < n; ++i) m = fmaxf(m, a.ml[at + i].x);
+  float2 p[kMaxSplits / 256];
+  float m = -INFINITY, l = 0.0f;
+#pragma unroll
+  for (int k = 0; k < kMaxSplits / 256; ++k) {
+    p[k] = k * 256 + tid < n ? a.ml[at + k * 256 + tid] : make_float2(-INFINITY, 0.0f);
+    m = fmaxf(m, p[k].x);
+  }
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+  if ((tid & 63) == 0) red[0][wave] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+#pragma unroll
+  for (int k = 0; k < kMaxSplits / 256; ++k) {
+    const float f = p[k].x == -INFINITY ? 0.0f : exp2_fast(p[k].x - m);
+    if (k * 256 + tid < n) factor[k * 256 + tid] = f;
+    l += p[k].y * f;
+  }
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) l += __shfl_xor(l, off, 64);
+  if ((tid & 63) == 0) red[1][wave] = l;
+  __syncthreads();
+  l = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
   float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  float l = 0.0f;
+#pragma unroll 4
   for (int i = side; i < n; i += SIDE) {
-    const float2 p = a.ml[at + i];
-    if (p.x == -INFINITY) continue;
-    const float f = exp2_fast(p.x - m);
+    const float f = factor[i];
     const float4 v = *reinterpret_cast<const float4*>(a.acc + (at + i) * DH + d * 4);
-    l += p.y * f;
-    o.x += v.x * f; o.y += v.y * f; o.z += v.z * f; o.w += v.w * f;
+    o.x = __builtin_fmaf(v.x, f, o.x); o.y = __builtin_fmaf(v.y, f, o.y);
+    o.z = __builtin_fmaf(v.z, f, o.z); o.w = __builtin_fmaf(v.w, f, o.w);
   }
   sum[side][d] = o;
-  if (d == 0) lsum[side] = l;
   __syncthreads();
   if (side) return;
+#pragma unroll
   for (int i = 1; i < SIDE; ++i) {
     const float4 v = sum[i][d];
     o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
-    l += lsum[i];
   }
   const float inv = m == -INFINITY ? 0.0f : 1.0f / l;
   *reinterpret_cast<uint2*>(a.Out + (q.row0 + qi) * a.ldo + (int64_t)head * DH + d * 4) =
@@ -299,16 +528,21 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnDev a, int tile_rows
 #endif
 }
 
+// Rows of a sequence and key head up to which they go in tiles of 16.
+constexpr int64_t kFewRows = 32;
+
 namespace {
-struct KvPlan { int tiles, n_splits, chunk; size_t acc_at, bytes; };
+struct KvPlan { bool prompt; int rows, tiles, n_splits, chunk; size_t acc_at, bytes; };
 KvPlan kv_plan(int64_t n_tok, int n_heads, const tlq_kv_batch& b, const tlq_kv_cache& c) {
   KvPlan p;
   const int group = n_heads / c.n_kv_heads;
   const int64_t most = b.max_new < n_tok ? b.max_new : n_tok;
-  p.tiles = (int)ceil_div(most * group, 16);
+  p.prompt = most * group > kFewRows;
+  p.rows = p.prompt ? 128 : 16;
+  p.tiles = (int)ceil_div(most * group, p.rows);
   const int64_t room = (int64_t)b.max_pages * c.page, keys = b.max_len < room ? b.max_len : room;
   const int64_t base = (int64_t)p.tiles * c.n_kv_heads * b.n_seq;
-  int64_t splits = ceil_div(1024, base);
+  int64_t splits = ceil_div(p.prompt ? 512 : 1024, base);
   const int64_t units = ceil_div(keys, 256);
   if (splits > units) splits = units;
   p.chunk = (int)(ceil_div(units, splits) * 256);
@@ -332,19 +566,28 @@ hipError_t launch_kv_attention(const void* Q, int64_t ldq, int64_t n_tok, int n_
   a.b = b; a.c = c; a.page_bits = __builtin_ctz((unsigned)c.page);
   a.Out = (uint16_t*)Out; a.ldo = ldo; a.n_splits = p.n_splits; a.chunk = p.chunk;
   a.ml = (float2*)workspace; a.acc = (float*)((unsigned char*)workspace + p.acc_at);
-  if ((int64_t)p.tiles * p.n_splits > 0x7fffffffLL) return hipErrorInvalidValue;
   const int64_t most = b.max_new < n_tok ? b.max_new : n_tok;
-  const dim3 grid((unsigned)(p.tiles * p.n_splits), (unsigned)c.n_kv_heads, (unsigned)b.n_seq);
+  a.tiles = p.tiles;
+  a.n_pairs = (int64_t)b.n_seq * c.n_kv_heads;
+  a.ways = a.n_pairs < 8 ? (unsigned)a.n_pairs : 8u;
+  const int64_t groups = ceil_div(a.n_pairs, a.ways);
+  a.members = (unsigned)(groups < 8 ? groups : 8);
+  const int64_t chunks = ceil_div(groups, a.members), gy = chunks < 32768 ? chunks : 32768;
+  const int64_t work = (int64_t)p.tiles * p.n_splits, gx = p.prompt ? work * a.ways * a.members : work;
+  if (gx > 0x7fffffffLL) return hipErrorInvalidValue;
+  const dim3 grid = p.prompt ? dim3((unsigned)gx, (unsigned)gy, (unsigned)ceil_div(chunks, gy))
+                             : dim3((unsigned)gx, (unsigned)c.n_kv_heads, (unsigned)b.n_seq);
   auto pick = [&](auto t, auto dh) {
     using T = decltype(t);
     constexpr int DH = decltype(dh)::value;
     {
       ProfScope ps("kv_attention", stream, 4.0 * (double)n_tok * n_heads * c.head_dim * (double)b.max_len);
-      kv_few_kernel<T, DH><<<grid, 256, 0, stream>>>(a);
+      if (p.prompt) kv_prompt_kernel<T, DH><<<grid, 256, 0, stream>>>(a);
+      else kv_few_kernel<T, DH><<<grid, 256, 0, stream>>>(a);
     }
     if (hipError_t e = hipGetLastError(); e != hipSuccess || p.n_splits == 1) return e;
     ProfScope ps("kv_join", stream, 4.0 * (double)n_tok * n_heads * p.n_splits * c.head_dim);
-    kv_join_kernel<T, DH><<<dim3((unsigned)most, (unsigned)n_heads, (unsigned)b.n_seq), 256, 0, stream>>>(a, 16);
+    kv_join_kernel<T, DH><<<dim3((unsigned)most, (unsigned)n_heads, (unsigned)b.n_seq), 256, 0, stream>>>(a, p.rows);
     return hipGetLastError();
   };
   using W128 = std::integral_constant<int, 128>;
