@@ -49,6 +49,15 @@ __device__ __forceinline__ f16x8 widen_codes8(uint32_t a, uint32_t b) {
   widen_codes(b, v.z, v.w);
   return __builtin_bit_cast(f16x8, v);
 }
+// the largest of a value that lane ^ 16 and lane ^ 32 hold (as in block.hip: the builtins' two results come out as one; the wait
+// states are what the swaps need behind the write of an operand)
+__device__ __forceinline__ float column_max(float v) {
+  float a = v, b = v;
+  asm("s_nop 1\n\tv_permlane16_swap_b32 %0, %1" : "+v"(a), "+v"(b));
+  a = b = fmaxf(a, b);
+  asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(a), "+v"(b));
+  return fmaxf(a, b);
+}
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // A lane's channels of its query as halves, eight at a time and STEP apart (negated if asked); the factor that undoes their
@@ -129,33 +138,43 @@ __global__ __launch_bounds__(256, 3) void kv_few_kernel(KvAttnDev a) {
   uint4 kr[4][LW], vr[ND];
   float ks = 0.0f, vs = 1.0f;
   bool seen = false;                    // this lane's 16 keys lie in a page that there is
+  // The table's entries are fetched a turn before the pages they name (keys behind the last are never seen: any entry will
+  // do); an entry outside the pool becomes the first page, in reach and never seen
+  const int32_t* row_table = a.b.table + (int64_t)s * a.b.ld_table;
   const int64_t head_bytes = (int64_t)a.c.page * DH;
-  auto slot_of = [&](int key, bool& ok) {     // (a page that is not there: the pool's first, in reach and never seen)
-    const int id = key < end ? kv_page(a.b, a.c, s, key >> a.page_bits) : -1;
-    ok = id >= 0;
-    return (int64_t)(ok ? id : 0) * a.c.n_kv_heads + hk;
-  };
+  const uint32_t page_stride = (uint32_t)a.c.n_kv_heads * a.c.page * DH, n_pages = (uint32_t)a.c.n_pages;
+  const int8_t* kp = a.c.k + hk * head_bytes + (l16 & 3) * DH + fq * (DH / 4);
+  const int8_t* vp = a.c.v + hk * head_bytes + l16 * a.c.page;
+  const int kgroup = (l16 >> 2) * 16, vgroup = fq * 16;
+  uint32_t kid = 0, vid = 0;
+  auto entry = [&](int key) { return (uint32_t)row_table[(key < k1 ? key : k1 - 1) >> a.page_bits]; };
   auto load_k = [&](int unit) {
-    bool ok;
-    const int key = unit + (l16 >> 2) * 16;
-    const int8_t* p = a.c.k + slot_of(key, ok) * head_bytes + (int64_t)((key & (a.c.page - 1)) + (l16 & 3)) * DH + fq * (DH / 4);
+    const int8_t* p = kp + (uint64_t)(kid < n_pages ? kid : 0) * page_stride + ((unit + kgroup) & (a.c.page - 1)) * DH;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int i = 0; i < LW; ++i) kr[j][i] = *reinterpret_cast<const uint4*>(p + j * 4 * DH + i * 16);
+    kid = entry(unit + 256 + kgroup);
   };
   auto load_v = [&](int unit) {
-    const int key = unit + fq * 16;
-    const int64_t slot = slot_of(key, seen);
-    const int8_t* p = a.c.v + slot * head_bytes + (key & (a.c.page - 1)) + (int64_t)l16 * a.c.page;
+    seen = vid < n_pages;
+    const uint32_t id = seen ? vid : 0;
+    const int8_t* p = vp + (uint64_t)id * page_stride + ((unit + vgroup) & (a.c.page - 1));
 #pragma unroll
-    for (int d = 0; d < ND; ++d) vr[d] = *reinterpret_cast<const uint4*>(p + (int64_t)d * 16 * a.c.page);
+    for (int d = 0; d < ND; ++d) vr[d] = *reinterpret_cast<const uint4*>(p + d * 16 * a.c.page);
+    const uint64_t slot = (uint64_t)id * a.c.n_kv_heads + hk;
     ks = seen ? a.c.k_step[slot] : 0.0f;
     vs = seen ? fmaxf(a.c.v_step[slot], kSmallStep) : 1.0f;
+    vid = entry(unit + 256 + vgroup);
   };
 
   int unit = k0 + wave * 64;
-  if (unit < k1) { load_k(unit); load_v(unit); }
+  if (unit < k1) {
+    kid = entry(unit + kgroup);
+    vid = entry(unit + vgroup);
+    load_k(unit);
+    load_v(unit);
+  }
   for (; unit < k1; unit += 256) {
     f32x4 sc[4];
 #pragma unroll
@@ -170,7 +189,7 @@ __global__ __launch_bounds__(256, 3) void kv_few_kernel(KvAttnDev a) {
     }
     if (unit + 256 < k1) load_k(unit + 256);
     // lane: keys unit + 16 fq + 4 j + r of its query
-    const float f = fac * ks, lg = __log2f(vs), rv = 1.0f / vs;
+    const float f = fac * ks, lg = __builtin_amdgcn_logf(vs), rv = __builtin_amdgcn_rcpf(vs);
     const int limit = seen ? (pos < k1 - 1 ? pos : k1 - 1) - (unit + fq * 16) : -1;    // last visible of the 16
     float mx = -INFINITY;
 #pragma unroll
@@ -181,8 +200,7 @@ __global__ __launch_bounds__(256, 3) void kv_few_kernel(KvAttnDev a) {
         sc[j][r] = 4 * j + r <= limit ? z : -INFINITY;
         mx = fmaxf(mx, sc[j][r]);
       }
-    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    mx = column_max(mx);
     if (mx > m_run) {
       const float next = weight_ref(mx), alpha = exp2_fast(ref - next);       // (0 at the first visible key)
       m_run = mx;
@@ -305,34 +323,44 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
   for (int d = 0; d < ND; ++d) acc[d][0] = acc[d][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   float m_run[2] = {-INFINITY, -INFINITY}, ref[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.0f, 0.0f};
 
-  // what a thread moves: K rows tid / (CPK / 2) and further ones, 16 codes; V channels tid / 4 and 64 further, 16 keys
-  const int krow = tid / (CPK / 2), kch = tid % (CPK / 2) * 2, vrow = tid >> 2, vgr = tid & 3;
+  // what a thread moves: K rows tid / (CPK / 2) and further ones, 16 codes; V channels 16 wave + l16 and 64 further, the 16 keys
+  // that it has the scores of.  A wave's K rows of one load lie in one page.
+  const int krow = tid / (CPK / 2), kch = tid % (CPK / 2) * 2, vrow = wave * 16 + l16;
   constexpr int KSTEP = 512 / CPK;                          // rows between a thread's loads of K
+  const int32_t* row_table = a.b.table + (int64_t)s * a.b.ld_table;
   const int64_t head_bytes = (int64_t)a.c.page * DH;
+  const uint32_t page_stride = (uint32_t)a.c.n_kv_heads * a.c.page * DH, n_pages = (uint32_t)a.c.n_pages;
+  const int8_t* kp = a.c.k + hk * head_bytes + kch * 8;
+  const int8_t* vp = a.c.v + hk * head_bytes + vrow * a.c.page;
+  const int kgroup = wave * (KSTEP / 4) & ~15, vgroup = fq * 16;
   uint4 kr[LR], vr[LR];
+  uint32_t kid[LR], vid;
   bool seen = false, seen_next = false;
   float ks = 0.0f, vs = 1.0f, ks_next = 0.0f, vs_next = 1.0f;
-  auto slot_of = [&](int key, bool& ok) {
-    const int id = key < k1 ? kv_page(a.b, a.c, s, key >> a.page_bits) : -1;
-    ok = id >= 0;
-    return (int64_t)(ok ? id : 0) * a.c.n_kv_heads + hk;
+  // (entries are fetched a step before the pages they name, see above)
+  auto entry = [&](int key) { return (uint32_t)row_table[(key < k1 ? key : k1 - 1) >> a.page_bits]; };
+  auto entries = [&](int unit) {
+#pragma unroll
+    for (int i = 0; i < LR; ++i) kid[i] = entry(unit + kgroup + i * KSTEP);
+    vid = entry(unit + vgroup);
   };
   auto load = [&](int unit) {
-    bool ok;
 #pragma unroll
-    for (int i = 0; i < LR; ++i) {
-      const int key = unit + krow + i * KSTEP;
-      kr[i] = *reinterpret_cast<const uint4*>(a.c.k + slot_of(key, ok) * head_bytes + (int64_t)(key & (a.c.page - 1)) * DH + kch * 8);
-    }
-    const int key = unit + vgr * 16;
-    const int8_t* p = a.c.v + slot_of(key, ok) * head_bytes + (int64_t)vrow * a.c.page + (key & (a.c.page - 1));
+    for (int i = 0; i < LR; ++i)
+      kr[i] = *reinterpret_cast<const uint4*>(kp + (uint64_t)(kid[i] < n_pages ? kid[i] : 0) * page_stride +
+                                              ((unit + krow + i * KSTEP) & (a.c.page - 1)) * DH);
+    seen_next = vid < n_pages;
+    const uint32_t id = seen_next ? vid : 0;
+    const int8_t* p = vp + (uint64_t)id * page_stride + ((unit + vgroup) & (a.c.page - 1));
 #pragma unroll
-    for (int i = 0; i < LR; ++i) vr[i] = *reinterpret_cast<const uint4*>(p + (int64_t)i * 64 * a.c.page);
-    const int64_t slot = slot_of(unit + fq * 16, seen_next);
+    for (int i = 0; i < LR; ++i) vr[i] = *reinterpret_cast<const uint4*>(p + i * 64 * a.c.page);
+    const uint64_t slot = (uint64_t)id * a.c.n_kv_heads + hk;
     ks_next = seen_next ? a.c.k_step[slot] : 0.0f;
     vs_next = seen_next ? fmaxf(a.c.v_step[slot], kSmallStep) : 1.0f;
+    entries(unit + 64);
   };
-  // 16-byte chunks lie at chunk ^ key of their row: the rows that the 16 lanes of a fragment read name have different ones
+  // 16-byte chunks lie at chunk ^ key of their row: the rows that the 16 lanes of a fragment read name have different ones.
+  // (V's chunks 2 fq + u at 4 u + fq: the lanes that are served together have neighbouring fq)
   auto kkey = [](int row) { return DH == 128 ? (row >> 4 & 3) * 4 + (row & 3) : (row >> 4 & 3) * 2 + (row >> 1 & 1); };
   auto stage = [&](unsigned char* at) {
 #pragma unroll
@@ -345,8 +373,8 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
 #pragma unroll
     for (int i = 0; i < LR; ++i) {
       const int row = vrow + i * 64;
-      *reinterpret_cast<f16x8*>(at + row * VB + (((vgr * 2) ^ (row >> 1 & 7)) << 4)) = widen_codes8(vr[i].x, vr[i].y);
-      *reinterpret_cast<f16x8*>(at + row * VB + (((vgr * 2 + 1) ^ (row >> 1 & 7)) << 4)) = widen_codes8(vr[i].z, vr[i].w);
+      *reinterpret_cast<f16x8*>(at + row * VB + ((fq ^ (row >> 1 & 7)) << 4)) = widen_codes8(vr[i].x, vr[i].y);
+      *reinterpret_cast<f16x8*>(at + row * VB + (((fq + 4) ^ (row >> 1 & 7)) << 4)) = widen_codes8(vr[i].z, vr[i].w);
     }
   };
   const int my_row = (l16 >> 2) * 16 + (l16 & 3);           // row of K of score tile 0 (tile j: 4 j further, the same key)
@@ -354,6 +382,7 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
   const int vbase = 64 * KB + l16 * VB, vx = l16 >> 1;      // (row of V^T: 16 d + l16, the same key for all d)
 
   if (k0 < k1) {
+    entries(k0);
     load(k0);
     stage(lds);
     seen = seen_next; ks = ks_next; vs = vs_next;
@@ -385,7 +414,7 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
       if (unit + 128 < k1) load(unit + 128);
     }
     if (!work) continue;
-    const float lg = __log2f(vst), rv = 1.0f / vst;
+    const float lg = __builtin_amdgcn_logf(vst), rv = __builtin_amdgcn_rcpf(vst);
     if (unit + 64 > wfull || unit + 64 > wend || __any(!now_seen)) {
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
@@ -404,8 +433,7 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
       for (int e = 1; e < 16; ++e) mx = fmaxf(mx, sc[e >> 2][n][e & 3]);
       const float f = fmaxf(fac[n] * kst, 1e-37f);       // (zero times a masked product would not be -inf)
       mx = mx == -INFINITY ? mx : __builtin_fmaf(mx, f, lg);
-      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      mx = column_max(mx);
       if (mx > m_run[n]) {
         const float next = weight_ref(mx), alpha = exp2_fast(ref[n] - next);
         m_run[n] = mx;
@@ -428,7 +456,7 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
     for (int d = 0; d < ND; ++d)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const f16x8 vf = *reinterpret_cast<const f16x8*>(kv + vbase + d * 16 * VB + (((fq * 2 + u) ^ vx) << 4));
+        const f16x8 vf = *reinterpret_cast<const f16x8*>(kv + vbase + d * 16 * VB + (((fq + 4 * u) ^ vx) << 4));
         acc[d][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[0][u], acc[d][0], 0, 0, 0);
         acc[d][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[1][u], acc[d][1], 0, 0, 0);
       }
