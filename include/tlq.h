@@ -407,8 +407,10 @@ tlq_status tlq_kv_append(const void* K, int64_t ldk, const void* V, int64_t ldv,
  * scale: any finite number, 0 = 1 / sqrt(head_dim).  A row that sees no token gives zeros; a query that is not finite
  * makes its own row undefined and no other.  Scores, softmax and sums are
  * float; the matrix products take codes as they are, queries exactly (bf16 ones times a power of two of their row) and
- * probabilities times the page's step in fp16 with the largest at 2^15; Out is rounded to x_dtype.
- * Q, Out [n_tok, n_heads * head_dim] x_dtype, 16-byte aligned, strides multiples of 8; n_heads a multiple of n_kv_heads.
+ * probabilities times the page's step in fp16, which the softmax's sum takes as well; Out is rounded to x_dtype.  Steps have to
+ * be positive, and scores below 2^21 in size (beyond, a float holds them to a quarter at best); other rows are undefined.
+ * Q, Out [n_tok, n_heads * head_dim] x_dtype, 16-byte aligned, strides multiples of 8; n_heads a multiple of n_kv_heads;
+ * n_tok * (n_heads / n_kv_heads) and n_seq * n_kv_heads below 2^31 - 256.
  * The workspace query reads sizes only, no pointer; the result does not depend on the workspace's contents. */
 size_t tlq_kv_attention_workspace_bytes(int64_t n_tok, int32_t n_heads, const tlq_kv_batch* b, const tlq_kv_cache* c);
 tlq_status tlq_kv_attention(const void* Q, int64_t ldq, int64_t n_tok, int32_t n_heads, float scale, const tlq_kv_batch* b,

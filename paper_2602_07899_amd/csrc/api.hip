@@ -936,7 +936,8 @@ static tlq_status check_kv_sizes(const tlq_kv_batch* b, const tlq_kv_cache* c) {
   if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128 && c->page != 256) return TLQ_ERR_UNSUPPORTED;
   if (c->n_kv_heads <= 0 || c->n_kv_heads > 65535 || c->n_pages <= 0 || c->n_pages >= (1LL << 31) || b->n_seq <= 0 ||
       b->n_seq > 65535 || b->max_pages <= 0 || b->ld_table < b->max_pages || b->max_new <= 0 || b->max_len < b->max_new ||
-      b->max_len > (1 << 30))
+      b->max_len > (1 << 30) ||
+      (int64_t)b->n_seq * c->n_kv_heads >= (1LL << 31))
     return TLQ_ERR_SHAPE;
   return TLQ_OK;
 }
@@ -961,7 +962,9 @@ tlq_status tlq_kv_append(const void* K, int64_t ldk, const void* V, int64_t ldv,
 }
 
 static tlq_status check_kv_heads(int64_t n_tok, int32_t n_heads, const tlq_kv_cache* c) {
-  if (n_tok <= 0 || n_tok >= (1LL << 31) || n_heads <= 0 || n_heads > 65535 || (n_heads % c->n_kv_heads) != 0) return TLQ_ERR_SHAPE;
+  if (n_tok <= 0 || n_tok >= (1LL << 31) || n_heads <= 0 || n_heads > 65535 || (n_heads % c->n_kv_heads) != 0 ||
+      n_tok * (n_heads / c->n_kv_heads) >= (1LL << 31) - 256)      // (rows are counted in 32 bits)
+    return TLQ_ERR_SHAPE;
   return TLQ_OK;
 }
 

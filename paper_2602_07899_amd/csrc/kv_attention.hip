@@ -5,9 +5,11 @@
 //   out = sum_j 2^(z_j - m) vcode_j  /  sum_j 2^(z_j - m) / vs(j):
 // the values' step goes into the exponent for nothing, so that the codes enter the second product as they are and the
 // weights that are rounded to 16 bits are those of the contributions, not of the probabilities - a page of small values
-// (a first token's) cannot push the rest below the smallest half.  m is the running maximum of z less 15: the largest
-// weight is exactly 2^15, and weights stay normal halves down to 2^-29 of it (with the largest at 1, 2^-14: over 10^5 keys
-// what falls below would show).  Both products run on fp16 matrix instructions whatever x_dtype is: codes are exact in
+// (a first token's) cannot push the rest below the smallest half.  m, the row's reference, is 7 below the largest z when it
+// is set, and is set again when a z lies 15 above it: weights stay between 2^15 and, as normal halves, 2^-21 of the largest
+// at least (with the largest at 1, 2^-14: over 10^5 keys what falls below would show), and sums are rescaled a few times a
+// row instead of at every new maximum.  The denominator sums the rounded weights, in 32 bits: where one key has nearly all
+// of the weight its rounding cancels.  Both products run on fp16 matrix instructions whatever x_dtype is: codes are exact in
 // fp16; bf16 queries are multiplied with the power of two that brings the largest of the row to [2^14, 2^15).
 // The products are transposed, S^T = K Q^T and O^T = V^T P^T, so that a lane owns one query column and P stays in
 // registers; values are stored channel by channel so that V^T's rows are read as they lie.
@@ -22,20 +24,36 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
 
+// r / d for 0 <= r < 2^31, 1 <= d < 2^31, as a product: m = ceil(2^(31+s) / d), s = ceil(log2 d)
+struct KvDiv {
+  uint32_t m, s, d;
+  __device__ __forceinline__ uint32_t of(uint32_t r) const { return __umulhi(r << 1, m) >> s; }
+};
+static KvDiv kv_div(uint32_t d) {
+  uint32_t s = 0;
+  while ((1ull << s) < d) ++s;
+  return {(uint32_t)(((1ull << (31 + s)) + d - 1) / d), s, d};
+}
+
 struct KvAttnDev {
-  const uint16_t* Q; int64_t ldq, n_tok; int n_heads, group; float scale2;    // scale * log2(e)
+  const uint16_t* Q; int64_t ldq, n_tok; int n_heads, group; KvDiv by_group; float scale2;    // scale * log2(e)
   tlq_kv_batch b; tlq_kv_cache c; int page_bits;
   uint16_t* Out; int64_t ldo;
   int n_splits, chunk;          // keys of a split
-  int tiles; unsigned ways, members; int64_t n_pairs;      // kv_prompt_kernel: row tiles, and the order of its blocks
+  int tiles; unsigned way_bits, member_bits, n_pairs; KvDiv by_heads;      // kv_prompt_kernel: row tiles, and the order of its blocks
   float2* ml; float* acc;       // per (row, head, split): reference and sum; [head_dim] sums of codes
 };
 
 #if defined(__HIP_DEVICE_COMPILE__)
 constexpr float kSmallStep = 1e-30f;    // (a step of zero: its codes' page counts as zeros)
-// The reference for a largest exponent m: the weight of m is 2^15 exactly.  (Exponents so large that m - 15 is not exact have
-// weight 1: a rounded reference could push it beyond the largest half.)
-__device__ __forceinline__ float weight_ref(float m) { return m - (fabsf(m) < 4194304.0f ? 15.0f : 0.0f); }
+constexpr float kTop = 7.0f, kRaise = 15.0f;      // exponents of the largest weight: when the reference is set, at most
+// sum of eight weights (rounded already) and c
+__device__ __forceinline__ float add_weights(f16x8 w, float c) {
+  const f16x2 one = {(_Float16)1.0f, (_Float16)1.0f};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_fdot2(f16x2{w[2 * i], w[2 * i + 1]}, one, c, false);
+  return c;
+}
 // four codes -> four halves: byte + 128 behind the exponent of 1024, less 1152
 __device__ __forceinline__ void widen_codes(uint32_t w, uint32_t& lo, uint32_t& hi) {
   w ^= 0x80808080u;
@@ -113,14 +131,12 @@ __global__ __launch_bounds__(256, 3) void kv_few_kernel(KvAttnDev a) {
   const int s = blockIdx.z, hk = blockIdx.y;
   const int tile = (int)blockIdx.x / a.n_splits, split = (int)blockIdx.x % a.n_splits;
   const KvSeq q = kv_sequence(a.b, a.c.page, a.n_tok, s);
-  const int64_t rows = (int64_t)q.n_new * a.group;
-  const int64_t first_row = (int64_t)tile * 16;
+  const uint32_t rows = (uint32_t)q.n_new * a.group, first_row = (uint32_t)tile * 16;
   if (first_row >= rows) return;
-  const int64_t row = first_row + l16 < rows ? first_row + l16 : rows - 1;
-  const int qi = (int)(row / a.group), g = (int)(row % a.group);
+  const uint32_t row = first_row + l16 < rows ? first_row + l16 : rows - 1;
+  const int qi = (int)a.by_group.of(row), g = (int)(row - qi * a.group);
   const int pos = q.first + qi;
-  const int64_t last_row = first_row + 15 < rows ? first_row + 15 : rows - 1;
-  const int last = q.first + (int)(last_row / a.group);      // the tile's latest position
+  const int last = q.first + (int)a.by_group.of(first_row + 15 < rows ? first_row + 15 : rows - 1);      // the tile's latest position
   const int end = last + 1 < q.len ? last + 1 : q.len;
   const int k0 = split * a.chunk;
   if (k0 >= end && a.n_splits > 1) return;
@@ -133,7 +149,7 @@ __global__ __launch_bounds__(256, 3) void kv_few_kernel(KvAttnDev a) {
   f32x4 acc[ND];
 #pragma unroll
   for (int d = 0; d < ND; ++d) acc[d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  float m_run = -INFINITY, ref = -INFINITY, l_run = 0.0f;      // largest exponent, its reference, this lane's share of the sum
+  float ref = -INFINITY, l_run = 0.0f;      // the row's reference, this lane's share of its sum
 
   uint4 kr[4][LW], vr[ND];
   float ks = 0.0f, vs = 1.0f;
@@ -201,9 +217,8 @@ __global__ __launch_bounds__(256, 3) void kv_few_kernel(KvAttnDev a) {
         mx = fmaxf(mx, sc[j][r]);
       }
     mx = column_max(mx);
-    if (mx > m_run) {
-      const float next = weight_ref(mx), alpha = exp2_fast(ref - next);       // (0 at the first visible key)
-      m_run = mx;
+    if (mx > ref + kRaise) {
+      const float next = mx - kTop, alpha = exp2_fast(ref - next);       // (0 at the first visible key)
       ref = next;
       l_run *= alpha;
 #pragma unroll
@@ -211,16 +226,9 @@ __global__ __launch_bounds__(256, 3) void kv_few_kernel(KvAttnDev a) {
     }
     const float from = ref == -INFINITY ? 0.0f : ref;
     f16x8 pf[2];
-    float ps = 0.0f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float e = exp2_fast(sc[j][r] - from);
-        ps += e;
-        pf[j >> 1][(j & 1) * 4 + r] = (_Float16)e;
-      }
-    l_run = __builtin_fmaf(ps, rv, l_run);
+    for (int e = 0; e < 16; ++e) pf[e >> 3][e & 7] = (_Float16)exp2_fast(sc[e >> 2][e & 3] - from);
+    l_run = __builtin_fmaf(add_weights(pf[1], add_weights(pf[0], 0.0f)), rv, l_run);
 #pragma unroll
     for (int d = 0; d < ND; ++d) {
       acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen_codes8(vr[d].x, vr[d].y), pf[0], acc[d], 0, 0, 0);
@@ -250,7 +258,8 @@ __global__ __launch_bounds__(256, 3) void kv_few_kernel(KvAttnDev a) {
     if (ml[w][r].x != -INFINITY) l += ml[w][r].y * exp2_fast(ml[w][r].x - m);
 #pragma unroll
   for (int e = 0; e < PER; ++e) o[e] = (part[0][r][d0 + e] + part[1][r][d0 + e]) + (part[2][r][d0 + e] + part[3][r][d0 + e]);
-  const int64_t orow = first_row + r, token = q.row0 + orow / a.group, head = (int64_t)hk * a.group + orow % a.group;
+  const uint32_t oq = a.by_group.of(first_row + r);
+  const int64_t token = q.row0 + oq, head = (int64_t)hk * a.group + (first_row + r - oq * a.group);
   if (a.n_splits > 1) {
     const int64_t at = (token * a.n_heads + head) * a.n_splits + split;
     if ((tid & 15) == 0) a.ml[at] = make_float2(m, l);
@@ -286,24 +295,25 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, fq = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // blockIdx.x = ways * (members * (split, tile) + member) + pair
-  unsigned pair = blockIdx.x % a.ways, rest = blockIdx.x / a.ways;
-  const unsigned which = rest / a.members, member = rest - which * a.members;
-  const int64_t sh = (((int64_t)blockIdx.z * gridDim.y + blockIdx.y) * a.members + member) * a.ways + pair;
+  const unsigned pair = blockIdx.x & ((1u << a.way_bits) - 1), rest = blockIdx.x >> a.way_bits;
+  const unsigned which = rest >> a.member_bits, member = rest & ((1u << a.member_bits) - 1);
+  const unsigned sh = ((((blockIdx.z * gridDim.y + blockIdx.y) << a.member_bits) + member) << a.way_bits) + pair;
   if (sh >= a.n_pairs) return;
-  const int tile = a.tiles - 1 - (int)which / a.n_splits, split = (int)which % a.n_splits;
-  const int s = (int)(sh / a.c.n_kv_heads), hk = (int)(sh % a.c.n_kv_heads);
+  const unsigned turn = a.n_splits == 1 ? which : which / (unsigned)a.n_splits;
+  const int tile = a.tiles - 1 - (int)turn, split = (int)(which - turn * a.n_splits);
+  const int s = (int)a.by_heads.of(sh), hk = (int)(sh - s * a.by_heads.d);
   const KvSeq q = kv_sequence(a.b, a.c.page, a.n_tok, s);
-  const int64_t rows = (int64_t)q.n_new * a.group, first_row = (int64_t)tile * 128;
+  const uint32_t rows = (uint32_t)q.n_new * a.group, first_row = (uint32_t)tile * 128;
   if (first_row >= rows) return;
-  auto last_key = [&](int64_t r) {      // number of keys that rows up to r see
-    const int p = q.first + (int)((r < rows - 1 ? r : rows - 1) / a.group);
+  auto last_key = [&](uint32_t r) {      // number of keys that rows up to r see
+    const int p = q.first + (int)a.by_group.of(r < rows - 1 ? r : rows - 1);
     return p + 1 < q.len ? p + 1 : q.len;
   };
   const int end = last_key(first_row + 127);
   const int k0 = split * a.chunk;
   if (k0 >= end && a.n_splits > 1) return;
   const int k1 = end - k0 < a.chunk ? end : k0 + a.chunk;
-  const int64_t wrow = first_row + wave * 32;
+  const uint32_t wrow = first_row + wave * 32;
   const int wend = wrow < rows ? (last_key(wrow + 31) < k1 ? last_key(wrow + 31) : k1) : 0;    // keys of this wave
   const int wfull = wrow < rows ? last_key(wrow) : 0;                                          // keys that all of its rows see
 
@@ -312,8 +322,8 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
   int pos[2];
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
-    const int64_t r = wrow + n * 16 + l16 < rows ? wrow + n * 16 + l16 : rows - 1;
-    const int qi = (int)(r / a.group), g = (int)(r % a.group);
+    const uint32_t r = wrow + n * 16 + l16 < rows ? wrow + n * 16 + l16 : rows - 1;
+    const int qi = (int)a.by_group.of(r), g = (int)(r - qi * a.group);
     pos[n] = q.first + qi;
     const uint16_t* p = a.Q + (q.row0 + qi) * a.ldq + ((int64_t)hk * a.group + g) * DH + fq * 8;
     fac[n] = fabsf(a.scale2) * load_queries<T, NS, 32>(p, qf[n], a.scale2 < 0.0f);
@@ -321,7 +331,7 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
   f32x4 acc[ND][2];
 #pragma unroll
   for (int d = 0; d < ND; ++d) acc[d][0] = acc[d][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  float m_run[2] = {-INFINITY, -INFINITY}, ref[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.0f, 0.0f};
+  float ref[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.0f, 0.0f};
 
   // what a thread moves: K rows tid / (CPK / 2) and further ones, 16 codes; V channels 16 wave + l16 and 64 further, the 16 keys
   // that it has the scores of.  A wave's K rows of one load lie in one page.
@@ -392,7 +402,8 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
   for (int unit = k0; unit < k1; unit += 64, cur ^= 1) {
     __syncthreads();
     const unsigned char* kv = lds + cur * STAGE;
-    const bool work = unit < wend;
+    const bool work = unit < wend, now_seen = seen;
+    const float kst = ks, vst = vs;
     f32x4 sc[4][2];
     if (work) {
 #pragma unroll
@@ -406,69 +417,71 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
         }
       }
     }
-    const bool now_seen = seen;
-    const float kst = ks, vst = vs;
     if (unit + 64 < k1) {
       stage(lds + (cur ^ 1) * STAGE);
       seen = seen_next; ks = ks_next; vs = vs_next;
       if (unit + 128 < k1) load(unit + 128);
     }
     if (!work) continue;
-    const float lg = __builtin_amdgcn_logf(vst), rv = __builtin_amdgcn_rcpf(vst);
     if (unit + 64 > wfull || unit + 64 > wend || __any(!now_seen)) {
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
         const int limit = now_seen ? (pos[n] < k1 - 1 ? pos[n] : k1 - 1) - (unit + fq * 16) : -1;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) sc[j][n][r] = 4 * j + r <= limit ? sc[j][n][r] : -INFINITY;
+        for (int e = 0; e < 16; ++e) sc[e >> 2][n][e & 3] = e <= limit ? sc[e >> 2][n][e & 3] : -INFINITY;
       }
     }
-    f16x8 pf[2][2];
+    const float lg = __builtin_amdgcn_logf(vst), rv = __builtin_amdgcn_rcpf(vst);
+    float f[2], mx[2];
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
-      float mx = sc[0][n][0];
+      f[n] = fmaxf(fac[n] * kst, 1e-37f);       // (zero times a masked product would not be -inf)
+      mx[n] = sc[0][n][0];
 #pragma unroll
-      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, sc[e >> 2][n][e & 3]);
-      const float f = fmaxf(fac[n] * kst, 1e-37f);       // (zero times a masked product would not be -inf)
-      mx = mx == -INFINITY ? mx : __builtin_fmaf(mx, f, lg);
-      mx = column_max(mx);
-      if (mx > m_run[n]) {
-        const float next = weight_ref(mx), alpha = exp2_fast(ref[n] - next);
-        m_run[n] = mx;
-        ref[n] = next;
-        l_run[n] *= alpha;
-#pragma unroll
-        for (int d = 0; d < ND; ++d) acc[d][n] *= alpha;
-      }
-      const float off = ref[n] != -INFINITY ? lg - ref[n] : 0.0f;
-      float ps = 0.0f;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float w = exp2_fast(__builtin_fmaf(sc[e >> 2][n][e & 3], f, off));
-        ps += w;
-        pf[n][e >> 3][e & 7] = (_Float16)w;
-      }
-      l_run[n] = __builtin_fmaf(ps, rv, l_run[n]);
+      for (int e = 1; e < 16; ++e) mx[n] = fmaxf(mx[n], sc[e >> 2][n][e & 3]);
+      mx[n] = column_max(mx[n] == -INFINITY ? mx[n] : __builtin_fmaf(mx[n], f[n], lg));
     }
+    if (__any(mx[0] > ref[0] + kRaise || mx[1] > ref[1] + kRaise)) {
 #pragma unroll
-    for (int d = 0; d < ND; ++d)
+      for (int n = 0; n < 2; ++n)
+        if (mx[n] > ref[n] + kRaise) {
+          const float next = mx[n] - kTop, alpha = exp2_fast(ref[n] - next);
+          ref[n] = next;
+          l_run[n] *= alpha;
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const f16x8 vf = *reinterpret_cast<const f16x8*>(kv + vbase + d * 16 * VB + (((fq + 4 * u) ^ vx) << 4));
-        acc[d][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[0][u], acc[d][0], 0, 0, 0);
-        acc[d][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[1][u], acc[d][1], 0, 0, 0);
+          for (int d = 0; d < ND; ++d) acc[d][n] *= alpha;
+        }
+    }
+    float off[2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) off[n] = ref[n] != -INFINITY ? lg - ref[n] : 0.0f;
+    // half of the keys after the other, so that the weights of one are formed beside the products of the other
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      f16x8 pf[2];
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) pf[n][e] = (_Float16)exp2_fast(__builtin_fmaf(sc[2 * u + (e >> 2)][n][e & 3], f[n], off[n]));
+        l_run[n] = __builtin_fmaf(add_weights(pf[n], 0.0f), rv, l_run[n]);
       }
+#pragma unroll
+      for (int d = 0; d < ND; ++d) {
+        const f16x8 vf = *reinterpret_cast<const f16x8*>(kv + vbase + d * 16 * VB + (((fq + 4 * u) ^ vx) << 4));
+        acc[d][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[0], acc[d][0], 0, 0, 0);
+        acc[d][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[1], acc[d][1], 0, 0, 0);
+      }
+    }
   }
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
     float l = l_run[n];
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
-    const int64_t r = wrow + n * 16 + l16;
+    const uint32_t r = wrow + n * 16 + l16;
     if (r >= rows) continue;
-    const int64_t token = q.row0 + r / a.group, head = (int64_t)hk * a.group + r % a.group;
+    const uint32_t qi = a.by_group.of(r);
+    const int64_t token = q.row0 + qi, head = (int64_t)hk * a.group + (r - qi * a.group);
     if (a.n_splits > 1) {
       const int64_t at = (token * a.n_heads + head) * a.n_splits + split;
       if (fq == 0) a.ml[at] = make_float2(ref[n], l);
@@ -493,7 +506,7 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
 // split, 1024 / DH splits side by side.
 constexpr int kMaxSplits = 1024;
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void kv_join_kernel(KvAttnDev a, int tile_rows) {
+__global__ __launch_bounds__(256) void kv_join_kernel(KvAttnDev a, uint32_t tile_rows) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int LPR = DH / 4, SIDE = 256 / LPR;
   __shared__ __attribute__((aligned(16))) float4 sum[SIDE][LPR];
@@ -503,10 +516,10 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnDev a, int tile_rows
   const KvSeq q = kv_sequence(a.b, a.c.page, a.n_tok, s);
   if (qi >= q.n_new) return;
   // the splits that its tile has written (see the kernels)
-  const int64_t rows = (int64_t)q.n_new * a.group;
-  int64_t last_row = ((int64_t)qi * a.group + head % a.group) / tile_rows * tile_rows + tile_rows - 1;
+  const uint32_t rows = (uint32_t)q.n_new * a.group;
+  uint32_t last_row = ((uint32_t)qi * a.group + (uint32_t)head % (uint32_t)a.group) / tile_rows * tile_rows + tile_rows - 1;
   if (last_row > rows - 1) last_row = rows - 1;
-  const int last = q.first + (int)(last_row / a.group);
+  const int last = q.first + (int)a.by_group.of(last_row);
   const int end = last + 1 < q.len ? last + 1 : q.len;
   const int n = end <= 0 ? 0 : (end + a.chunk - 1) / a.chunk;
   const int64_t at = ((q.row0 + qi) * a.n_heads + head) * a.n_splits;
@@ -596,13 +609,17 @@ hipError_t launch_kv_attention(const void* Q, int64_t ldq, int64_t n_tok, int n_
   a.ml = (float2*)workspace; a.acc = (float*)((unsigned char*)workspace + p.acc_at);
   const int64_t most = b.max_new < n_tok ? b.max_new : n_tok;
   a.tiles = p.tiles;
-  a.n_pairs = (int64_t)b.n_seq * c.n_kv_heads;
-  a.ways = a.n_pairs < 8 ? (unsigned)a.n_pairs : 8u;
-  const int64_t groups = ceil_div(a.n_pairs, a.ways);
-  a.members = (unsigned)(groups < 8 ? groups : 8);
-  const int64_t chunks = ceil_div(groups, a.members), gy = chunks < 32768 ? chunks : 32768;
-  const int64_t work = (int64_t)p.tiles * p.n_splits, gx = p.prompt ? work * a.ways * a.members : work;
-  if (gx > 0x7fffffffLL) return hipErrorInvalidValue;
+  a.by_group = kv_div((uint32_t)a.group);
+  a.by_heads = kv_div((uint32_t)c.n_kv_heads);
+  const int64_t n_pairs = (int64_t)b.n_seq * c.n_kv_heads;
+  a.n_pairs = (unsigned)n_pairs;
+  // (powers of two: up to eight pairs side by side, and up to eight of an XCD together)
+  for (a.way_bits = 0; a.way_bits < 3 && (2 << a.way_bits) <= n_pairs; ++a.way_bits) {}
+  const int64_t groups = ceil_div(n_pairs, 1 << a.way_bits);
+  for (a.member_bits = 0; a.member_bits < 3 && (2 << a.member_bits) <= groups; ++a.member_bits) {}
+  const int64_t chunks = ceil_div(groups, 1 << a.member_bits), gy = chunks < 32768 ? chunks : 32768;
+  const int64_t work = (int64_t)p.tiles * p.n_splits, gx = p.prompt ? work << (a.way_bits + a.member_bits) : work;
+  if (gx > 0x7fffffffLL || n_pairs >= (1LL << 31)) return hipErrorInvalidValue;
   const dim3 grid = p.prompt ? dim3((unsigned)gx, (unsigned)gy, (unsigned)ceil_div(chunks, gy))
                              : dim3((unsigned)gx, (unsigned)c.n_kv_heads, (unsigned)b.n_seq);
   auto pick = [&](auto t, auto dh) {
@@ -615,7 +632,7 @@ hipError_t launch_kv_attention(const void* Q, int64_t ldq, int64_t n_tok, int n_
     }
     if (hipError_t e = hipGetLastError(); e != hipSuccess || p.n_splits == 1) return e;
     ProfScope ps("kv_join", stream, 4.0 * (double)n_tok * n_heads * p.n_splits * c.head_dim);
-    kv_join_kernel<T, DH><<<dim3((unsigned)most, (unsigned)n_heads, (unsigned)b.n_seq), 256, 0, stream>>>(a, p.rows);
+    kv_join_kernel<T, DH><<<dim3((unsigned)most, (unsigned)n_heads, (unsigned)b.n_seq), 256, 0, stream>>>(a, (uint32_t)p.rows);
     return hipGetLastError();
   };
   using W128 = std::integral_constant<int, 128>;

@@ -328,11 +328,12 @@ def _check_attention(gpu, c, heads, dt, q, scale=0.0):
     none = np.isnan(want[:, 0])
     assert np.all(got[none] == 3.0)                            # rows behind the last sequence stay as they were
     got, want, mag, sens = got[~none], want[~none], mag[~none], np.repeat(sens[~none], c.dh, 1)
-    # weights in 16 bits (2^-11; those below 2^-29 of the largest: 2^-40 of it), scores as sums of dh products (a relative
-    # error of e^(2 ds) in p and in the sum of p), sums over the keys in 32 bits, the output
+    # weights in 16 bits, above the line and below it: sum_j p_j e_j (v_j - out), |e_j| <= 2^-11, at most 2^-11 (mag + |out|);
+    # those below 2^-21 of the largest to 2^-32 of it; scores as sums of dh products (a relative error of e^(2 ds) in p and in
+    # the sum of p), sums over the keys in 32 bits, the output
     n = c.max_len
     ds = ((c.dh + 6) * sens + 64) * U
-    bound = mag * (2.0 ** -11 + 2.1 * ds + (n / 4 + 64) * U) + n * 2.0 ** -40 * 127 * c.vs.max() + np.abs(want) * HALF[dt] * 1.001 + TINY[dt] * 1.01
+    bound = (mag + np.abs(want)) * 2.0 ** -11 + mag * (2.1 * ds + (n / 4 + 64) * U) + n * 2.0 ** -32 * 127 * c.vs.max() + np.abs(want) * HALF[dt] * 1.001 + TINY[dt] * 1.01
     within(got, want, bound)
     # well inside on average: the weights' roundings do not line up
     assert np.abs(got - want).mean() <= 0.6 * bound.mean()
@@ -391,7 +392,7 @@ def test_kv_attention_of_pages_that_are_not_there(gpu):
         got = _attend(gpu, c, 4, dt, q)
         want, mag, sens = ob.kv_attention(q, 4, c.kc, c.ks, c.vc, c.vs, c.cu, c.lens, c.table, c.max_len)
         ds = ((128 + 6) * np.repeat(sens, 128, 1) + 64) * U
-        within(got, want, mag * (2.0 ** -11 + 2.1 * ds + 200 * U) + 200 * 2.0 ** -40 * 127 * top + np.abs(want) * HALF[dt] * 1.001 + TINY[dt] * 1.01)
+        within(got, want, (mag + np.abs(want)) * 2.0 ** -11 + mag * (2.1 * ds + 200 * U) + 200 * 2.0 ** -32 * 127 * top + np.abs(want) * HALF[dt] * 1.001 + TINY[dt] * 1.01)
         assert (want == 0).all(axis=1).any()
 
 
@@ -499,7 +500,7 @@ def test_a_block_in_eight_bits(gpu, dt, heads, kv, dh):
         a = tlq.kv_attention(q, heads, batch, cache, p, new(n, heads * dh))
         want, mag, sens = ob.kv_attention(host(q), heads, c.kc, c.ks, c.vc, c.vs, cu, lens, c.table, 64)
         ds = ((dh + 6) * np.repeat(sens, dh, 1) + 64) * U
-        within(host(a), want, mag * (2.0 ** -11 + 2.1 * ds + 100 * U) + np.abs(want) * HALF[dt] * 1.001 + TINY[dt] + 1e-7)
+        within(host(a), want, (mag + np.abs(want)) * 2.0 ** -11 + mag * (2.1 * ds + 100 * U) + np.abs(want) * HALF[dt] * 1.001 + TINY[dt] + 1e-7)
         h = tlq.residual_add(h, linear(a, "o"), p, h)
         gu = linear(tlq.rmsnorm_mul(h, p, new(n, d)), "gate_up")
         m = tlq.silu_mul(gu[:, :ffn], gu[:, ffn:], p, new(n, ffn))
