@@ -44,6 +44,14 @@ struct KvAttnDev {
   float2* ml; float* acc;       // per (row, head, split): reference and sum; [head_dim] sums of codes
 };
 
+template <int I, int N, typename Fn>
+__device__ __forceinline__ void static_for(Fn&& f) {
+  if constexpr (I < N) {
+    f(std::integral_constant<int, I>{});
+    static_for<I + 1, N>(f);
+  }
+}
+
 #if defined(__HIP_DEVICE_COMPILE__)
 constexpr float kSmallStep = 1e-30f;    // (a step of zero: its codes' page counts as zeros)
 constexpr float kTop = 7.0f, kRaise = 15.0f;      // exponents of the largest weight: when the reference is set, at most
@@ -372,20 +380,21 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
   // 16-byte chunks lie at chunk ^ key of their row: the rows that the 16 lanes of a fragment read name have different ones.
   // (V's chunks 2 fq + u at 4 u + fq: the lanes that are served together have neighbouring fq)
   auto kkey = [](int row) { return DH == 128 ? (row >> 4 & 3) * 4 + (row & 3) : (row >> 4 & 3) * 2 + (row >> 1 & 1); };
-  auto stage = [&](unsigned char* at) {
-#pragma unroll
-    for (int i = 0; i < LR; ++i) {
-      const int row = krow + i * KSTEP;
-      *reinterpret_cast<f16x8*>(at + row * KB + ((kch ^ kkey(row)) << 4)) = widen_codes8(kr[i].x, kr[i].y);
-      *reinterpret_cast<f16x8*>(at + row * KB + (((kch + 1) ^ kkey(row)) << 4)) = widen_codes8(kr[i].z, kr[i].w);
+  // one of a thread's 4 LR pieces of the next stage: eight codes, widened
+  auto stage = [&](unsigned char* at, auto piece) __attribute__((always_inline)) {
+    constexpr int I = decltype(piece)::value, L = I >> 1 & (LR - 1), HALF = I & 1;
+    const uint4 raw = I < 2 * LR ? kr[L] : vr[L];
+    const f16x8 v = HALF ? widen_codes8(raw.z, raw.w) : widen_codes8(raw.x, raw.y);
+    if constexpr (I < 2 * LR) {
+      const int row = krow + L * KSTEP;
+      *reinterpret_cast<f16x8*>(at + row * KB + (((kch + HALF) ^ kkey(row)) << 4)) = v;
+    } else {
+      const int row = vrow + L * 64;
+      *reinterpret_cast<f16x8*>(at + 64 * KB + row * VB + (((fq + 4 * HALF) ^ (row >> 1 & 7)) << 4)) = v;
     }
-    at += 64 * KB;
-#pragma unroll
-    for (int i = 0; i < LR; ++i) {
-      const int row = vrow + i * 64;
-      *reinterpret_cast<f16x8*>(at + row * VB + ((fq ^ (row >> 1 & 7)) << 4)) = widen_codes8(vr[i].x, vr[i].y);
-      *reinterpret_cast<f16x8*>(at + row * VB + (((fq + 4) ^ (row >> 1 & 7)) << 4)) = widen_codes8(vr[i].z, vr[i].w);
-    }
+  };
+  auto stage_all = [&](unsigned char* at) __attribute__((always_inline)) {
+    static_for<0, 4 * LR>([&](auto i) { stage(at, i); });
   };
   const int my_row = (l16 >> 2) * 16 + (l16 & 3);           // row of K of score tile 0 (tile j: 4 j further, the same key)
   const int kbase = my_row * KB, kx = kkey(my_row);
@@ -394,7 +403,7 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
   if (k0 < k1) {
     entries(k0);
     load(k0);
-    stage(lds);
+    stage_all(lds);
     seen = seen_next; ks = ks_next; vs = vs_next;
     if (k0 + 64 < k1) load(k0 + 64);
   }
@@ -405,20 +414,35 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
     const bool work = unit < wend, now_seen = seen;
     const float kst = ks, vst = vs;
     f32x4 sc[4][2];
+    unsigned char* next = lds + (cur ^ 1) * STAGE;
     if (work) {
+      // the scores, 2 k32 steps' fragments ahead; between their products the next stage is widened (behind the last step
+      // that is done with what the registers hold: nobody reads it)
+      f16x8 kf[2][4];
+      auto read_k = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        sc[j][0] = sc[j][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int j = 0; j < 4; ++j)
+          kf[i & 1][j] = *reinterpret_cast<const f16x8*>(kv + kbase + j * 4 * KB + (((i * 4 + fq) ^ kx) << 4));
+      };
+      read_k(0);
 #pragma unroll
-        for (int i = 0; i < NS; ++i) {
-          const f16x8 kf = *reinterpret_cast<const f16x8*>(kv + kbase + j * 4 * KB + (((i * 4 + fq) ^ kx) << 4));
-          sc[j][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[0][i], sc[j][0], 0, 0, 0);
-          sc[j][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[1][i], sc[j][1], 0, 0, 0);
-        }
-      }
+      for (int j = 0; j < 4; ++j) sc[j][0] = sc[j][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      static_for<0, NS>([&](auto ic) {
+        constexpr int i = decltype(ic)::value;
+        if constexpr (i + 1 < NS) read_k(i + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        static_for<0, 4>([&](auto jc) {
+          constexpr int j = decltype(jc)::value, at = i * 4 + j;      // 4 NS places for 4 LR pieces, NS = 2 LR
+          sc[j][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i & 1][j], qf[0][i], sc[j][0], 0, 0, 0);
+          sc[j][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i & 1][j], qf[1][i], sc[j][1], 0, 0, 0);
+          if constexpr ((at & 1) == 0) stage(next, std::integral_constant<int, at / 2>{});
+          __builtin_amdgcn_sched_barrier(0);
+        });
+      });
+    } else {
+      stage_all(next);
     }
     if (unit + 64 < k1) {
-      stage(lds + (cur ^ 1) * STAGE);
       seen = seen_next; ks = ks_next; vs = vs_next;
       if (unit + 128 < k1) load(unit + 128);
     }
@@ -455,23 +479,32 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
     float off[2];
 #pragma unroll
     for (int n = 0; n < 2; ++n) off[n] = ref[n] != -INFINITY ? lg - ref[n] : 0.0f;
-    // half of the keys after the other, so that the weights of one are formed beside the products of the other
+    // half of the keys after the other: the weights of the second half are formed between the products of the first
+    f16x8 pf[2][2], vf[4];
+    auto read_v = [&](int at) __attribute__((always_inline)) {
+      const int d = at % ND, u = at / ND;
+      vf[at & 3] = *reinterpret_cast<const f16x8*>(kv + vbase + d * 16 * VB + (((fq + 4 * u) ^ vx) << 4));
+    };
+    auto weigh = [&](auto uc, auto ec) __attribute__((always_inline)) {
+      constexpr int u = decltype(uc)::value, e = decltype(ec)::value;
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      f16x8 pf[2];
+      for (int n = 0; n < 2; ++n)
+        pf[u][n][e] = (_Float16)exp2_fast(__builtin_fmaf(sc[2 * u + (e >> 2)][n][e & 3], f[n], off[n]));
+    };
 #pragma unroll
-      for (int n = 0; n < 2; ++n) {
+    for (int at = 0; at < 4; ++at) read_v(at);
+    static_for<0, 8>([&](auto ec) { weigh(std::integral_constant<int, 0>{}, ec); });
+    static_for<0, 2 * ND>([&](auto ac) {
+      constexpr int at = decltype(ac)::value, d = at % ND, u = at / ND, E = 8 / ND;
+      acc[d][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[at & 3], pf[u][0], acc[d][0], 0, 0, 0);
+      acc[d][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[at & 3], pf[u][1], acc[d][1], 0, 0, 0);
+      if constexpr (at + 4 < 2 * ND) read_v(at + 4);
+      if constexpr (u == 0)
+        static_for<0, E>([&](auto ec) { weigh(std::integral_constant<int, 1>{}, std::integral_constant<int, d * E + decltype(ec)::value>{}); });
+      __builtin_amdgcn_sched_barrier(0);
+    });
 #pragma unroll
-        for (int e = 0; e < 8; ++e) pf[n][e] = (_Float16)exp2_fast(__builtin_fmaf(sc[2 * u + (e >> 2)][n][e & 3], f[n], off[n]));
-        l_run[n] = __builtin_fmaf(add_weights(pf[n], 0.0f), rv, l_run[n]);
-      }
-#pragma unroll
-      for (int d = 0; d < ND; ++d) {
-        const f16x8 vf = *reinterpret_cast<const f16x8*>(kv + vbase + d * 16 * VB + (((fq + 4 * u) ^ vx) << 4));
-        acc[d][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[0], acc[d][0], 0, 0, 0);
-        acc[d][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[1], acc[d][1], 0, 0, 0);
-      }
-    }
+    for (int n = 0; n < 2; ++n) l_run[n] = __builtin_fmaf(add_weights(pf[1][n], add_weights(pf[0][n], 0.0f)), rv, l_run[n]);
   }
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
