@@ -377,9 +377,11 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
     vs_next = seen_next ? fmaxf(a.c.v_step[slot], kSmallStep) : 1.0f;
     entries(unit + 64);
   };
-  // 16-byte chunks lie at chunk ^ key of their row: the rows that the 16 lanes of a fragment read name have different ones.
-  // (V's chunks 2 fq + u at 4 u + fq: the lanes that are served together have neighbouring fq)
-  auto kkey = [](int row) { return DH == 128 ? (row >> 4 & 3) * 4 + (row & 3) : (row >> 4 & 3) * 2 + (row >> 1 & 1); };
+  // Chunk c of a row lies at place(c) ^ key(row), such that neither the eight lanes of a write that are served together (128
+  // bytes) nor the sixteen of a read (lanes 0 - 3, 12 - 15, 20 - 27 of 32 and the others, 256 bytes) meet in a bank: sixteen
+  // bytes for each row parity and key.  Rows of 256 bytes have the even chunks in front, the others with bits 2 and 3 turned.
+  auto kkey = [](int row) { return DH == 128 ? (row >> 4 & 3) * 4 + (row & 3) : (row >> 4 & 1) * 4 + (row & 3); };
+  auto kplace = [](int c) { return DH == 128 ? c >> 1 ^ (c & 1) * 12 : c; };
   // one of a thread's 4 LR pieces of the next stage: eight codes, widened
   auto stage = [&](unsigned char* at, auto piece) __attribute__((always_inline)) {
     constexpr int I = decltype(piece)::value, L = I >> 1 & (LR - 1), HALF = I & 1;
@@ -387,10 +389,10 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
     const f16x8 v = HALF ? widen_codes8(raw.z, raw.w) : widen_codes8(raw.x, raw.y);
     if constexpr (I < 2 * LR) {
       const int row = krow + L * KSTEP;
-      *reinterpret_cast<f16x8*>(at + row * KB + (((kch + HALF) ^ kkey(row)) << 4)) = v;
+      *reinterpret_cast<f16x8*>(at + row * KB + ((kplace(kch + HALF) ^ kkey(row)) << 4)) = v;
     } else {
       const int row = vrow + L * 64;
-      *reinterpret_cast<f16x8*>(at + 64 * KB + row * VB + (((fq + 4 * HALF) ^ (row >> 1 & 7)) << 4)) = v;
+      *reinterpret_cast<f16x8*>(at + 64 * KB + row * VB + (((fq + 4 * HALF) ^ (row & 7)) << 4)) = v;
     }
   };
   auto stage_all = [&](unsigned char* at) __attribute__((always_inline)) {
@@ -398,7 +400,7 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
   };
   const int my_row = (l16 >> 2) * 16 + (l16 & 3);           // row of K of score tile 0 (tile j: 4 j further, the same key)
   const int kbase = my_row * KB, kx = kkey(my_row);
-  const int vbase = 64 * KB + l16 * VB, vx = l16 >> 1;      // (row of V^T: 16 d + l16, the same key for all d)
+  const int vbase = 64 * KB + l16 * VB, vx = l16 & 7;      // (row of V^T: 16 d + l16, the same key for all d)
 
   if (k0 < k1) {
     entries(k0);
@@ -422,7 +424,7 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
       auto read_k = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          kf[i & 1][j] = *reinterpret_cast<const f16x8*>(kv + kbase + j * 4 * KB + (((i * 4 + fq) ^ kx) << 4));
+          kf[i & 1][j] = *reinterpret_cast<const f16x8*>(kv + kbase + j * 4 * KB + ((kplace(i * 4 + fq) ^ kx) << 4));
       };
       read_k(0);
 #pragma unroll
