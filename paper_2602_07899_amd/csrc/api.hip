@@ -867,8 +867,7 @@ tlq_status tlq_row_codes(const void* X, int64_t n, int64_t c, int64_t ldx, const
   if (!dims_ok(n, c, ldx) || (c % 8) != 0 || ldc < int8_row(c) || ldc >= (1LL << 31)) return TLQ_ERR_SHAPE;
   if (!mat16_aligned(X, ldx) || !aligned(codes, 16) || (ldc % 16) != 0 || (factor && !aligned(factor, 16)) || !aligned(steps, 4))
     return TLQ_ERR_ALIGN;
-  return hip_status(launch_act_quant(X, n, c, ldx, p->x_dtype == TLQ_BF16, factor, 0, 1, bits, codes, steps,
-                                     (hipStream_t)stream, ldc));
+  return hip_status(launch_row_codes(X, n, c, ldx, p->x_dtype == TLQ_BF16, factor, bits, codes, ldc, steps, (hipStream_t)stream));
 }
 
 size_t tlq_linear_i8_workspace_bytes(int64_t n_tok, int64_t c_in) {
@@ -894,7 +893,7 @@ tlq_status tlq_linear_i8(const void* X, int64_t n_tok, int64_t c_in, int64_t ldx
   const int64_t ld8 = int8_row(c_in);
   int8_t* codes = c.take<int8_t>((size_t)n_tok * ld8);
   float* steps = c.take<float>((size_t)n_tok);
-  TLQ_HIP(launch_act_quant(X, n_tok, c_in, ldx, p->x_dtype == TLQ_BF16, factor, 0, 1, p->act_bits, codes, steps, st, ld8));
+  TLQ_HIP(launch_row_codes(X, n_tok, c_in, ldx, p->x_dtype == TLQ_BF16, factor, p->act_bits, codes, ld8, steps, st));
   if (n_tok <= kLinearFew)
     return hip_status(launch_linear_few({codes, n_tok, ld8, steps, w_codes, c_out, ldw, ld8, w_steps, Y, ldy, p->yref_dtype}, st));
   GemmArgs g{};

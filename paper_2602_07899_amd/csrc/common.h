@@ -174,6 +174,11 @@ hipError_t launch_act_quant(const void* X, int64_t n_tok, int64_t c_in, int64_t 
                             const float* inv_table, int k0, int nb, int act_bits, void* codes,
                             float* sigma, hipStream_t stream, int64_t ld8 = 0);
 
+// The same codes of one candidate (factor: [c_in] or NULL) as int8 rows of ldc bytes, zeros behind c_in up to the next multiple
+// of 128.
+hipError_t launch_row_codes(const void* X, int64_t n, int64_t c_in, int64_t ldx, bool bf16, const float* factor, int bits,
+                            int8_t* codes, int64_t ldc, float* steps, hipStream_t stream);
+
 // Wout[o,c] = round16(Win[o,c] * inv_s[c])
 hipError_t launch_fold_scale(const void* Win, int64_t c_out, int64_t c_in, int64_t ldw, bool bf16,
                              const float* inv_s, const uint32_t* xmax_bits, bool out_f16, void* Wout,

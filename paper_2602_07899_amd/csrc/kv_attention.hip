@@ -325,56 +325,53 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
   const int wend = wrow < rows ? (last_key(wrow + 31) < k1 ? last_key(wrow + 31) : k1) : 0;    // keys of this wave
   const int wfull = wrow < rows ? last_key(wrow) : 0;                                          // keys that all of its rows see
 
-  f16x8 qf[2][NS];
-  float fac[2];
-  int pos[2];
-#pragma unroll
-  for (int n = 0; n < 2; ++n) {
-    const uint32_t r = wrow + n * 16 + l16 < rows ? wrow + n * 16 + l16 : rows - 1;
-    const int qi = (int)a.by_group.of(r), g = (int)(r - qi * a.group);
-    pos[n] = q.first + qi;
-    const uint16_t* p = a.Q + (q.row0 + qi) * a.ldq + ((int64_t)hk * a.group + g) * DH + fq * 8;
-    fac[n] = fabsf(a.scale2) * load_queries<T, NS, 32>(p, qf[n], a.scale2 < 0.0f);
-  }
   f32x4 acc[ND][2];
 #pragma unroll
   for (int d = 0; d < ND; ++d) acc[d][0] = acc[d][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   float ref[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.0f, 0.0f};
 
   // what a thread moves: K rows tid / (CPK / 2) and further ones, 16 codes; V channels 16 wave + l16 and 64 further, the 16 keys
-  // that it has the scores of.  A wave's K rows of one load lie in one page.
+  // that it has the scores of.
   const int krow = tid / (CPK / 2), kch = tid % (CPK / 2) * 2, vrow = wave * 16 + l16;
   constexpr int KSTEP = 512 / CPK;                          // rows between a thread's loads of K
-  const int32_t* row_table = a.b.table + (int64_t)s * a.b.ld_table;
-  const int64_t head_bytes = (int64_t)a.c.page * DH;
-  const uint32_t page_stride = (uint32_t)a.c.n_kv_heads * a.c.page * DH, n_pages = (uint32_t)a.c.n_pages;
-  const int8_t* kp = a.c.k + hk * head_bytes + kch * 8;
-  const int8_t* vp = a.c.v + hk * head_bytes + vrow * a.c.page;
-  const int kgroup = wave * (KSTEP / 4) & ~15, vgroup = fq * 16;
+  // Table entries are the same for the whole block (scalar loads, a step before the pages they name are loaded); entries behind
+  // the last key are never seen, any will do, and one outside the pool becomes the first page, in reach and never seen.
+  // A step's first key is a multiple of 64, so a page's part of an offset is a scalar.
+  const auto row_table = (const __attribute__((address_space(4))) int32_t*)(a.b.table + (int64_t)s * a.b.ld_table);
+  const uint32_t head_bytes = (uint32_t)a.c.page * DH, page_stride = (uint32_t)a.c.n_kv_heads * head_bytes;
+  const uint32_t n_pages = (uint32_t)a.c.n_pages, in_page = (uint32_t)a.c.page - 1;
+  const int8_t *kp = a.c.k + (uint64_t)hk * head_bytes, *vp = a.c.v + (uint64_t)hk * head_bytes;
+  uint32_t koff[LR], voff[LR];
+#pragma unroll
+  for (int i = 0; i < LR; ++i) {
+    koff[i] = ((uint32_t)(krow + i * KSTEP) & in_page) * DH + kch * 8;
+    voff[i] = (uint32_t)(vrow + i * 64) * a.c.page + ((uint32_t)(fq * 16) & in_page);
+  }
   uint4 kr[LR], vr[LR];
-  uint32_t kid[LR], vid;
+  uint32_t ids[4];                     // of the next four 16 keys
   bool seen = false, seen_next = false;
   float ks = 0.0f, vs = 1.0f, ks_next = 0.0f, vs_next = 1.0f;
-  // (entries are fetched a step before the pages they name, see above)
-  auto entry = [&](int key) { return (uint32_t)row_table[(key < k1 ? key : k1 - 1) >> a.page_bits]; };
   auto entries = [&](int unit) {
 #pragma unroll
-    for (int i = 0; i < LR; ++i) kid[i] = entry(unit + kgroup + i * KSTEP);
-    vid = entry(unit + vgroup);
+    for (int g = 0; g < 4; ++g) ids[g] = (uint32_t)row_table[(unit + g * 16 < k1 ? unit + g * 16 : k1 - 1) >> a.page_bits];
   };
   auto load = [&](int unit) {
+    const uint32_t at = (uint32_t)unit & in_page;
 #pragma unroll
-    for (int i = 0; i < LR; ++i)
-      kr[i] = *reinterpret_cast<const uint4*>(kp + (uint64_t)(kid[i] < n_pages ? kid[i] : 0) * page_stride +
-                                              ((unit + krow + i * KSTEP) & (a.c.page - 1)) * DH);
-    seen_next = vid < n_pages;
-    const uint32_t id = seen_next ? vid : 0;
-    const int8_t* p = vp + (uint64_t)id * page_stride + ((unit + vgroup) & (a.c.page - 1));
+    for (int i = 0; i < LR; ++i) {     // (DH = 128: a wave's rows lie in one group of 16 keys; 64: wave w has group w)
+      const int g = DH == 128 ? (wave >> 1) + 2 * i : wave;
+      const uint32_t id = g == 0 ? ids[0] : g == 1 ? ids[1] : g == 2 ? ids[2] : ids[3];
+      kr[i] = *reinterpret_cast<const uint4*>(kp + ((uint64_t)(id < n_pages ? id : 0) * page_stride + at * DH) + koff[i]);
+    }
+    const uint32_t mine = fq < 2 ? (fq == 0 ? ids[0] : ids[1]) : (fq == 2 ? ids[2] : ids[3]);
+    seen_next = mine < n_pages;
+    const uint32_t id = seen_next ? mine : 0;
+    const int8_t* p = vp + at + (uint64_t)id * page_stride;
 #pragma unroll
-    for (int i = 0; i < LR; ++i) vr[i] = *reinterpret_cast<const uint4*>(p + i * 64 * a.c.page);
-    const uint64_t slot = (uint64_t)id * a.c.n_kv_heads + hk;
-    ks_next = seen_next ? a.c.k_step[slot] : 0.0f;
-    vs_next = seen_next ? fmaxf(a.c.v_step[slot], kSmallStep) : 1.0f;
+    for (int i = 0; i < LR; ++i) vr[i] = *reinterpret_cast<const uint4*>(p + voff[i]);
+    const uint64_t slot = (uint64_t)id * (uint32_t)a.c.n_kv_heads + (uint32_t)hk;
+    ks_next = a.c.k_step[slot];
+    vs_next = a.c.v_step[slot];
     entries(unit + 64);
   };
   // Chunk c of a row lies at place(c) ^ key(row), such that neither the eight lanes of a write that are served together (128
@@ -405,8 +402,26 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
   if (k0 < k1) {
     entries(k0);
     load(k0);
+  }
+  f16x8 qf[2][NS];
+  float fac[2];
+  int pos[2];
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    const uint32_t r = wrow + n * 16 + l16 < rows ? wrow + n * 16 + l16 : rows - 1;
+    const int qi = (int)a.by_group.of(r), g = (int)(r - qi * a.group);
+    pos[n] = q.first + qi;
+    const uint16_t* p = a.Q + (q.row0 + qi) * a.ldq + ((int64_t)hk * a.group + g) * DH + fq * 8;
+    fac[n] = fabsf(a.scale2) * load_queries<T, NS, 32>(p, qf[n], a.scale2 < 0.0f);
+  }
+  auto take_steps = [&]() {      // of the pages just staged
+    seen = seen_next;
+    ks = seen ? ks_next : 0.0f;
+    vs = seen ? fmaxf(vs_next, kSmallStep) : 1.0f;
+  };
+  if (k0 < k1) {
     stage_all(lds);
-    seen = seen_next; ks = ks_next; vs = vs_next;
+    take_steps();
     if (k0 + 64 < k1) load(k0 + 64);
   }
   int cur = 0;
@@ -445,7 +460,7 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
       stage_all(next);
     }
     if (unit + 64 < k1) {
-      seen = seen_next; ks = ks_next; vs = vs_next;
+      take_steps();
       if (unit + 128 < k1) load(unit + 128);
     }
     if (!work) continue;

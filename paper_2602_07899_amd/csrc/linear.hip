@@ -29,7 +29,7 @@ __global__ __launch_bounds__(NW * 64) void linear_few_kernel(LinearI8Args a) {
   i32x4 acc[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) acc[n] = i32x4{0, 0, 0, 0};
-  constexpr int U = NT <= 2 ? 8 : 4;
+  constexpr int U = NT == 1 ? 8 : 4;
   int c = c0;
   auto some = [&](auto count) {
     constexpr int N = decltype(count)::value;
@@ -71,9 +71,11 @@ __global__ __launch_bounds__(NW * 64) void linear_few_kernel(LinearI8Args a) {
 hipError_t launch_linear_few(const LinearI8Args& a, hipStream_t stream) {
   ProfScope ps("linear_few", stream, (double)a.c_out * (double)a.K);
   const unsigned bo = (unsigned)ceil_div(a.c_out, 16);
-  if (a.n_tok <= 16) linear_few_kernel<1, 8><<<dim3(bo, 1), 512, 0, stream>>>(a);
-  else if (a.n_tok <= 32) linear_few_kernel<2, 8><<<dim3(bo, 1), 512, 0, stream>>>(a);
-  else linear_few_kernel<4, 8><<<dim3(bo, (unsigned)ceil_div(a.n_tok, 64)), 512, 0, stream>>>(a);
+  auto go = [&](auto kern, int waves, int tokens) { kern<<<dim3(bo, (unsigned)ceil_div(a.n_tok, tokens)), waves * 64, 0, stream>>>(a); };
+  if (a.n_tok <= 16) go(linear_few_kernel<1, 16>, 16, 16);
+  else if (a.n_tok <= 32) go(linear_few_kernel<2, 16>, 16, 32);
+  else if (a.n_tok <= 48) go(linear_few_kernel<3, 16>, 16, 48);
+  else go(linear_few_kernel<4, 16>, 16, 64);
   return hipGetLastError();
 }
 

@@ -699,6 +699,87 @@ hipError_t launch_act_quant(const void* X, int64_t n_tok, int64_t c_in, int64_t 
   return hipGetLastError();
 }
 
+// Rows to int8 codes, one factor for each channel (a single candidate): W waves have a row, P passes of 512 W channels, which
+// stay in registers between the maximum and the codes, so that X is read once.  The same arithmetic as above, bit for bit.
+// With one wave a row a block has four rows.
+template <typename T, int W, int P>
+__global__ __launch_bounds__(W == 1 ? 256 : W * 64) void row_codes_kernel(const uint16_t* __restrict__ X, int64_t n, int64_t c_in,
+                                                                          int64_t ldx, const float* __restrict__ factor, float qa,
+                                                                          float* __restrict__ steps, int8_t* __restrict__ codes,
+                                                                          int64_t ldc) {
+  __shared__ float red[W];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t row = W == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
+  if (W == 1 && row >= n) return;
+  const int64_t c0 = ((W == 1 ? 0 : wave) * 64 + lane) * 8;
+  uint4 x[P];
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    const int64_t c = c0 + p * (512 * W);
+    x[p] = c < c_in ? *reinterpret_cast<const uint4*>(X + row * ldx + c) : make_uint4(0, 0, 0, 0);
+  }
+  float w[8], f[8], xt[8];
+  auto scaled = [&](int p) {       // (behind c_in zeros, whatever the factors are)
+    const int64_t c = c0 + p * (512 * W);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = 1.0f;
+    if (factor && c < c_in) load8(factor + c, f);
+    widen8<T>(x[p], w);
+    times8(w, f, xt);
+  };
+  float m = 0.0f;
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    scaled(p);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(xt[j]));
+  }
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+  if constexpr (W > 1) {
+    if (lane == 0) red[wave] = m;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < W; ++i) m = fmaxf(m, red[i]);
+  }
+  Grid g;
+  g.delta = fmaxf(m, kRangeFloor) / qa;
+  g.rd = __builtin_amdgcn_rcpf(g.delta);
+  g.lim = g.delta < 1e36f ? 0.49999976f - 4.8e-7f * (qa + 1.0f) : -1.0f;
+  if (lane == 0 && (W == 1 || wave == 0)) steps[row] = g.delta;
+  const int64_t end = (c_in + 127) / 128 * 128;
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    const int64_t c = c0 + p * (512 * W);
+    if (c >= end) break;
+    scaled(p);
+    float q[8];
+    if (!(rint_quotient8(xt, g, 0.0f, q) < g.lim)) divide8(xt, g, q);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q[j] = __builtin_amdgcn_fmed3f(q[j], -qa - 1.0f, qa);
+    *reinterpret_cast<uint2*>(codes + row * ldc + c) = make_uint2(pack_i8(q[0], q[1], q[2], q[3]), pack_i8(q[4], q[5], q[6], q[7]));
+  }
+}
+
+hipError_t launch_row_codes(const void* X, int64_t n, int64_t c_in, int64_t ldx, bool bf16, const float* factor, int bits,
+                            int8_t* codes, int64_t ldc, float* steps, hipStream_t stream) {
+  if (c_in > 16384) return launch_act_quant(X, n, c_in, ldx, bf16, factor, 0, 1, bits, codes, steps, stream, ldc);
+  ProfScope ps("row_codes", stream, 3.0 * (double)n * (double)c_in);
+  const float qa = (float)((1 << (bits - 1)) - 1);
+  auto go = [&](auto kern, int waves) {
+    kern<<<(unsigned)(waves == 1 ? ceil_div(n, 4) : n), (waves == 1 ? 256 : waves * 64), 0, stream>>>(
+        (const uint16_t*)X, n, c_in, ldx, factor, qa, steps, codes, ldc);
+  };
+  auto pick = [&](auto t) {
+    using T = decltype(t);
+    if (c_in <= 1024) go(row_codes_kernel<T, 1, 2>, 1);
+    else if (c_in <= 4096) go(row_codes_kernel<T, 4, 2>, 4);
+    else go(row_codes_kernel<T, 8, 4>, 8);
+  };
+  bf16 ? pick(BF16{}) : pick(F16{});
+  return hipGetLastError();
+}
+
 template <typename T, bool SYM, int MODE>
 static void launch_quant(QuantDev d, hipStream_t stream) {
   // Enough blocks to fill the chip: the candidates of small matrices are split over blockIdx.y (W is
