@@ -85,8 +85,8 @@ bool use_int8(const tlq_params* p, int64_t c_in) {
   return p->act_bits != 0 && (p->group == 0 || p->group == c_in) && c_in >= 72 && c_in <= 16384 &&
          (p->symmetric || p->bits <= 7);
 }
-// tlq_linear_i8: rows of at most this many codes (the sums stay below 2^31), and tokens up to which the kernels for few are taken
-constexpr int64_t kMaxLinearI8 = 65536, kLinearFew = 64;
+// tlq_linear_i8: rows of at most this many codes (the sums stay below 2^31)
+constexpr int64_t kMaxLinearI8 = 65536;
 int64_t int8_row(int64_t c_in) { return (int64_t)align_up((size_t)c_in, 128); }
 
 struct SearchPlan {
@@ -872,7 +872,8 @@ tlq_status tlq_row_codes(const void* X, int64_t n, int64_t c, int64_t ldx, const
 
 size_t tlq_linear_i8_workspace_bytes(int64_t n_tok, int64_t c_in) {
   if (n_tok <= 0 || c_in <= 0 || n_tok >= (1LL << 31) || c_in > kMaxLinearI8) return 0;
-  return align_up((size_t)n_tok * int8_row(c_in), 256) + align_up((size_t)n_tok * sizeof(float), 256);
+  return align_up((size_t)n_tok * int8_row(c_in), 256) + align_up((size_t)n_tok * sizeof(float), 256) +
+         (n_tok <= kLinearMidTokens ? (size_t)(n_tok < 64 ? n_tok : 64) * kLinearMidInts * sizeof(int) : 0);
 }
 
 tlq_status tlq_linear_i8(const void* X, int64_t n_tok, int64_t c_in, int64_t ldx, const float* factor,
@@ -893,9 +894,13 @@ tlq_status tlq_linear_i8(const void* X, int64_t n_tok, int64_t c_in, int64_t ldx
   const int64_t ld8 = int8_row(c_in);
   int8_t* codes = c.take<int8_t>((size_t)n_tok * ld8);
   float* steps = c.take<float>((size_t)n_tok);
-  TLQ_HIP(launch_row_codes(X, n_tok, c_in, ldx, p->x_dtype == TLQ_BF16, factor, p->act_bits, codes, ld8, steps, st));
-  if (n_tok <= kLinearFew)
-    return hip_status(launch_linear_few({codes, n_tok, ld8, steps, w_codes, c_out, ldw, ld8, w_steps, Y, ldy, p->yref_dtype}, st));
+  int* partial = c.take<int>(0);
+  const bool bf16 = p->x_dtype == TLQ_BF16;
+  const LinearI8Args l{codes, n_tok, ld8, steps, w_codes, c_out, ldw, ld8, w_steps, Y, ldy, p->yref_dtype};
+  TLQ_HIP(launch_row_codes(X, n_tok, c_in, ldx, bf16, factor, p->act_bits, codes, ld8, steps, st));
+  const LinearKind kind = linear_kind(n_tok, c_out, ld8);
+  if (kind == kLinearFew) return hip_status(launch_linear_few(l, st));
+  if (kind == kLinearMid) return hip_status(launch_linear_mid(l, linear_mid_splits(n_tok, c_out, ld8), partial, st));
   GemmArgs g{};
   g.X = codes; g.n_tok = n_tok; g.tok_scale = steps; g.Wh = w_codes; g.c_out = c_out; g.n_cand = 1; g.row_scale = w_steps;
   g.i8_k = c_in; g.c_in = g.ldx = ld8 / 2; g.ldw = ldw / 2;      // (in units of 16 bits)

@@ -259,13 +259,20 @@ hipError_t launch_rmsnorm_mul(const void* Z, int64_t ldz, const void* Zb, int64_
                               int64_t c, bool bf16, const float* m_a, const float* m_b, int period,
                               int split, void* out, int64_t ldo, hipStream_t stream);
 
-// products of few tokens' codes with stored codes (linear.hip); launch_gemm_store has the others.  K = row length in codes, a multiple of 128
+// products of tokens' codes with stored codes: few tokens (linear.hip, up to 64), up to kLinearMidTokens (there, too), any (launch_gemm_store).  K = row length in codes, a multiple of 128
 struct LinearI8Args {
   const int8_t* xc; int64_t n_tok, ldx; const float* xs;    // token codes and steps
   const int8_t* wc; int64_t c_out, ldw, K; const float* ws;
   void* Y; int64_t ldy; int ydt;
 };
+enum LinearKind { kLinearFew, kLinearMid, kLinearTiles };
+constexpr int64_t kLinearMidTokens = 256;
+LinearKind linear_kind(int64_t n_tok, int64_t c_out, int64_t K);
 hipError_t launch_linear_few(const LinearI8Args& a, hipStream_t stream);
+// for more tokens; partial: scratch of kLinearMidInts ints for each token of the first 64, not used with one split
+constexpr int64_t kLinearMidInts = 256 * 128;      // (splits times blocks of 128 outputs and 64 tokens are at most 256)
+int linear_mid_splits(int64_t n_tok, int64_t c_out, int64_t K);
+hipError_t launch_linear_mid(const LinearI8Args& a, int splits, int* partial, hipStream_t stream);
 
 // queries and keys of a decoder block (rope.hip)
 struct QkRopeArgs {

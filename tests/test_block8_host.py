@@ -37,7 +37,9 @@ def test_linear_refusals():
     assert call(work=None) == call(size=16) == tlq.ERR_WORKSPACE
     assert call(work=ODD) == tlq.ERR_ALIGN
     q = tlq.linear_i8_workspace_bytes
-    assert q(0, 8) == q(4, 0) == q(4, 65544) == q(1 << 31, 8) == 0 and q(3, 72) == 512 + 256
+    assert q(0, 8) == q(4, 0) == q(4, 65544) == q(1 << 31, 8) == 0 and q(300, 72) == 300 * 128 + 1280
+    # sums of parts of the codes: room for up to 64 tokens' at a time, up to 256 tokens
+    assert q(3, 72) == 512 + 256 + 3 * 131072 and q(256, 128) == 256 * 128 + 1024 + 64 * 131072
 
 
 def test_rope_refusals():

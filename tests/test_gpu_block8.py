@@ -120,7 +120,10 @@ def _padded(wc, gpu, extra=0):
 @pytest.mark.parametrize("n,ci,co,bits", [
     (1, 8, 1, 8), (1, 4096, 16, 8), (2, 72, 3, 8), (4, 1096, 33, 6), (5, 264, 17, 8), (16, 640, 100, 8), (17, 136, 31, 4),
     (32, 128, 16, 8), (33, 2056, 50, 8), (64, 384, 130, 8), (65, 256, 20, 8), (129, 72, 129, 8), (300, 1096, 263, 6),
-    (1, 13824, 24, 8), (3, 11008, 70, 2), (257, 512, 257, 8)])
+    (1, 13824, 24, 8), (3, 11008, 70, 2), (257, 512, 257, 8),
+    # tokens shared through LDS: parts of the row of codes and one part, odd numbers of 128 codes, ragged outputs and tokens
+    (16, 8200, 9001, 8), (17, 4104, 9001, 8), (40, 2568, 13000, 6), (64, 1096, 20001, 8), (65, 2048, 130, 8), (130, 4104, 1003, 8),
+    (256, 2056, 129, 4), (33, 136, 70001, 8)])
 def test_linear_i8(gpu, dt, out, n, ci, co, bits):
     import torch
     g = np.random.default_rng([23, n, ci, co])
