@@ -554,7 +554,7 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
 
 // The splits of a row: sums joined with the largest of their references.  A block has one row; DH / 4 lanes read the sums of a
 // split, 1024 / DH splits side by side.
-constexpr int kMaxSplits = 1024;
+[[maybe_unused]] constexpr int kMaxSplits = 1024;
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnDev a, uint32_t tile_rows) {
 #if defined(__HIP_DEVICE_COMPILE__)

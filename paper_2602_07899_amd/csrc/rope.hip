@@ -13,8 +13,8 @@ typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
 // uses them for all heads it takes.  Angles are reduced to a fraction of a turn in double: at position 2^31 a float
 // product would be off by whole turns.
 // Bound by the bytes of Q and K, read and written once.
-template <typename T, int DH, bool PAIRS, bool NORM>
-__global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkRopeArgs a, int wpt) {
+template <typename T, int DH, bool PAIRS, bool NORM, bool NT>
+__global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkRopeArgs a, int wpt, bool nts) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int LPH = DH / 8, HPW = 64 / LPH;
   __shared__ __attribute__((aligned(16))) float cs[4][2][DH / 2];
@@ -60,14 +60,17 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkRopeArgs a, int wpt
     wq[j] = NORM && a.wq ? a.wq[d0 + j] : 1.0f;
     wk[j] = NORM && a.wk ? a.wk[d0 + j] : 1.0f;
   }
+  // two groups of heads in flight
   const int heads = a.n_heads + a.n_kv_heads;
   const int step = (int)gridDim.y * wpt * HPW;
-  for (int h0 = ((int)blockIdx.y * wpt + wave % wpt) * HPW; h0 < heads; h0 += step) {
-    const int h = h0 + lane / LPH;
-    const bool live = h < heads, key = h >= a.n_heads;
-    const int hc = live ? (key ? h - a.n_heads : h) : 0;
-    const uint16_t* in = live && key ? (const uint16_t*)a.K + t * a.ldk : (const uint16_t*)a.Q + t * a.ldq;
-    u16x8 v = *reinterpret_cast<const u16x8*>(in + (int64_t)hc * DH + d0);
+  auto in_of = [&](int h) {
+    const bool key = h >= a.n_heads;
+    const int hc = h < heads ? (key ? h - a.n_heads : h) : 0;      // (past the last head: the first query's, never stored)
+    return (key && h < heads ? (const uint16_t*)a.K + t * a.ldk : (const uint16_t*)a.Q + t * a.ldq) + (int64_t)hc * DH + d0;
+  };
+  auto one = [&](int h, uint4 raw) {
+    const bool key = h >= a.n_heads;
+    u16x8 v = __builtin_bit_cast(u16x8, raw);
     float u[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) u[j] = T::to_float(v[j]);
@@ -90,17 +93,21 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkRopeArgs a, int wpt
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float w = __shfl(u[j], other & 63, 64);
-        o[j] = turned ? u[j] * c[j] - w * s[j] : u[j];
-      }
+      for (int j = 0; j < 8; ++j) o[j] = u[j] * c[j] - __shfl(u[j], other & 63, 64) * s[j];
     }
-    if (!live) continue;
+    if (h >= heads) return;
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = T::from_float(turned ? o[j] : u[j]);
-    uint16_t* out = key ? (uint16_t*)a.Ko + t * a.ldko : (uint16_t*)a.Qo + t * a.ldqo;
-    *reinterpret_cast<u16x8*>(out + (int64_t)hc * DH + d0) = v;
+    uint16_t* out = key ? (uint16_t*)a.Ko + t * a.ldko + (int64_t)(h - a.n_heads) * DH : (uint16_t*)a.Qo + t * a.ldqo + (int64_t)h * DH;
+    store16(out + d0, __builtin_bit_cast(uint4, v), nts);
+  };
+  int h0 = ((int)blockIdx.y * wpt + wave % wpt) * HPW + lane / LPH;
+  for (; h0 - lane / LPH + step < heads; h0 += 2 * step) {
+    const uint4 x = load16<NT>(in_of(h0)), y = load16<NT>(in_of(h0 + step));
+    one(h0, x);
+    one(h0 + step, y);
   }
+  if (h0 - lane / LPH < heads) one(h0, load16<NT>(in_of(h0)));
 #endif
 }
 
@@ -116,12 +123,19 @@ hipError_t launch_qk_norm_rope(const QkRopeArgs& a, hipStream_t stream) {
     gy = (unsigned)(want < most ? want : most);
   }
   const dim3 grid((unsigned)ceil_div(a.n_tok, 4 / wpt), gy);
-  auto go = [&](auto kern) { kern<<<grid, 256, 0, stream>>>(a, wpt); };
+  const double bytes = 2.0 * (double)a.n_tok * heads * a.head_dim;
+  const bool nt = streams_past(2.0 * bytes), nts = nt && outgrows_cache(bytes);
+  auto go = [&](auto kern) { kern<<<grid, 256, 0, stream>>>(a, wpt, nts); };
   auto form = [&](auto t, auto dh) {
     using T = decltype(t);
     constexpr int DH = decltype(dh)::value;
-    if (a.interleaved) a.norm ? go(qk_norm_rope_kernel<T, DH, true, true>) : go(qk_norm_rope_kernel<T, DH, true, false>);
-    else a.norm ? go(qk_norm_rope_kernel<T, DH, false, true>) : go(qk_norm_rope_kernel<T, DH, false, false>);
+    auto norm = [&](auto past) {
+      constexpr bool NT = decltype(past)::value;
+      if (a.interleaved) a.norm ? go(qk_norm_rope_kernel<T, DH, true, true, NT>) : go(qk_norm_rope_kernel<T, DH, true, false, NT>);
+      else a.norm ? go(qk_norm_rope_kernel<T, DH, false, true, NT>) : go(qk_norm_rope_kernel<T, DH, false, false, NT>);
+    };
+    if (nt) norm(std::true_type{});
+    else norm(std::false_type{});
   };
   auto width = [&](auto t) {
     if (a.head_dim == 64) form(t, std::integral_constant<int, 64>{});
