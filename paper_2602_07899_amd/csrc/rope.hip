@@ -7,16 +7,58 @@ namespace tlq {
 
 typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
 
+#if defined(__HIP_DEVICE_COMPILE__)
+template <int CTRL, int BANKS = 0xf>
+__device__ __forceinline__ float dpp(float old, float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, old), __builtin_bit_cast(int, v), CTRL, 0xf, BANKS, true));
+}
+// v and lane ^ 16's, as {of the even row of 16, of the odd one} (in assembly because the builtin's two results come out as one;
+// the wait states are what the swap needs behind the write of its operands)
+__device__ __forceinline__ void both_rows(float v, float& even, float& odd) {
+  even = odd = v;
+  asm("s_nop 1\n\tv_permlane16_swap_b32 %0, %1" : "+v"(even), "+v"(odd));
+}
+// sum over the N lanes of a head, in all of them
+template <int N>
+__device__ __forceinline__ float head_sum(float v) {
+  v += dpp<0xB1>(0.0f, v);          // lane ^ 1
+  v += dpp<0x4E>(0.0f, v);          // lane ^ 2
+  v += dpp<0x141>(0.0f, v);         // the other four of eight
+  if constexpr (N >= 16) v += dpp<0x140>(0.0f, v);      // the other eight of sixteen
+  if constexpr (N >= 32) {
+    float a, b;
+    both_rows(v, a, b);
+    v = a + b;
+  }
+  return v;
+}
+// the value of the lane half a head (N / 2 lanes) away
+template <int N>
+__device__ __forceinline__ float half_head(float v, bool upper) {
+  if constexpr (N == 8) return dpp<0x114, 0xa>(dpp<0x104, 0x5>(0.0f, v), v);      // four up for the lower, four down for the upper
+  else if constexpr (N == 16) return dpp<0x128>(0.0f, v);
+  else {
+    float a, b;
+    both_rows(v, a, b);
+    return upper ? a : b;
+  }
+}
+#endif
+
 // u = x / sqrt(mean x^2 + eps) * w over the head_dim channels of a head, then the pair (u_a, u_b) turned by
-// pos * inv_freq[i].  DH / 8 lanes hold a head, eight channels each, so a wave has 512 / DH heads of one token at a time.
-// The angles belong to the token: a wave computes each cosine and sine once (a lane one or two of them, through LDS) and
-// uses them for all heads it takes.  Angles are reduced to a fraction of a turn in double: at position 2^31 a float
-// product would be off by whole turns.
-// Bound by the bytes of Q and K, read and written once.
-template <typename T, int DH, bool PAIRS, bool NORM, bool NT>
+// pos * inv_freq[i].  DH / 8 lanes hold a head, eight channels each, so a wave has 512 / DH heads of one token at a time, two
+// groups of them in flight.  The angles belong to the token: a wave computes each cosine and sine once (a lane one or two
+// of them, through LDS) and uses them for all heads it takes.  Angles are reduced to a fraction of a turn in double: at
+// position 2^31 a float product would be off by whole turns.
+// FORM: pairs half a head apart (their lanes trade by lane permutations), half of fewer rotated channels (by LDS), neighbours.
+// Bound by the bytes of Q and K, read and written once: 40,800 tokens x 80 heads of 128 4.7 TB/s where a copy of as many
+// bytes reaches 3.9 - 5.1, of which the angles are a tenth.
+enum { kHalfHead, kHalfRot, kNeighbours };
+template <typename T, int DH, int FORM>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkRopeArgs a, int wpt, bool nts) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int LPH = DH / 8, HPW = 64 / LPH;
+  constexpr bool PAIRS = FORM == kNeighbours;
   __shared__ __attribute__((aligned(16))) float cs[4][2][DH / 2];
   const int lane = threadIdx.x & 63, sub = lane & (LPH - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -40,7 +82,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkRopeArgs a, int wpt
   // this lane's channels: pairs of neighbours, or the lower or upper half of pairs rot / 2 apart
   const int d0 = sub * 8, hs = half >> 3;         // (rot is a multiple of 16)
   const bool turned = d0 < a.rot, upper = !PAIRS && sub >= hs;
-  const int other = lane + (upper ? -hs : hs);    // lane that holds the other member of the pairs
+  const int other = (lane + (upper ? -hs : hs)) & 63;      // lane that holds the other member of the pairs
   float c[8], s[8];
   if (turned) {
     const int i0 = PAIRS ? d0 >> 1 : (upper ? d0 - half : d0);
@@ -57,16 +99,16 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkRopeArgs a, int wpt
   float wq[8], wk[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    wq[j] = NORM && a.wq ? a.wq[d0 + j] : 1.0f;
-    wk[j] = NORM && a.wk ? a.wk[d0 + j] : 1.0f;
+    wq[j] = a.wq ? a.wq[d0 + j] : 1.0f;
+    wk[j] = a.wk ? a.wk[d0 + j] : 1.0f;
   }
-  // two groups of heads in flight
   const int heads = a.n_heads + a.n_kv_heads;
   const int step = (int)gridDim.y * wpt * HPW;
-  auto in_of = [&](int h) {
+  auto fetch = [&](int h) {
     const bool key = h >= a.n_heads;
     const int hc = h < heads ? (key ? h - a.n_heads : h) : 0;      // (past the last head: the first query's, never stored)
-    return (key && h < heads ? (const uint16_t*)a.K + t * a.ldk : (const uint16_t*)a.Q + t * a.ldq) + (int64_t)hc * DH + d0;
+    const uint16_t* p = (key && h < heads ? (const uint16_t*)a.K + t * a.ldk : (const uint16_t*)a.Q + t * a.ldq) + (int64_t)hc * DH + d0;
+    return *reinterpret_cast<const uint4*>(p);
   };
   auto one = [&](int h, uint4 raw) {
     const bool key = h >= a.n_heads;
@@ -74,13 +116,13 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkRopeArgs a, int wpt
     float u[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) u[j] = T::to_float(v[j]);
-    if constexpr (NORM) {
+    if (a.norm) {
       float ss = 0.0f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) ss = __builtin_fmaf(u[j], u[j], ss);
-#pragma unroll
-      for (int off = LPH / 2; off >= 1; off >>= 1) ss += __shfl_xor(ss, off, 64);
-      const float inv = 1.0f / sqrtf(ss * (1.0f / DH) + a.eps);
+      const float mean = head_sum<LPH>(ss) * (1.0f / DH) + a.eps;
+      float inv = __builtin_amdgcn_rsqf(mean);
+      if (mean < 1e-30f) inv = 1.0f / sqrtf(mean);
 #pragma unroll
       for (int j = 0; j < 8; ++j) u[j] = u[j] * inv * (key ? wk[j] : wq[j]);
     }
@@ -93,21 +135,24 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkRopeArgs a, int wpt
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) o[j] = u[j] * c[j] - __shfl(u[j], other & 63, 64) * s[j];
+      for (int j = 0; j < 8; ++j) {
+        const float w = FORM == kHalfHead ? half_head<LPH>(u[j], upper) : __shfl(u[j], other, 64);
+        o[j] = u[j] * c[j] - w * s[j];
+      }
     }
     if (h >= heads) return;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = T::from_float(turned ? o[j] : u[j]);
+    for (int j = 0; j < 8; ++j) v[j] = T::from_float(FORM == kHalfHead || turned ? o[j] : u[j]);
     uint16_t* out = key ? (uint16_t*)a.Ko + t * a.ldko + (int64_t)(h - a.n_heads) * DH : (uint16_t*)a.Qo + t * a.ldqo + (int64_t)h * DH;
     store16(out + d0, __builtin_bit_cast(uint4, v), nts);
   };
   int h0 = ((int)blockIdx.y * wpt + wave % wpt) * HPW + lane / LPH;
   for (; h0 - lane / LPH + step < heads; h0 += 2 * step) {
-    const uint4 x = load16<NT>(in_of(h0)), y = load16<NT>(in_of(h0 + step));
+    const uint4 x = fetch(h0), y = fetch(h0 + step);
     one(h0, x);
     one(h0 + step, y);
   }
-  if (h0 - lane / LPH < heads) one(h0, load16<NT>(in_of(h0)));
+  if (h0 - lane / LPH < heads) one(h0, fetch(h0));
 #endif
 }
 
@@ -115,8 +160,9 @@ hipError_t launch_qk_norm_rope(const QkRopeArgs& a, hipStream_t stream) {
   const int heads = a.n_heads + a.n_kv_heads;
   ProfScope ps("qk_norm_rope", stream, 4.0 * (double)a.n_tok * heads * a.head_dim);
   const int groups = (int)ceil_div((int64_t)heads * a.head_dim, 512);
-  // a wave takes all heads of a token where the tokens alone fill the chip, otherwise a share of them
-  const int wpt = a.n_tok >= 8192 ? 1 : 4;
+  // a wave takes all heads of a token where the tokens alone fill the chip, otherwise a share of them (80 heads of 128, us a
+  // wave and four a token: 40,800 tokens 355 454, 10,000 91 110)
+  const int wpt = a.n_tok >= 4096 ? 1 : 4;
   unsigned gy = 1;
   if (wpt == 4) {
     const int64_t most = ceil_div(groups, 4), want = ceil_div(2048, a.n_tok);
@@ -124,18 +170,14 @@ hipError_t launch_qk_norm_rope(const QkRopeArgs& a, hipStream_t stream) {
   }
   const dim3 grid((unsigned)ceil_div(a.n_tok, 4 / wpt), gy);
   const double bytes = 2.0 * (double)a.n_tok * heads * a.head_dim;
-  const bool nt = streams_past(2.0 * bytes), nts = nt && outgrows_cache(bytes);
+  const bool nts = streams_past(2.0 * bytes) && outgrows_cache(bytes);      // (loads past the caches: the same time)
   auto go = [&](auto kern) { kern<<<grid, 256, 0, stream>>>(a, wpt, nts); };
   auto form = [&](auto t, auto dh) {
     using T = decltype(t);
     constexpr int DH = decltype(dh)::value;
-    auto norm = [&](auto past) {
-      constexpr bool NT = decltype(past)::value;
-      if (a.interleaved) a.norm ? go(qk_norm_rope_kernel<T, DH, true, true, NT>) : go(qk_norm_rope_kernel<T, DH, true, false, NT>);
-      else a.norm ? go(qk_norm_rope_kernel<T, DH, false, true, NT>) : go(qk_norm_rope_kernel<T, DH, false, false, NT>);
-    };
-    if (nt) norm(std::true_type{});
-    else norm(std::false_type{});
+    if (a.interleaved) go(qk_norm_rope_kernel<T, DH, kNeighbours>);
+    else if (a.rot == DH) go(qk_norm_rope_kernel<T, DH, kHalfHead>);
+    else go(qk_norm_rope_kernel<T, DH, kHalfRot>);
   };
   auto width = [&](auto t) {
     if (a.head_dim == 64) form(t, std::integral_constant<int, 64>{});

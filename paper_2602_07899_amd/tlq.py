@@ -392,38 +392,66 @@ def residual_add(H, Z, p, Out):
 
 
 # ------------------------------------------------------------------ a decoder block in 8 bits
-def _expect(ok, what):
+# (Single tokens are bound by the issue of their calls: the checks are written out, one torch call for each thing that they
+# look at.)
+_t = None      # torch and its types, on first use
+_KV_CACHE_BYTES, _KV_BATCH_BYTES = C.sizeof(KvCache), C.sizeof(KvBatch)
+
+
+class _Torch:
+    def __init__(self):
+        import torch
+        self.torch, self.i8, self.i32, self.f32, self.f64 = torch, torch.int8, torch.int32, torch.float32, torch.float64
+        self.of = (torch.float16, torch.bfloat16, torch.float32)
+        self.device = torch._C._cuda_getDevice
+
+
+def _types():
+    global _t
+    if _t is None:
+        _t = _Torch()
+    return _t
+
+
+def _wrong(t, want, name, here):
+    if t.dtype is not want:
+        raise ValueError(f"{name}: a tensor of {t.dtype} where {want} is read")
+    raise ValueError(f"{name}: not on the current device (device {here}, tensor on {t.device})")
+
+
+def _current(t):
+    """The current device, asked for a tensor that has to be on it."""
+    if not t.is_cuda:
+        raise ValueError("tensors have to be on the current device, a GPU")
+    return _types().device()
+
+
+def _shape(ok, what):
     if not ok:
         raise ValueError(what)
 
 
-def _here(p, types, *tensors):
-    """The tensors are of the types that the call reads them as, and on the device whose stream it takes."""
-    import torch
-    here = None
-    for t, dt in zip(tensors, types):
-        if t is None:
-            continue
-        want = dt if not isinstance(dt, str) else (torch.float16, torch.bfloat16, torch.float32)[p.x_dtype if dt == "x" else p.yref_dtype]
-        if t.dtype != want:
-            raise ValueError(f"a tensor of {t.dtype} where {want} is read")
-        if here is None and t.is_cuda:
-            here = torch._C._cuda_getDevice()
-        if not t.is_cuda or t.get_device() != here:
-            raise ValueError("tensors have to be on the current device")
+def _rows(t, name):
+    """Row stride of a matrix with neighbouring columns."""
+    ld, one = t.stride() if t.dim() == 2 else (0, 0)
+    if one != 1 and t.size(-1) != 1:
+        raise ValueError(f"{name}: a row-major matrix with unit column stride")
+    return ld
 
 
 def row_codes(X, bits, p, codes, steps, factor=None):
     """Rows of X * factor as signed codes of `bits` bits (int8 [n, >= c rounded up to 128]) and steps (float [n])."""
-    import torch
-    n, c = X.shape
-    f32 = torch.float32
-    _here(p, ("x", torch.int8, f32, f32), X, codes, steps, factor)
-    _expect(codes.shape[0] == n and _ld(codes) >= codes.shape[1] >= -(-c // 128) * 128, "codes: n rows, zeros behind c up to a multiple of 128")
-    _expect(steps.numel() == n and steps.is_contiguous(), "one step a row")
-    _expect(factor is None or factor.numel() == c and factor.is_contiguous(), "one factor a channel")
-    _check(lib().tlq_row_codes(_ptr(X), n, c, _ld(X), _ptr(factor), bits, C.byref(p), _ptr(codes), _ld(codes), _ptr(steps),
-                               _stream()), "tlq_row_codes")
+    ty, here = _types(), _current(X)
+    for t, want, name in ((X, ty.of[p.x_dtype], "X"), (codes, ty.i8, "codes"), (steps, ty.f32, "steps"), (factor, ty.f32, "factor")):
+        if t is not None and (t.dtype is not want or t.get_device() != here):
+            _wrong(t, want, name, here)
+    n, c = X.size(0), X.size(1)
+    ldc = _rows(codes, "codes")
+    _shape(codes.size(0) == n and ldc >= codes.size(1) >= -(-c // 128) * 128, "codes: n rows, zeros behind c up to a multiple of 128")
+    _shape(steps.numel() == n and steps.is_contiguous(), "steps: one a row")
+    _shape(factor is None or factor.numel() == c and factor.is_contiguous(), "factor: one a channel")
+    _check(lib().tlq_row_codes(X.data_ptr(), n, c, _rows(X, "X"), None if factor is None else factor.data_ptr(), bits, C.byref(p),
+                               codes.data_ptr(), ldc, steps.data_ptr(), _stream()), "tlq_row_codes")
 
 
 def linear_i8_workspace_bytes(n_tok, c_in):
@@ -432,48 +460,53 @@ def linear_i8_workspace_bytes(n_tok, c_in):
 
 def linear_i8(X, w_codes, w_steps, p, Y, factor=None, workspace=None):
     """Y = step_t * step_o * codes(X * factor) . w_codes^T; the tokens' codes have p.act_bits bits."""
-    import torch
-    n, ci = X.shape
-    co = w_codes.shape[0]
-    f32 = torch.float32
-    _here(p, ("x", torch.int8, f32, "y", f32), X, w_codes, w_steps, Y, factor)
-    _expect(w_codes.shape[1] >= -(-ci // 128) * 128, "w_codes: rows with zeros behind c_in up to a multiple of 128")
-    _expect(w_steps.numel() == co and w_steps.is_contiguous(), "one step an output")
-    _expect(Y.shape == (n, co), "Y: [n_tok, c_out]")
-    _expect(factor is None or factor.numel() == ci and factor.is_contiguous(), "one factor a channel")
+    ty, here = _types(), _current(X)
+    for t, want, name in ((X, ty.of[p.x_dtype], "X"), (w_codes, ty.i8, "w_codes"), (w_steps, ty.f32, "w_steps"),
+                          (Y, ty.of[p.yref_dtype], "Y"), (factor, ty.f32, "factor")):
+        if t is not None and (t.dtype is not want or t.get_device() != here):
+            _wrong(t, want, name, here)
+    n, ci, co = X.size(0), X.size(1), w_codes.size(0)
+    _shape(w_codes.size(1) >= -(-ci // 128) * 128, "w_codes: rows with zeros behind c_in up to a multiple of 128")
+    _shape(w_steps.numel() == co and w_steps.is_contiguous(), "w_steps: one an output")
+    _shape(Y.size(0) == n and Y.size(1) == co, "Y: [n_tok, c_out]")
+    _shape(factor is None or factor.numel() == ci and factor.is_contiguous(), "factor: one a channel")
     ws = workspace if workspace is not None else _ws(linear_i8_workspace_bytes(n, ci), X)
-    _check(lib().tlq_linear_i8(_ptr(X), n, ci, _ld(X), _ptr(factor), _ptr(w_codes), co, _ld(w_codes), _ptr(w_steps), C.byref(p),
-                               _ptr(Y), _ld(Y), _ptr(ws), ws.numel(), _stream()), "tlq_linear_i8")
+    _check(lib().tlq_linear_i8(X.data_ptr(), n, ci, _rows(X, "X"), None if factor is None else factor.data_ptr(), w_codes.data_ptr(), co,
+                               _rows(w_codes, "w_codes"), w_steps.data_ptr(), C.byref(p), Y.data_ptr(), _rows(Y, "Y"), ws.data_ptr(),
+                               ws.numel(), _stream()), "tlq_linear_i8")
     return Y
 
 
 def qk_norm_rope(Q, K, head_dim, pos, inv_freq, p, Q_out, K_out, wq=None, wk=None, eps=1e-6, norm=True, interleaved=False):
     """Heads of Q [n, heads * head_dim] and K normalised (unless norm is False) and the first 2 * len(inv_freq) channels of
     each turned by pos * inv_freq."""
-    import torch
-    n = Q.shape[0]
-    f32 = torch.float32
-    _here(p, ("x", "x", "x", "x", torch.int32, torch.float64, f32, f32), Q, K, Q_out, K_out, pos, inv_freq, wq, wk)
-    _expect(K.shape[0] == n and Q_out.shape == Q.shape and K_out.shape == K.shape, "outputs of the inputs' shapes")
-    _expect(Q.shape[1] % head_dim == 0 and K.shape[1] % head_dim == 0, "whole heads")
-    _expect(pos.numel() == n and pos.is_contiguous() and (inv_freq is None or inv_freq.is_contiguous()), "one position a row")
-    _expect(all(w is None or (w.numel() == head_dim and w.is_contiguous()) for w in (wq, wk)), "one weight a channel of a head")
-    rot = 0 if inv_freq is None else 2 * inv_freq.numel()
-    _check(lib().tlq_qk_norm_rope(_ptr(Q), _ld(Q), Q.shape[1] // head_dim, _ptr(K), _ld(K), K.shape[1] // head_dim, n, head_dim,
-                                  rot, 1 if interleaved else 0, 1 if norm else 0, eps, _ptr(wq), _ptr(wk), _ptr(pos),
-                                  _ptr(inv_freq), C.byref(p), _ptr(Q_out), _ld(Q_out), _ptr(K_out), _ld(K_out), _stream()),
-           "tlq_qk_norm_rope")
+    ty, here = _types(), _current(Q)
+    x, f32 = ty.of[p.x_dtype], ty.f32
+    for t, want, name in ((Q, x, "Q"), (K, x, "K"), (Q_out, x, "Q_out"), (K_out, x, "K_out"), (pos, ty.i32, "pos"),
+                          (inv_freq, ty.f64, "inv_freq"), (wq, f32, "wq"), (wk, f32, "wk")):
+        if t is not None and (t.dtype is not want or t.get_device() != here):
+            _wrong(t, want, name, here)
+    n, nq, nk = Q.size(0), Q.size(1), K.size(1)
+    _shape(K.size(0) == n == Q_out.size(0) == K_out.size(0) and Q_out.size(1) == nq and K_out.size(1) == nk, "outputs of the inputs' shapes")
+    _shape(head_dim > 0 and nq % head_dim == 0 and nk % head_dim == 0, "whole heads")
+    _shape(pos.numel() == n and pos.is_contiguous() and (inv_freq is None or inv_freq.is_contiguous()), "pos: one a row")
+    for w in (wq, wk):
+        _shape(w is None or w.numel() == head_dim and w.is_contiguous(), "one weight a channel of a head")
+    _check(lib().tlq_qk_norm_rope(Q.data_ptr(), _rows(Q, "Q"), nq // head_dim, K.data_ptr(), _rows(K, "K"), nk // head_dim, n, head_dim,
+                                  0 if inv_freq is None else 2 * inv_freq.numel(), 1 if interleaved else 0, 1 if norm else 0, eps,
+                                  None if wq is None else wq.data_ptr(), None if wk is None else wk.data_ptr(), pos.data_ptr(),
+                                  None if inv_freq is None else inv_freq.data_ptr(), C.byref(p), Q_out.data_ptr(),
+                                  _rows(Q_out, "Q_out"), K_out.data_ptr(), _rows(K_out, "K_out"), _stream()), "tlq_qk_norm_rope")
     return Q_out, K_out
 
 
 def kv_cache(k, k_step, v, v_step):
     """The cache made of k int8 [n_pages, n_kv_heads, page, head_dim], v int8 [n_pages, n_kv_heads, head_dim, page] and
     their steps float [n_pages, n_kv_heads]."""
-    import torch
     n, h, page, dh = k.shape
-    _expect(tuple(v.shape) == (n, h, dh, page) and tuple(k_step.shape) == (n, h) == tuple(v_step.shape), "the shapes of a cache's parts differ")
-    _expect(all(t.is_contiguous() for t in (k, k_step, v, v_step)), "a cache's parts are dense")
-    c = KvCache(C.sizeof(KvCache), h, dh, page, n, _ptr(k), _ptr(k_step), _ptr(v), _ptr(v_step))
+    _shape(tuple(v.shape) == (n, h, dh, page) and tuple(k_step.shape) == (n, h) == tuple(v_step.shape), "the shapes of a cache's parts differ")
+    _shape(k.is_contiguous() and v.is_contiguous() and k_step.is_contiguous() and v_step.is_contiguous(), "a cache's parts are dense")
+    c = KvCache(_KV_CACHE_BYTES, h, dh, page, n, k.data_ptr(), k_step.data_ptr(), v.data_ptr(), v_step.data_ptr())
     c.parts = (k, v, k_step, v_step)       # (they live as long as the structure that points to them)
     return c
 
@@ -482,26 +515,29 @@ def kv_batch(cu_new, lens, table, max_new, max_len):
     """Sequences of a call: their rows (int32 [n + 1]), lengths with the new tokens (int32 [n]), pages (int32 [n, max_pages])
     and the host's bounds of new tokens and of lengths."""
     n = lens.numel()
-    _expect(cu_new.numel() == n + 1 and table.dim() == 2 and table.shape[0] == n and (table.stride(1) == 1 or table.shape[1] == 1),
-            "cu_new [n + 1], lens [n], table [n, pages]")
-    _expect(cu_new.is_contiguous() and lens.is_contiguous(), "cu_new and lens are dense")
-    ld = max(table.stride(0), table.shape[1])
-    b = KvBatch(C.sizeof(KvBatch), n, _ptr(cu_new), _ptr(lens), _ptr(table), ld, table.shape[1], max_new, max_len, 0)
+    _shape(table.dim() == 2 and table.size(0) == n and cu_new.numel() == n + 1, "cu_new [n + 1], lens [n], table [n, pages]")
+    _shape(cu_new.is_contiguous() and lens.is_contiguous(), "cu_new and lens are dense")
+    pages = table.size(1)
+    b = KvBatch(_KV_BATCH_BYTES, n, cu_new.data_ptr(), lens.data_ptr(), table.data_ptr(), max(_rows(table, "table"), pages), pages, max_new, max_len, 0)
     b.parts = (cu_new, lens, table)
     return b
 
 
-def _kv_here(p, b, c, *xs):
-    import torch
-    i8, f32, i32 = torch.int8, torch.float32, torch.int32
-    _here(p, ("x",) * len(xs) + (i32,) * 3 + (i8, i8, f32, f32), *xs, *b.parts, *c.parts)
+def _kv_tensors(p, batch, cache, x, y, names):
+    ty, here = _types(), _current(x)
+    i8, i32, f32, want_x = ty.i8, ty.i32, ty.f32, ty.of[p.x_dtype]
+    for t, want, name in ((x, want_x, names[0]), (y, want_x, names[1]), *zip(batch.parts, (i32, i32, i32), ("cu_new", "lens", "table")),
+                          *zip(cache.parts, (i8, i8, f32, f32), ("k", "v", "k_step", "v_step"))):
+        if t.dtype is not want or t.get_device() != here:
+            _wrong(t, want, name, here)
 
 
 def kv_append(K, V, batch, cache, p):
     """New rows of keys and values [n_tok, n_kv_heads * head_dim] into the cache's pages."""
-    _kv_here(p, batch, cache, K, V)
-    _expect(K.shape == V.shape and K.shape[1] == cache.n_kv_heads * cache.head_dim, "K, V: [n_tok, n_kv_heads * head_dim]")
-    _check(lib().tlq_kv_append(_ptr(K), _ld(K), _ptr(V), _ld(V), K.shape[0], C.byref(batch), C.byref(cache), C.byref(p),
+    _kv_tensors(p, batch, cache, K, V, "KV")
+    n, width = K.size(0), K.size(1)
+    _shape(V.size(0) == n and V.size(1) == width == cache.n_kv_heads * cache.head_dim, "K, V: [n_tok, n_kv_heads * head_dim]")
+    _check(lib().tlq_kv_append(K.data_ptr(), _rows(K, "K"), V.data_ptr(), _rows(V, "V"), n, C.byref(batch), C.byref(cache), C.byref(p),
                                _stream()), "tlq_kv_append")
 
 
@@ -511,11 +547,12 @@ def kv_attention_workspace_bytes(n_tok, n_heads, batch, cache):
 
 def kv_attention(Q, n_heads, batch, cache, p, Out, scale=0.0, workspace=None):
     """Causal attention of the new rows Q [n_tok, n_heads * head_dim] over the cache, their own tokens among it."""
-    _kv_here(p, batch, cache, Q, Out)
-    _expect(Q.shape == Out.shape and Q.shape[1] == n_heads * cache.head_dim, "Q, Out: [n_tok, n_heads * head_dim]")
-    ws = workspace if workspace is not None else _ws(kv_attention_workspace_bytes(Q.shape[0], n_heads, batch, cache), Q)
-    _check(lib().tlq_kv_attention(_ptr(Q), _ld(Q), Q.shape[0], n_heads, scale, C.byref(batch), C.byref(cache), C.byref(p),
-                                  _ptr(Out), _ld(Out), _ptr(ws), ws.numel(), _stream()), "tlq_kv_attention")
+    _kv_tensors(p, batch, cache, Q, Out, ("Q", "Out"))
+    n, width = Q.size(0), Q.size(1)
+    _shape(Out.size(0) == n and Out.size(1) == width == n_heads * cache.head_dim, "Q, Out: [n_tok, n_heads * head_dim]")
+    ws = workspace if workspace is not None else _ws(kv_attention_workspace_bytes(n, n_heads, batch, cache), Q)
+    _check(lib().tlq_kv_attention(Q.data_ptr(), _rows(Q, "Q"), n, n_heads, scale, C.byref(batch), C.byref(cache), C.byref(p),
+                                  Out.data_ptr(), _rows(Out, "Out"), ws.data_ptr(), ws.numel(), _stream()), "tlq_kv_attention")
     return Out
 
 
