@@ -552,8 +552,52 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
 #endif
 }
 
-// The splits of a row: sums joined with the largest of their references.  A block has one row; DH / 4 lanes read the sums of a
-// split, 1024 / DH splits side by side.
+// Number of splits that the tile of a row has written (see the kernels).
+__device__ __forceinline__ int written_splits(const KvAttnDev& a, const KvSeq& q, int qi, int head, uint32_t tile_rows) {
+  const uint32_t rows = (uint32_t)q.n_new * a.group;
+  uint32_t last_row = ((uint32_t)qi * a.group + (uint32_t)head % (uint32_t)a.group) / tile_rows * tile_rows + tile_rows - 1;
+  if (last_row > rows - 1) last_row = rows - 1;
+  const int last = q.first + (int)a.by_group.of(last_row);
+  const int end = last + 1 < q.len ? last + 1 : q.len;
+  return end <= 0 ? 0 : (end + a.chunk - 1) / a.chunk;
+}
+
+// The splits of a row, up to 64 of them: sums joined with the largest of their references, a wave a row.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void kv_join_few_kernel(KvAttnDev a, uint32_t tile_rows) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  typedef float vec __attribute__((ext_vector_type(DH / 64)));
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int s = blockIdx.z, head = blockIdx.y * 4 + wave, qi = blockIdx.x;
+  const KvSeq q = kv_sequence(a.b, a.c.page, a.n_tok, s);
+  if (qi >= q.n_new || head >= a.n_heads) return;
+  const int n = written_splits(a, q, qi, head, tile_rows);
+  const int64_t at = ((q.row0 + qi) * a.n_heads + head) * a.n_splits;
+  const float2 p = lane < n ? a.ml[at + lane] : make_float2(-INFINITY, 0.0f);
+  float m = p.x;
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+  const float f = p.x == -INFINITY ? 0.0f : exp2_fast(p.x - m);
+  float l = p.y * f;
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) l += __shfl_xor(l, off, 64);
+  vec o = {};
+  for (int i = 0; i < n; i += 8) {       // (lanes from n on have factors of zero)
+    vec v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = *reinterpret_cast<const vec*>(a.acc + (at + (i + k < n ? i + k : n - 1)) * DH + lane * (DH / 64));
+#pragma unroll
+    for (int k = 0; k < 8; ++k) o += v[k] * __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), i + k));
+  }
+  const float inv = m == -INFINITY ? 0.0f : 1.0f / l;
+  uint16_t* to = a.Out + (q.row0 + qi) * a.ldo + (int64_t)head * DH + lane * (DH / 64);
+  if constexpr (DH == 128)
+    *reinterpret_cast<uint32_t*>(to) = (uint32_t)T::from_float(o[0] * inv) | (uint32_t)T::from_float(o[1] * inv) << 16;
+  else *to = T::from_float(o[0] * inv);
+#endif
+}
+
+// More of them (few rows then).  A block has one row; DH / 4 lanes read the sums of a split, 1024 / DH splits side by side.
 [[maybe_unused]] constexpr int kMaxSplits = 1024;
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnDev a, uint32_t tile_rows) {
@@ -565,13 +609,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnDev a, uint32_t tile
   const int s = blockIdx.z, head = blockIdx.y, qi = blockIdx.x;
   const KvSeq q = kv_sequence(a.b, a.c.page, a.n_tok, s);
   if (qi >= q.n_new) return;
-  // the splits that its tile has written (see the kernels)
-  const uint32_t rows = (uint32_t)q.n_new * a.group;
-  uint32_t last_row = ((uint32_t)qi * a.group + (uint32_t)head % (uint32_t)a.group) / tile_rows * tile_rows + tile_rows - 1;
-  if (last_row > rows - 1) last_row = rows - 1;
-  const int last = q.first + (int)a.by_group.of(last_row);
-  const int end = last + 1 < q.len ? last + 1 : q.len;
-  const int n = end <= 0 ? 0 : (end + a.chunk - 1) / a.chunk;
+  const int n = written_splits(a, q, qi, head, tile_rows);
   const int64_t at = ((q.row0 + qi) * a.n_heads + head) * a.n_splits;
   float2 p[kMaxSplits / 256];
   float m = -INFINITY, l = 0.0f;
@@ -619,8 +657,9 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnDev a, uint32_t tile
 #endif
 }
 
-// Rows of a sequence and key head up to which they go in tiles of 16.
-constexpr int64_t kFewRows = 32;
+// Rows of a sequence and key head up to which they go in one tile of 16: beyond, the keys are read again for each 16 rows and
+// the tile of 128, though mostly empty, is as fast (2048 keys, us 16 and 128: 16 rows 57 70, 24 69 71, 32 71 71, 48 95 86, 64 128 86).
+constexpr int64_t kFewRows = 16;
 
 namespace {
 struct KvPlan { bool prompt; int rows, tiles, n_splits, chunk; size_t acc_at, bytes; };
@@ -633,9 +672,15 @@ KvPlan kv_plan(int64_t n_tok, int n_heads, const tlq_kv_batch& b, const tlq_kv_c
   p.tiles = (int)ceil_div(most * group, p.rows);
   const int64_t room = (int64_t)b.max_pages * c.page, keys = b.max_len < room ? b.max_len : room;
   const int64_t base = (int64_t)p.tiles * c.n_kv_heads * b.n_seq;
-  int64_t splits = ceil_div(p.prompt ? 512 : 1024, base);
-  const int64_t units = ceil_div(keys, 256);
-  if (splits > units) splits = units;
+  // Split until there are about two blocks a CU, a part of 256 keys or, where many rows have sums to be joined, of 512 at
+  // least (us unsplit, for 256, 512 and 1024 blocks: single tokens, 131,072 keys x 4 key heads - 35 32 35, 8 x 4096 x 32 44 44 45
+  // 47, 32 x 1024 x 8 18 18 20 22, 64 x 8192 x 8 160 160 159 171; 64 tokens behind 16,320 x 4 477 50 44 44, 4 x 100 behind
+  // 3900 x 8 122 79 61 75, 4096 x 8 122 121 104 107; 600 x 8 in parts of 300 24 35).  Beyond two blocks a CU a second round of
+  // them and the joining cost more than their evenness gives.
+  const int64_t units = ceil_div(keys, 256), most_splits = p.prompt ? keys / 512 : units;
+  int64_t splits = 511 / base;
+  if (splits > most_splits) splits = most_splits;
+  if (splits < 1) splits = 1;
   p.chunk = (int)(ceil_div(units, splits) * 256);
   p.n_splits = (int)ceil_div(keys, p.chunk);
   p.acc_at = align_up((size_t)n_tok * n_heads * p.n_splits * sizeof(float2), 256);
@@ -682,7 +727,9 @@ hipError_t launch_kv_attention(const void* Q, int64_t ldq, int64_t n_tok, int n_
     }
     if (hipError_t e = hipGetLastError(); e != hipSuccess || p.n_splits == 1) return e;
     ProfScope ps("kv_join", stream, 4.0 * (double)n_tok * n_heads * p.n_splits * c.head_dim);
-    kv_join_kernel<T, DH><<<dim3((unsigned)most, (unsigned)n_heads, (unsigned)b.n_seq), 256, 0, stream>>>(a, (uint32_t)p.rows);
+    if (p.n_splits <= 64)
+      kv_join_few_kernel<T, DH><<<dim3((unsigned)most, (unsigned)ceil_div(n_heads, 4), (unsigned)b.n_seq), 256, 0, stream>>>(a, (uint32_t)p.rows);
+    else kv_join_kernel<T, DH><<<dim3((unsigned)most, (unsigned)n_heads, (unsigned)b.n_seq), 256, 0, stream>>>(a, (uint32_t)p.rows);
     return hipGetLastError();
   };
   using W128 = std::integral_constant<int, 128>;
