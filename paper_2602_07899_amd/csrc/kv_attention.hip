@@ -355,23 +355,24 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
 #pragma unroll
     for (int g = 0; g < 4; ++g) ids[g] = (uint32_t)row_table[(unit + g * 16 < k1 ? unit + g * 16 : k1 - 1) >> a.page_bits];
   };
-  auto load = [&](int unit) {
+  auto load = [&](int unit) {          // (the steps in front: who waits for them waits for what was issued before)
     const uint32_t at = (uint32_t)unit & in_page;
-#pragma unroll
-    for (int i = 0; i < LR; ++i) {     // (DH = 128: a wave's rows lie in one group of 16 keys; 64: wave w has group w)
-      const int g = DH == 128 ? (wave >> 1) + 2 * i : wave;
-      const uint32_t id = g == 0 ? ids[0] : g == 1 ? ids[1] : g == 2 ? ids[2] : ids[3];
-      kr[i] = *reinterpret_cast<const uint4*>(kp + ((uint64_t)(id < n_pages ? id : 0) * page_stride + at * DH) + koff[i]);
-    }
     const uint32_t mine = fq < 2 ? (fq == 0 ? ids[0] : ids[1]) : (fq == 2 ? ids[2] : ids[3]);
     seen_next = mine < n_pages;
     const uint32_t id = seen_next ? mine : 0;
-    const int8_t* p = vp + at + (uint64_t)id * page_stride;
-#pragma unroll
-    for (int i = 0; i < LR; ++i) vr[i] = *reinterpret_cast<const uint4*>(p + voff[i]);
     const uint64_t slot = (uint64_t)id * (uint32_t)a.c.n_kv_heads + (uint32_t)hk;
     ks_next = a.c.k_step[slot];
     vs_next = a.c.v_step[slot];
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < LR; ++i) {     // (DH = 128: a wave's rows lie in one group of 16 keys; 64: wave w has group w)
+      const int g = DH == 128 ? (wave >> 1) + 2 * i : wave;
+      const uint32_t k = g == 0 ? ids[0] : g == 1 ? ids[1] : g == 2 ? ids[2] : ids[3];
+      kr[i] = *reinterpret_cast<const uint4*>(kp + ((uint64_t)(k < n_pages ? k : 0) * page_stride + at * DH) + koff[i]);
+    }
+    const int8_t* p = vp + at + (uint64_t)id * page_stride;
+#pragma unroll
+    for (int i = 0; i < LR; ++i) vr[i] = *reinterpret_cast<const uint4*>(p + voff[i]);
     entries(unit + 64);
   };
   // Chunk c of a row lies at place(c) ^ key(row), such that neither the eight lanes of a write that are served together (128
@@ -422,7 +423,7 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
   if (k0 < k1) {
     stage_all(lds);
     take_steps();
-    if (k0 + 64 < k1) load(k0 + 64);
+    load(k0 + 64);
   }
   int cur = 0;
   for (int unit = k0; unit < k1; unit += 64, cur ^= 1) {
@@ -441,6 +442,7 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
         for (int j = 0; j < 4; ++j)
           kf[i & 1][j] = *reinterpret_cast<const f16x8*>(kv + kbase + j * 4 * KB + ((kplace(i * 4 + fq) ^ kx) << 4));
       };
+      __builtin_amdgcn_s_setprio(1);      // (the wave that feeds the matrix cores goes first: 1.5 %)
       read_k(0);
 #pragma unroll
       for (int j = 0; j < 4; ++j) sc[j][0] = sc[j][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -456,13 +458,14 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
           __builtin_amdgcn_sched_barrier(0);
         });
       });
+      __builtin_amdgcn_s_setprio(0);
     } else {
       stage_all(next);
     }
-    if (unit + 64 < k1) {
-      take_steps();
-      if (unit + 128 < k1) load(unit + 128);
-    }
+    // (not in a branch: registers that meet behind one are copied, and a copy waits for the loads just issued.  Behind the last
+    // key the last page's codes come again and are never seen)
+    take_steps();
+    load(unit + 128);
     if (!work) continue;
     if (unit + 64 > wfull || unit + 64 > wend || __any(!now_seen)) {
 #pragma unroll
