@@ -291,8 +291,7 @@ __global__ __launch_bounds__(256, 3) void kv_few_kernel(KvAttnDev a) {
 // a step are widened once for the block on their way into LDS: what comes from memory during one step is written during
 // the next into the stage that nobody reads (one barrier a step).  A lane has 16 neighbouring keys of two queries: they lie
 // in one page, so its steps are two numbers, and the largest exponent is found on the bare products.
-// All row tiles of a sequence and key head run on one XCD, up to eight of those together with the longest tiles first (as
-// in block.hip).
+// All row tiles of a sequence and key head run on one XCD, as many of those together as fill it, the longest tiles first.
 template <typename T, int DH>
 __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -310,6 +309,20 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
   const unsigned turn = a.n_splits == 1 ? which : which / (unsigned)a.n_splits;
   const int tile = a.tiles - 1 - (int)turn, split = (int)(which - turn * a.n_splits);
   const int s = (int)a.by_heads.of(sh), hk = (int)(sh - s * a.by_heads.d);
+  const int k0 = split * a.chunk;
+  // Table entries are the same for the whole block (scalar loads, a step before the pages they name are loaded, the first beside the
+  // lengths); entries behind the last key are never seen, any will do, and one outside the pool becomes the first page, in
+  // reach and never seen.  A step's first key is a multiple of 64, so a page's part of an offset is a scalar.
+  const auto row_table = (const __attribute__((address_space(4))) int32_t*)(a.b.table + (int64_t)s * a.b.ld_table);
+  uint32_t ids[4];                     // of the next four 16 keys
+  auto entries = [&](int unit) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int at = (unit + g * 16) >> a.page_bits;
+      ids[g] = (uint32_t)row_table[at < a.b.max_pages ? at : a.b.max_pages - 1];
+    }
+  };
+  entries(k0);
   const KvSeq q = kv_sequence(a.b, a.c.page, a.n_tok, s);
   const uint32_t rows = (uint32_t)q.n_new * a.group, first_row = (uint32_t)tile * 128;
   if (first_row >= rows) return;
@@ -318,7 +331,6 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
     return p + 1 < q.len ? p + 1 : q.len;
   };
   const int end = last_key(first_row + 127);
-  const int k0 = split * a.chunk;
   if (k0 >= end && a.n_splits > 1) return;
   const int k1 = end - k0 < a.chunk ? end : k0 + a.chunk;
   const uint32_t wrow = first_row + wave * 32;
@@ -334,10 +346,6 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
   // that it has the scores of.
   const int krow = tid / (CPK / 2), kch = tid % (CPK / 2) * 2, vrow = wave * 16 + l16;
   constexpr int KSTEP = 512 / CPK;                          // rows between a thread's loads of K
-  // Table entries are the same for the whole block (scalar loads, a step before the pages they name are loaded); entries behind
-  // the last key are never seen, any will do, and one outside the pool becomes the first page, in reach and never seen.
-  // A step's first key is a multiple of 64, so a page's part of an offset is a scalar.
-  const auto row_table = (const __attribute__((address_space(4))) int32_t*)(a.b.table + (int64_t)s * a.b.ld_table);
   const uint32_t head_bytes = (uint32_t)a.c.page * DH, page_stride = (uint32_t)a.c.n_kv_heads * head_bytes;
   const uint32_t n_pages = (uint32_t)a.c.n_pages, in_page = (uint32_t)a.c.page - 1;
   const int8_t *kp = a.c.k + (uint64_t)hk * head_bytes, *vp = a.c.v + (uint64_t)hk * head_bytes;
@@ -348,13 +356,8 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
     voff[i] = (uint32_t)(vrow + i * 64) * a.c.page + ((uint32_t)(fq * 16) & in_page);
   }
   uint4 kr[LR], vr[LR];
-  uint32_t ids[4];                     // of the next four 16 keys
   bool seen = false, seen_next = false;
   float ks = 0.0f, vs = 1.0f, ks_next = 0.0f, vs_next = 1.0f;
-  auto entries = [&](int unit) {
-#pragma unroll
-    for (int g = 0; g < 4; ++g) ids[g] = (uint32_t)row_table[(unit + g * 16 < k1 ? unit + g * 16 : k1 - 1) >> a.page_bits];
-  };
   auto load = [&](int unit) {          // (the steps in front: who waits for them waits for what was issued before)
     const uint32_t at = (uint32_t)unit & in_page;
     const uint32_t mine = fq < 2 ? (fq == 0 ? ids[0] : ids[1]) : (fq == 2 ? ids[2] : ids[3]);
@@ -400,10 +403,7 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
   const int kbase = my_row * KB, kx = kkey(my_row);
   const int vbase = 64 * KB + l16 * VB, vx = l16 & 7;      // (row of V^T: 16 d + l16, the same key for all d)
 
-  if (k0 < k1) {
-    entries(k0);
-    load(k0);
-  }
+  if (k0 < k1) load(k0);
   f16x8 qf[2][NS];
   float fac[2];
   int pos[2];
@@ -714,7 +714,10 @@ hipError_t launch_kv_attention(const void* Q, int64_t ldq, int64_t n_tok, int n_
   // (powers of two: up to eight pairs side by side, and up to eight of an XCD together)
   for (a.way_bits = 0; a.way_bits < 3 && (2 << a.way_bits) <= n_pairs; ++a.way_bits) {}
   const int64_t groups = ceil_div(n_pairs, 1 << a.way_bits);
-  for (a.member_bits = 0; a.member_bits < 3 && (2 << a.member_bits) <= groups; ++a.member_bits) {}
+  // (an XCD has 64 blocks at a time: more pairs than fill them only push each other's keys out of its cache.  us with eight
+  // pairs always and by this rule: 2 x 4800 x 40 heads 600 547, 9600 x 40 1452 1031, 16 x 1200 x 40 389 391)
+  for (a.member_bits = 0; a.member_bits < 3 && (2 << a.member_bits) <= groups && ((int64_t)p.tiles * p.n_splits << a.member_bits) < 64;
+       ++a.member_bits) {}
   const int64_t chunks = ceil_div(groups, 1 << a.member_bits), gy = chunks < 32768 ? chunks : 32768;
   const int64_t work = (int64_t)p.tiles * p.n_splits, gx = p.prompt ? work << (a.way_bits + a.member_bits) : work;
   if (gx > 0x7fffffffLL || n_pairs >= (1LL << 31)) return hipErrorInvalidValue;
