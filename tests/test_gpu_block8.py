@@ -53,7 +53,8 @@ def within(got, want, bound):
 # ------------------------------------------------------------------ row codes, integer linear
 @pytest.mark.parametrize("dt", ["f16", "bf16"])
 @pytest.mark.parametrize("n,c,bits,scaled", [(1, 8, 8, True), (3, 72, 8, False), (17, 128, 4, True), (9, 1096, 2, True),
-                                             (130, 520, 6, False), (2, 13824, 8, True)])
+                                             (130, 520, 6, False), (2, 13824, 8, True), (3, 1032, 8, True),
+                                             (5, 4104, 8, True), (2, 8200, 5, True), (3, 16392, 8, True), (70, 1024, 8, True)])
 def test_row_codes_are_exact(gpu, dt, n, c, bits, scaled):
     import torch
     g = np.random.default_rng([21, n, c])
