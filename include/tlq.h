@@ -359,7 +359,7 @@ tlq_status tlq_linear_i8(const void* X, int64_t n_tok, int64_t c_in, int64_t ldx
  * d >= rot is not rotated.  Float arithmetic, one rounding to x_dtype at the end.
  * Q [n_tok, n_heads * head_dim], K [n_tok, n_kv_heads * head_dim] x_dtype, 16-byte aligned, strides multiples of 8
  * (both may be column slices of one matrix); head_dim 64, 128 or 256 (TLQ_ERR_UNSUPPORTED otherwise); rot a multiple
- * of 16, 0 <= rot <= head_dim; pos int32 [n_tok] (any sign), inv_freq double [rot/2]; wq, wk float [head_dim], 16-byte
+ * of 16, 0 <= rot <= head_dim; eps >= 0 (with 0 a head of zeros gives NaN); pos int32 [n_tok] (any sign), inv_freq double [rot/2]; wq, wk float [head_dim], 16-byte
  * aligned, or NULL (ones; both have to be NULL without norm).  Q_out may be Q with the same stride, K_out likewise K; no
  * other overlap. */
 tlq_status tlq_qk_norm_rope(const void* Q, int64_t ldq, int32_t n_heads, const void* K, int64_t ldk, int32_t n_kv_heads,
@@ -378,7 +378,8 @@ tlq_status tlq_qk_norm_rope(const void* Q, int64_t ldq, int32_t n_heads, const v
  * max_new and max_len are upper bounds of a sequence's new tokens and of its length; launches are sized by them.
  * Device values are never trusted with an address: an entry of the table outside [0, n_pages) stands for a page of tokens
  * that do not exist (nothing is written, no query sees them), cu_new is held to [0, n_tok], new tokens beyond lens[s],
- * beyond the table or beyond the bounds are left out. */
+ * beyond the table or beyond the bounds are left out (the rows of Out behind a sequence's first max_new are then not written).
+ * Bounds far above the real lengths cost speed: the keys are split by max_len. */
 typedef struct tlq_kv_cache {
   uint32_t struct_size; /* = sizeof(tlq_kv_cache) */
   int32_t n_kv_heads, head_dim, page;
@@ -398,14 +399,14 @@ typedef struct tlq_kv_batch {
  *   step = max(max |x|, 1e-5) / 127, and at least the page's step if it held tokens of the sequence before;
  *   code = clip(rint(x / step), -127, 127); codes held before: rint(code * (old step / step)).
  * Infinities count as +-127 and NaN as 0, neither has a part in the step.  Codes behind a sequence's last token stay
- * as they were.  K, V [n_tok, n_kv_heads * head_dim] x_dtype, 16-byte aligned, strides multiples of 8.  Two sequences may
- * share pages that the call does not write; a page in which two sequences of one call have new tokens ends up undefined. */
+ * as they were.  K, V [n_tok, n_kv_heads * head_dim] x_dtype, 16-byte aligned, strides multiples of 8.  Sequences may
+ * share pages that the call does not write; a page that two entries of the table name and give new tokens ends up undefined. */
 tlq_status tlq_kv_append(const void* K, int64_t ldk, const void* V, int64_t ldv, int64_t n_tok, const tlq_kv_batch* b,
                          const tlq_kv_cache* c, const tlq_params* p, void* stream);
 /* tlq_kv_attention: Out[r, h] = sum_{j <= pos(r)} softmax_j(scale * q_r . key_j) value_j, head h with the keys of head
  * h / (n_heads / n_kv_heads); row r of sequence s is its token pos(r) = lens[s] - (cu_new[s+1] - cu_new[s]) + r - cu_new[s].
  * scale: any finite number, 0 = 1 / sqrt(head_dim).  A row that sees no token gives zeros; a query that is not finite
- * makes its own row undefined and no other.  Scores, softmax and sums are
+ * makes NaN of its own row and head and of no other.  Scores, softmax and sums are
  * float; the matrix products take codes as they are, queries exactly (bf16 ones times a power of two of their row) and
  * probabilities times the page's step in fp16, which the softmax's sum takes as well; Out is rounded to x_dtype.  Steps have to
  * be positive, and scores below 2^21 in size (beyond, a float holds them to a quarter at best); other rows are undefined.

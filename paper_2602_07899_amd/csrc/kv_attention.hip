@@ -86,6 +86,18 @@ __device__ __forceinline__ float column_max(float v) {
 }
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// A query with an infinity or NaN is not to end as a row without keys (all of its scores -inf, or none above the maximum so far):
+// a lane that holds such a number makes a NaN of it, and with it the products with every key.
+template <int N>
+__device__ __forceinline__ void mark_queries(f16x8 (&qf)[N]) {
+  const f16x2 zero = {(_Float16)0.0f, (_Float16)0.0f};
+  float t = 0.0f;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) t = __builtin_amdgcn_fdot2(f16x2{qf[i][e], qf[i][e + 1]}, zero, t, false);
+  qf[0][0] = t == t ? qf[0][0] : (_Float16)t;
+}
 // A lane's channels of its query as halves, eight at a time and STEP apart (negated if asked); the factor that undoes their
 // prescale.  Lanes lane ^ 16 and lane ^ 32 hold the other channels of the same query.
 template <typename T, int N, int STEP>
@@ -97,6 +109,7 @@ __device__ __forceinline__ float load_queries(const uint16_t* p, f16x8 (&qf)[N],
   if constexpr (std::is_same<T, F16>::value) {
 #pragma unroll
     for (int i = 0; i < N; ++i) qf[i] = __builtin_bit_cast(f16x8, raw[i]);
+    mark_queries(qf);
     return 1.0f;
   }
   uint32_t top = 0;
@@ -111,14 +124,15 @@ __device__ __forceinline__ float load_queries(const uint16_t* p, f16x8 (&qf)[N],
     const uint32_t o = (uint32_t)__shfl_xor((int)top, off, 64);
     top = o > top ? o : top;
   }
-  // exponent field of the largest -> 127 + 14; rows of zeros, subnormals, infinities or NaN keep factors that are finite
+  // exponent field of the largest -> 127 + 14; rows of zeros and subnormals keep factors that are finite, infinities stay
   int k = 141 - (int)(top >> 7);
-  k = k < -112 ? -112 : (k > 126 ? 126 : k);
+  k = k > 126 ? 126 : k;
   const float up = __builtin_bit_cast(float, (uint32_t)(127 + k) << 23);
 #pragma unroll
   for (int i = 0; i < N; ++i)
 #pragma unroll
     for (int e = 0; e < 8; ++e) qf[i][e] = (_Float16)(BF16::to_float(raw[i][e]) * up);
+  mark_queries(qf);
   return __builtin_bit_cast(float, (uint32_t)(127 - k) << 23);
 }
 #endif
@@ -263,7 +277,7 @@ __global__ __launch_bounds__(256, 3) void kv_few_kernel(KvAttnDev a) {
   for (int w = 0; w < 4; ++w) m = fmaxf(m, ml[w][r].x);
 #pragma unroll
   for (int w = 0; w < 4; ++w)
-    if (ml[w][r].x != -INFINITY) l += ml[w][r].y * exp2_fast(ml[w][r].x - m);
+    l += ml[w][r].y * (ml[w][r].x == -INFINITY ? 0.0f : exp2_fast(ml[w][r].x - m));      // (NaN stays)
 #pragma unroll
   for (int e = 0; e < PER; ++e) o[e] = (part[0][r][d0 + e] + part[1][r][d0 + e]) + (part[2][r][d0 + e] + part[3][r][d0 + e]);
   const uint32_t oq = a.by_group.of(first_row + r);
@@ -276,7 +290,7 @@ __global__ __launch_bounds__(256, 3) void kv_few_kernel(KvAttnDev a) {
       *reinterpret_cast<float4*>(a.acc + at * DH + d0 + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
     return;
   }
-  const float inv = m == -INFINITY ? 0.0f : 1.0f / l;
+  const float inv = m == -INFINITY && l == 0.0f ? 0.0f : 1.0f / l;
   uint16_t w[PER];
 #pragma unroll
   for (int e = 0; e < PER; ++e) w[e] = T::from_float(o[e] * inv);
@@ -542,7 +556,7 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
       for (int d = 0; d < ND; ++d) *reinterpret_cast<f32x4*>(a.acc + at * DH + d * 16 + fq * 4) = acc[d][n];
       continue;
     }
-    const float inv = ref[n] == -INFINITY ? 0.0f : 1.0f / l;
+    const float inv = ref[n] == -INFINITY && l == 0.0f ? 0.0f : 1.0f / l;
     uint16_t* to = a.Out + token * a.ldo + head * DH + fq * 4;
 #pragma unroll
     for (int d = 0; d < ND; ++d) {
@@ -592,7 +606,7 @@ __global__ __launch_bounds__(256) void kv_join_few_kernel(KvAttnDev a, uint32_t 
 #pragma unroll
     for (int k = 0; k < 8; ++k) o += v[k] * __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), i + k));
   }
-  const float inv = m == -INFINITY ? 0.0f : 1.0f / l;
+  const float inv = m == -INFINITY && l == 0.0f ? 0.0f : 1.0f / l;
   uint16_t* to = a.Out + (q.row0 + qi) * a.ldo + (int64_t)head * DH + lane * (DH / 64);
   if constexpr (DH == 128)
     *reinterpret_cast<uint32_t*>(to) = (uint32_t)T::from_float(o[0] * inv) | (uint32_t)T::from_float(o[1] * inv) << 16;
@@ -653,7 +667,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnDev a, uint32_t tile
     const float4 v = sum[i][d];
     o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
   }
-  const float inv = m == -INFINITY ? 0.0f : 1.0f / l;
+  const float inv = m == -INFINITY && l == 0.0f ? 0.0f : 1.0f / l;
   *reinterpret_cast<uint2*>(a.Out + (q.row0 + qi) * a.ldo + (int64_t)head * DH + d * 4) =
       make_uint2((uint32_t)T::from_float(o.x * inv) | (uint32_t)T::from_float(o.y * inv) << 16,
                  (uint32_t)T::from_float(o.z * inv) | (uint32_t)T::from_float(o.w * inv) << 16);

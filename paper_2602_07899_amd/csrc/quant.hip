@@ -763,7 +763,8 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void row_codes_kernel(const 
 
 hipError_t launch_row_codes(const void* X, int64_t n, int64_t c_in, int64_t ldx, bool bf16, const float* factor, int bits,
                             int8_t* codes, int64_t ldc, float* steps, hipStream_t stream) {
-  if (c_in > 16384) return launch_act_quant(X, n, c_in, ldx, bf16, factor, 0, 1, bits, codes, steps, stream, ldc);
+  // (a block a row: rows beyond what one launch can have go eight to a block)
+  if (c_in > 16384 || n > (1 << 22)) return launch_act_quant(X, n, c_in, ldx, bf16, factor, 0, 1, bits, codes, steps, stream, ldc);
   ProfScope ps("row_codes", stream, 3.0 * (double)n * (double)c_in);
   const float qa = (float)((1 << (bits - 1)) - 1);
   auto go = [&](auto kern, int waves) {

@@ -436,6 +436,8 @@ def _rows(t, name):
     ld, one = t.stride() if t.dim() == 2 else (0, 0)
     if one != 1 and t.size(-1) != 1:
         raise ValueError(f"{name}: a row-major matrix with unit column stride")
+    if ld < t.size(-1) and t.size(0) == 1:
+        return -(-t.size(-1) // 128) * 128       # (the stride of a single row is never used and may be anything)
     return ld
 
 
@@ -471,6 +473,7 @@ def linear_i8(X, w_codes, w_steps, p, Y, factor=None, workspace=None):
     _shape(Y.size(0) == n and Y.size(1) == co, "Y: [n_tok, c_out]")
     _shape(factor is None or factor.numel() == ci and factor.is_contiguous(), "factor: one a channel")
     ws = workspace if workspace is not None else _ws(linear_i8_workspace_bytes(n, ci), X)
+    _shape(ws.get_device() == here, "workspace: not on the current device")
     _check(lib().tlq_linear_i8(X.data_ptr(), n, ci, _rows(X, "X"), None if factor is None else factor.data_ptr(), w_codes.data_ptr(), co,
                                _rows(w_codes, "w_codes"), w_steps.data_ptr(), C.byref(p), Y.data_ptr(), _rows(Y, "Y"), ws.data_ptr(),
                                ws.numel(), _stream()), "tlq_linear_i8")
@@ -551,6 +554,7 @@ def kv_attention(Q, n_heads, batch, cache, p, Out, scale=0.0, workspace=None):
     n, width = Q.size(0), Q.size(1)
     _shape(Out.size(0) == n and Out.size(1) == width == n_heads * cache.head_dim, "Q, Out: [n_tok, n_heads * head_dim]")
     ws = workspace if workspace is not None else _ws(kv_attention_workspace_bytes(n, n_heads, batch, cache), Q)
+    _shape(ws.get_device() == Q.get_device(), "workspace: not on the current device")
     _check(lib().tlq_kv_attention(Q.data_ptr(), _rows(Q, "Q"), n, n_heads, scale, C.byref(batch), C.byref(cache), C.byref(p),
                                   Out.data_ptr(), _rows(Out, "Out"), ws.data_ptr(), ws.numel(), _stream()), "tlq_kv_attention")
     return Out

@@ -332,6 +332,9 @@ def _check_attention(gpu, c, heads, dt, q, scale=0.0):
     none = np.isnan(want[:, 0])
     assert np.all(got[none] == 3.0)                            # rows behind the last sequence stay as they were
     got, want, mag, sens = got[~none], want[~none], mag[~none], np.repeat(sens[~none], c.dh, 1)
+    lost = np.isnan(want)                                      # (of a query that is not finite)
+    assert np.isnan(got[lost]).all()
+    got, want, mag, sens = got[~lost], want[~lost], mag[~lost], sens[~lost]
     # weights in 16 bits, above the line and below it: sum_j p_j e_j (v_j - out), |e_j| <= 2^-11, at most 2^-11 (mag + |out|);
     # those below 2^-21 of the largest to 2^-32 of it; scores as sums of dh products (a relative error of e^(2 ds) in p and in
     # the sum of p), sums over the keys in 32 bits, the output
@@ -440,6 +443,62 @@ def test_kv_attention_of_a_long_sequence(gpu):
     c.kc[c.table[0, 300], 0, 5, :] = 127
     c.ks[:] = np.float32(17 * np.log(2) / (127 * 8))
     _check_attention(gpu, c, 2, "f16", np.ones((1, 128), np.float32))
+
+
+@pytest.mark.parametrize("new", [1, 20])
+def test_kv_attention_of_many_keys_far_below_one(gpu, new):
+    """One key 2^22 times as heavy as each of 40,000 others, whose weights are no normal halves: together one percent of the sum,
+    in the numerator and in the denominator alike."""
+    g = np.random.default_rng(57)
+    c = Pool(g, gpu, [40000 + new], [new], 1, 64, 64, "f16")
+    for page in (2, 300, 600):                               # the heavy key in front, in the middle, near the end
+        c.kc[:] = 0
+        c.kc[c.table[0, page], 0, 5, :] = 127
+        c.ks[:] = np.float32(22 * np.log(2) / (127 * 8))
+        c.vc[c.table[0, page], 0, :, 5] = 0                  # what is left is the others' alone
+        c.vc[:] = np.abs(c.vc)
+        c.vs[:] = np.float32(0.03)
+        got = _attend(gpu, c, 2, "f16", np.ones((new, 128), np.float32))
+        want, mag, _ = ob.kv_attention(np.ones((new, 128)), 2, c.kc, c.ks, c.vc, c.vs, c.cu, c.lens, c.table, c.max_len)
+        # weights of 2^-15 and 2^7, exact halves; the score to 2^-17 of itself, sums in 32 bits, a half of a small output
+        within(got, want, want * (22 * 64 * U + 2.0 ** -11 * 1.01 + 40000 / 16 * U) + TINY["f16"])
+
+
+def test_kv_attention_of_queries_near_the_types_largest(gpu):
+    """bf16 queries of 2^127 and more against keys as small as that they give ordinary scores; subnormal ones."""
+    g = np.random.default_rng(58)
+    c = Pool(g, gpu, [70, 300], [2, 30], 1, 128, 16, "bf16")
+    c.ks *= np.float32(2.0 ** -122)
+    q = rnd(g.standard_normal((c.rows, 256)), "bf16")
+    with np.errstate(over="ignore"):                         # (a number above 4 ends as an infinity: NaN for its head)
+        q = rnd(np.float32(2.0 ** 126) * q / np.abs(q).max(axis=1, keepdims=True) * 3.9, "bf16")
+    assert np.isfinite(q).mean() > 0.99
+    _check_attention(gpu, c, 2, "bf16", q)
+    c.ks *= np.float32(2.0 ** 122)
+    _check_attention(gpu, c, 2, "bf16", rnd(q.astype(np.float64) * 2.0 ** -258, "bf16"))
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("new", [1, 20, 150])
+def test_kv_attention_of_queries_that_are_not_finite(gpu, dt, new):
+    """An infinity or a NaN anywhere in a query makes its head NaN, whichever sign the keys have there, and no other head; a row
+    that sees no key gives zeros still.  Split and unsplit."""
+    g = np.random.default_rng(59)
+    for length in (200, 3000):
+        c = Pool(g, gpu, [length, 40], [new, 1], 2, 64, 32, dt)
+        c.kc[:, 0] = np.abs(c.kc[:, 0])
+        c.table[1, :] = -1
+        q = rnd(g.standard_normal((c.rows, 4 * 64)), dt)
+        clean = _attend(gpu, c, 4, dt, q)
+        bad = q.copy()
+        bad[0, 3], bad[0, 64 * 2 + 50] = -np.inf, np.nan       # heads 0 and 2
+        bad[new // 2, 64 + 63], bad[new // 2, 64 * 3] = np.inf, -np.inf
+        bad[c.rows - 1, 0] = np.nan
+        got = _attend(gpu, c, 4, dt, bad)
+        lost = np.repeat(~np.isfinite(bad).reshape(c.rows, 4, 64).all(2), 64, 1)
+        lost[c.rows - 1] = False
+        assert np.isfinite(clean).all() and (clean[c.rows - 1] == 0.0).all()
+        assert np.isnan(got[lost]).all() and np.array_equal(got[~lost], clean[~lost])
 
 
 # ------------------------------------------------------------------ together
@@ -600,3 +659,40 @@ def test_calls_on_another_stream(gpu):
         tlq.kv_attention(q, 4, b, cache, p, out)
     side.synchronize()
     assert torch.equal(out, want)
+
+
+def test_two_streams_at_once(gpu):
+    """Calls on two streams with workspaces and outputs of their own do not meet."""
+    import torch
+    g = np.random.default_rng(64)
+    p = tlq.params(act_bits=8)
+    c = Pool(g, gpu, [3000, 100], [1, 1], 2, 128, 64, "f16")
+    b, cache = c.load()
+    x, f, wc, ws = _linear_case(g, 40, 2056, 9001, "f16", 8)
+    X, W, S, F = dev(x, gpu, "f16"), _padded(wc, gpu), dev(ws, gpu), dev(f, gpu)
+    q = dev(rnd(g.standard_normal((2, 8 * 128)), "f16"), gpu, "f16")
+    y0 = tlq.linear_i8(X, W, S, p, torch.empty((40, 9008), dtype=torch.float16, device=gpu)[:, :9001], factor=F).clone()
+    a0 = tlq.kv_attention(q, 8, b, cache, p, torch.empty_like(q)).clone()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = []
+    torch.cuda.synchronize()
+    for i in range(6):
+        with torch.cuda.stream(streams[i % 2]):
+            y = torch.empty((40, 9008), dtype=torch.float16, device=gpu)[:, :9001]
+            outs.append((tlq.linear_i8(X, W, S, p, y, factor=F), tlq.kv_attention(q, 8, b, cache, p, torch.empty_like(q))))
+    torch.cuda.synchronize()
+    for y, a in outs:
+        assert torch.equal(y, y0) and torch.equal(a, a0)
+
+
+def test_single_rows_of_any_stride(gpu):
+    """The stride of a matrix of one row is never used."""
+    import torch
+    g = np.random.default_rng(65)
+    p = tlq.params(act_bits=8)
+    x, f, wc, ws = _linear_case(g, 1, 256, 24, "f16", 8)
+    X = dev(x, gpu, "f16")
+    column = X.reshape(256, 1).t()                            # [1, 256] with strides of one
+    W, S = _padded(wc, gpu), dev(ws, gpu)
+    a, b = (tlq.linear_i8(t, W, S, p, torch.empty((1, 24), dtype=torch.float16, device=gpu)) for t in (X, column))
+    assert column.stride() == (1, 1) and torch.equal(a, b)
