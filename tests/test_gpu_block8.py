@@ -257,6 +257,9 @@ APPENDS = [
     ([1], [1], 1, 64, 16), ([16, 17, 33], [16, 1, 33], 2, 128, 16), ([100, 64, 65, 1], [37, 64, 1, 1], 3, 128, 64),
     ([200, 0, 5], [90, 0, 5], 2, 64, 128), ([300, 299], [3, 299], 1, 128, 256), ([48, 40, 47], [9, 40, 2], 5, 128, 32),
     ([2, 130], [5, 2], 2, 64, 32),           # more new rows than the sequence has tokens
+    ([300, 128, 129, 1], [190, 100, 129, 1], 2, 128, 128), ([700, 256, 257, 300], [500, 130, 257, 299], 3, 64, 256),
+    ([200, 64], [150, 64], 1, 64, 64), ([90, 33], [80, 20], 2, 64, 32), ([70, 17], [60, 16], 2, 128, 16),
+    ([600, 513], [400, 513], 1, 128, 256),
 ]
 
 
@@ -352,6 +355,9 @@ ATTENTION = [   # lens, new, kv heads, group, dh, page
     ([40, 41, 64], [3, 9, 2], 2, 3, 128, 32), ([65, 130], [65, 130], 2, 1, 128, 64), ([33, 100], [33, 50], 1, 4, 64, 16),
     ([500], [129], 2, 1, 128, 64), ([700, 300, 5], [200, 300, 5], 1, 2, 64, 128), ([150, 0, 20], [150, 0, 20], 2, 6, 128, 16),
     ([1500], [17], 1, 1, 128, 64), ([20], [20], 1, 40, 64, 16),
+    ([2600, 700, 30], [40, 40, 30], 2, 3, 128, 32), ([2600, 700, 30], [40, 40, 30], 2, 3, 64, 256),   # splits that some lack
+    ([90, 10, 200, 33, 64], [90, 10, 150, 33, 1], 5, 2, 128, 16),                                      # 25 pairs
+    ([300] * 3, [140, 1, 300], 3, 1, 64, 16), ([1100, 1024, 513, 256], [1, 1, 1, 1], 1, 16, 64, 16),
 ]
 
 
@@ -430,6 +436,60 @@ def test_kv_attention_of_a_shared_prefix(gpu):
     c.table[1, :2] = c.table[0, :2]
     q = rnd(g.standard_normal((2, 4 * 128)), "f16")
     _check_attention(gpu, c, 4, "f16", q)
+
+
+@pytest.mark.parametrize("lens,new", [([700, 90], [1, 1]), ([700, 90], [40, 90])])
+def test_kv_tables_that_are_part_of_a_wider_one(gpu, lens, new):
+    """Rows of a table further apart than they are long, what lies between them naming pages of no sequence."""
+    g = np.random.default_rng(60)
+    dt = "bf16"
+    c = Pool(g, gpu, lens, new, 2, 128, 64, dt)
+    q = rnd(g.standard_normal((c.rows, 4 * 128)), dt)
+    x = rnd(g.standard_normal((c.rows, 2 * 128)), dt)
+    narrow = _attend(gpu, c, 4, dt, q)
+    b, cache = c.load()
+    wide = dev(np.concatenate([c.table, np.full((2, 5), c.n - 1, np.int32)], 1), gpu)
+    b = tlq.kv_batch(b.parts[0], b.parts[1], wide[:, :c.table.shape[1]], c.max_new, c.max_len)
+    Q, X, p = dev(q, gpu, dt), dev(x, gpu, dt), tlq.params(x_dtype=CODE[dt])
+    assert np.array_equal(host(tlq.kv_attention(Q, 4, b, cache, p, dev(q, gpu, dt))), narrow)
+    tlq.kv_append(X, X, b, cache, p)
+    ob.kv_append(x, c.kc, c.ks, c.cu, c.lens, c.table, c.max_len, False)
+    ob.kv_append(x, c.vc, c.vs, c.cu, c.lens, c.table, c.max_len, True)
+    for got, want in zip(c.t, (c.kc, c.ks, c.vc, c.vs)):
+        assert np.array_equal(got.cpu().numpy(), want)
+
+
+def test_kv_attention_of_more_splits_than_lanes(gpu):
+    """Parts of 256 keys of one sequence, and of a short one beside it."""
+    g = np.random.default_rng(61)
+    c = Pool(g, gpu, [40000, 300], [1, 1], 1, 128, 128, "bf16")
+    _check_attention(gpu, c, 4, "bf16", rnd(g.standard_normal((2, 4 * 128)), "bf16"))
+
+
+def test_kv_pools_beyond_two_to_the_31(gpu):
+    """Pages whose codes lie further than 2^31 and 2^32 bytes into the pool."""
+    import torch
+    kv, dh, page, n = 2, 128, 256, (1 << 16) + 300            # 65,536 bytes a page: 4.3 GB of keys, as many of values
+    kc, vc = (torch.empty((n, kv) + sh, dtype=torch.int8, device=gpu) for sh in ((page, dh), (dh, page)))
+    ks, vs = (torch.empty((n, kv), dtype=torch.float32, device=gpu) for _ in range(2))
+    cache = tlq.kv_cache(kc, ks, vc, vs)
+    small = [t[:8].clone() for t in (kc, ks, vc, vs)]
+    near = tlq.kv_cache(*small)
+    far = np.array([[n - 1, 40000, 5], [65537, 32769, 3]], np.int32)
+    cu, lens = np.array([0, 600, 1100], np.int32), np.array([600, 500], np.int32)
+    X = torch.randn((1100, kv * dh), device=gpu).half()
+    p = tlq.params()
+    outs = []
+    for table, pool in ((far, cache), (np.array([[0, 1, 2], [3, 4, 5]], np.int32), near)):
+        t = dev(table, gpu)
+        tlq.kv_append(X, X, tlq.kv_batch(dev(cu, gpu), dev(lens, gpu), t, 600, 600), pool, p)
+        Q = X.repeat(1, 2).contiguous()
+        outs.append(tlq.kv_attention(Q, 4, tlq.kv_batch(dev(cu, gpu), dev(lens, gpu), t, 600, 600), pool, p, torch.empty_like(Q)))
+        one = tlq.kv_batch(dev(np.array([0, 1, 2], np.int32), gpu), dev(lens, gpu), t, 1, 600)
+        tlq.kv_append(X[:2], X[2:4], one, pool, p)            # (the few-token kernels)
+        outs.append(tlq.kv_attention(Q[:2], 4, one, pool, p, torch.empty_like(Q[:2])))
+    assert torch.equal(outs[0], outs[2]) and torch.equal(outs[1], outs[3])
+    assert outs[0].isfinite().all() and outs[1].isfinite().all()
 
 
 def test_kv_attention_of_a_long_sequence(gpu):
