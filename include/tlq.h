@@ -346,7 +346,7 @@ tlq_status tlq_row_codes(const void* X, int64_t n, int64_t c, int64_t ldx, const
 /* tlq_linear_i8: Y[t,o] = step_t * w_step[o] * sum_c code[t,c] * w_codes[o,c], with the codes and steps that
  * tlq_row_codes gives X (factor as there, bits = p->act_bits, TLQ_ERR_UNSUPPORTED if that is 0); the sums are exact.
  * w_codes int8 [c_out, ldw] and w_steps float [c_out] as tlq_row_codes writes them (the zeros behind c_in up to the next
- * multiple of 128 are read; w_steps 16-byte aligned); c_in a multiple of 8, at most 65536; ldw < 2^22.
+ * multiple of 128 are read; w_steps 16-byte aligned); c_in a multiple of 8, at most 65536; ldw < 2^22; c_out < 2^29.
  * Y [n_tok, c_out] yref_dtype, 16-byte aligned, ldy a multiple of 8 (4 for float).  Workspace from the query. */
 size_t tlq_linear_i8_workspace_bytes(int64_t n_tok, int64_t c_in);
 tlq_status tlq_linear_i8(const void* X, int64_t n_tok, int64_t c_in, int64_t ldx, const float* factor,
@@ -357,7 +357,7 @@ tlq_status tlq_linear_i8(const void* X, int64_t n_tok, int64_t c_in, int64_t ldx
  *   u = x / sqrt(mean_d x^2 + eps) * w[d];  angle = pos[t] * inv_freq[i] (in double), i < rot / 2;
  *   (u_a, u_b) -> (u_a cos - u_b sin, u_b cos + u_a sin), (a, b) = (i, i + rot/2), or (2i, 2i+1) with interleaved = 1;
  * d >= rot is not rotated.  Float arithmetic, one rounding to x_dtype at the end.
- * Q [n_tok, n_heads * head_dim], K [n_tok, n_kv_heads * head_dim] x_dtype, 16-byte aligned, strides multiples of 8
+ * Q [n_tok, n_heads * head_dim], K [n_tok, n_kv_heads * head_dim] x_dtype, n_tok < 2^26, 16-byte aligned, strides multiples of 8
  * (both may be column slices of one matrix); head_dim 64, 128 or 256 (TLQ_ERR_UNSUPPORTED otherwise); rot a multiple
  * of 16, 0 <= rot <= head_dim; eps >= 0 (with 0 a head of zeros gives NaN); pos int32 [n_tok] (any sign), inv_freq double [rot/2]; wq, wk float [head_dim], 16-byte
  * aligned, or NULL (ones; both have to be NULL without norm).  Q_out may be Q with the same stride, K_out likewise K; no
@@ -400,18 +400,20 @@ typedef struct tlq_kv_batch {
  *   code = clip(rint(x / step), -127, 127); codes held before: rint(code * (old step / step)).
  * Infinities count as +-127 and NaN as 0, neither has a part in the step.  Codes behind a sequence's last token stay
  * as they were.  K, V [n_tok, n_kv_heads * head_dim] x_dtype, 16-byte aligned, strides multiples of 8.  Sequences may
- * share pages that the call does not write; a page that two entries of the table name and give new tokens ends up undefined. */
+ * share pages that the call does not write; a page that two entries of the table name and give new tokens ends up undefined.
+ * n_seq times the pages that max_new tokens can lie in: below 2^24. */
 tlq_status tlq_kv_append(const void* K, int64_t ldk, const void* V, int64_t ldv, int64_t n_tok, const tlq_kv_batch* b,
                          const tlq_kv_cache* c, const tlq_params* p, void* stream);
 /* tlq_kv_attention: Out[r, h] = sum_{j <= pos(r)} softmax_j(scale * q_r . key_j) value_j, head h with the keys of head
  * h / (n_heads / n_kv_heads); row r of sequence s is its token pos(r) = lens[s] - (cu_new[s+1] - cu_new[s]) + r - cu_new[s].
  * scale: any finite number, 0 = 1 / sqrt(head_dim).  A row that sees no token gives zeros; a query that is not finite
  * makes NaN of its own row and head and of no other.  Scores, softmax and sums are
- * float; the matrix products take codes as they are, queries exactly (bf16 ones times a power of two of their row) and
+ * float; the matrix products take codes as they are, queries exactly (bf16 ones times a power of two of their row; channels
+ * below 2^-31 of its largest are rounded to 2^-39 of it) and
  * probabilities times the page's step in fp16, which the softmax's sum takes as well; Out is rounded to x_dtype.  Steps have to
  * be positive, and scores below 2^21 in size (beyond, a float holds them to a quarter at best); other rows are undefined.
  * Q, Out [n_tok, n_heads * head_dim] x_dtype, 16-byte aligned, strides multiples of 8; n_heads a multiple of n_kv_heads;
- * n_tok * (n_heads / n_kv_heads) and n_seq * n_kv_heads below 2^31 - 256.
+ * n_tok * (n_heads / n_kv_heads) and n_seq * n_kv_heads below 2^31 - 256, max_new * (n_heads / n_kv_heads) below 2^28.
  * The workspace query reads sizes only, no pointer; the result does not depend on the workspace's contents. */
 size_t tlq_kv_attention_workspace_bytes(int64_t n_tok, int32_t n_heads, const tlq_kv_batch* b, const tlq_kv_cache* c);
 tlq_status tlq_kv_attention(const void* Q, int64_t ldq, int64_t n_tok, int32_t n_heads, float scale, const tlq_kv_batch* b,

@@ -882,7 +882,7 @@ tlq_status tlq_linear_i8(const void* X, int64_t n_tok, int64_t c_in, int64_t ldx
   if (!X || !w_codes || !w_steps || !Y) return TLQ_ERR_NULL;
   TLQ_TRY(check_params(p));
   if (p->act_bits == 0 || c_in > kMaxLinearI8) return TLQ_ERR_UNSUPPORTED;
-  if (!dims_ok(n_tok, c_in, ldx) || (c_in % 8) != 0 || !dims_ok(c_out, int8_row(c_in), ldw) || ldw >= (1LL << 22) ||
+  if (!dims_ok(n_tok, c_in, ldx) || (c_in % 8) != 0 || !dims_ok(c_out, int8_row(c_in), ldw) || ldw >= (1LL << 22) || c_out >= (1LL << 29) ||
       !dims_ok(n_tok, c_out, ldy))
     return TLQ_ERR_SHAPE;
   if (!mat16_aligned(X, ldx) || !aligned(w_codes, 16) || (ldw % 16) != 0 || !aligned(w_steps, 16) ||
@@ -919,7 +919,7 @@ tlq_status tlq_qk_norm_rope(const void* Q, int64_t ldq, int32_t n_heads, const v
   if ((head_dim != 64 && head_dim != 128 && head_dim != 256) || (interleaved != 0 && interleaved != 1) ||
       (norm != 0 && norm != 1) || (norm == 0 && (wq || wk)) || !(eps >= 0.0f) || eps > 3.0e38f)
     return TLQ_ERR_UNSUPPORTED;
-  if (n_tok <= 0 || n_tok >= (1LL << 31) || n_heads <= 0 || n_heads > 65535 || n_kv_heads <= 0 || n_kv_heads > 65535 || rot < 0 ||
+  if (n_tok <= 0 || n_tok >= (1LL << 26) || n_heads <= 0 || n_heads > 65535 || n_kv_heads <= 0 || n_kv_heads > 65535 || rot < 0 ||
       rot > head_dim || (rot % 16) != 0)
     return TLQ_ERR_SHAPE;
   const int64_t wide = (int64_t)n_heads * head_dim, narrow = (int64_t)n_kv_heads * head_dim;
@@ -961,19 +961,21 @@ tlq_status tlq_kv_append(const void* K, int64_t ldk, const void* V, int64_t ldv,
   TLQ_TRY(check_kv(b, c));
   const int64_t width = (int64_t)c->n_kv_heads * c->head_dim;
   if (n_tok <= 0 || n_tok >= (1LL << 31) || ldk < width || ldv < width) return TLQ_ERR_SHAPE;
+  if (b->n_seq * kv_append_pages(n_tok, *b, *c) >= (1LL << 24)) return TLQ_ERR_SHAPE;
   if (!mat16_aligned(K, ldk) || !mat16_aligned(V, ldv)) return TLQ_ERR_ALIGN;
   return hip_status(launch_kv_append(K, ldk, V, ldv, n_tok, *b, *c, p->x_dtype == TLQ_BF16, (hipStream_t)stream));
 }
 
-static tlq_status check_kv_heads(int64_t n_tok, int32_t n_heads, const tlq_kv_cache* c) {
+static tlq_status check_kv_heads(int64_t n_tok, int32_t n_heads, const tlq_kv_batch* b, const tlq_kv_cache* c) {
   if (n_tok <= 0 || n_tok >= (1LL << 31) || n_heads <= 0 || n_heads > 65535 || (n_heads % c->n_kv_heads) != 0 ||
-      n_tok * (n_heads / c->n_kv_heads) >= (1LL << 31) - 256)      // (rows are counted in 32 bits)
+      n_tok * (n_heads / c->n_kv_heads) >= (1LL << 31) - 256 ||      // (rows are counted in 32 bits; a launch has 2^24 blocks)
+      (b->max_new < n_tok ? b->max_new : n_tok) * (n_heads / c->n_kv_heads) >= (1LL << 28))
     return TLQ_ERR_SHAPE;
   return TLQ_OK;
 }
 
 size_t tlq_kv_attention_workspace_bytes(int64_t n_tok, int32_t n_heads, const tlq_kv_batch* b, const tlq_kv_cache* c) {
-  if (check_kv_sizes(b, c) != TLQ_OK || check_kv_heads(n_tok, n_heads, c) != TLQ_OK) return 0;
+  if (check_kv_sizes(b, c) != TLQ_OK || check_kv_heads(n_tok, n_heads, b, c) != TLQ_OK) return 0;
   return kv_attention_workspace(n_tok, n_heads, *b, *c);
 }
 
@@ -983,7 +985,7 @@ tlq_status tlq_kv_attention(const void* Q, int64_t ldq, int64_t n_tok, int32_t n
   if (!Q || !Out) return TLQ_ERR_NULL;
   TLQ_TRY(check_params(p));
   TLQ_TRY(check_kv(b, c));
-  TLQ_TRY(check_kv_heads(n_tok, n_heads, c));
+  TLQ_TRY(check_kv_heads(n_tok, n_heads, b, c));
   if (!(scale - scale == 0.0f)) return TLQ_ERR_UNSUPPORTED;
   const int64_t width = (int64_t)n_heads * c->head_dim;
   if (ldq < width || ldo < width) return TLQ_ERR_SHAPE;

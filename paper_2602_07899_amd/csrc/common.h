@@ -283,7 +283,8 @@ struct QkRopeArgs {
 };
 hipError_t launch_qk_norm_rope(const QkRopeArgs& a, hipStream_t stream);
 
-// the 8-bit cache (kv_append.hip, kv_attention.hip)
+// the 8-bit cache (kv_append.hip, kv_attention.hip); pages that the new tokens of a sequence can lie in
+int64_t kv_append_pages(int64_t n_tok, const tlq_kv_batch& b, const tlq_kv_cache& c);
 hipError_t launch_kv_append(const void* K, int64_t ldk, const void* V, int64_t ldv, int64_t n_tok, const tlq_kv_batch& b,
                             const tlq_kv_cache& c, bool bf16, hipStream_t stream);
 size_t kv_attention_workspace(int64_t n_tok, int n_heads, const tlq_kv_batch& b, const tlq_kv_cache& c);

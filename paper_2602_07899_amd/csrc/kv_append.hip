@@ -278,13 +278,17 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const uint16_t* __restri
 #endif
 }
 
+int64_t kv_append_pages(int64_t n_tok, const tlq_kv_batch& b, const tlq_kv_cache& c) {
+  const int64_t most = b.max_new < n_tok ? b.max_new : n_tok;
+  return (most - 1 + c.page - 1) / c.page + 1;
+}
+
 hipError_t launch_kv_append(const void* K, int64_t ldk, const void* V, int64_t ldv, int64_t n_tok, const tlq_kv_batch& b,
                             const tlq_kv_cache& c, bool bf16, hipStream_t stream) {
   ProfScope ps("kv_append", stream, 6.0 * (double)n_tok * c.n_kv_heads * c.head_dim);
   const int64_t most = b.max_new < n_tok ? b.max_new : n_tok;
-  const int max_touch = (int)((most - 1 + c.page - 1) / c.page + 1);     // pages that `most` tokens can lie in
+  const int max_touch = (int)kv_append_pages(n_tok, b, c);
   const int64_t gx = (int64_t)b.n_seq * max_touch;
-  if (gx > 0x7fffffffLL) return hipErrorInvalidValue;
   // Where less than half a page is new the pieces of the other kernel are mostly empty; pages of 256 x 128 would need twice the
   // registers there are for two blocks.  64 sequences x 8 heads of 128, us few and many, by new tokens: pages of 16, 8 7.9 8.2, 16
   // 9.1 8.5; of 64, 1 5.7 12.4, 24 13.0 14.0, 32 14.6 13.9, 128 28.9 21.8; of 128, 32 16.2 21.1, 64 26.4 25.7; of 256, 128 47 66,

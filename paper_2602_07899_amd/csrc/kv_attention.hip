@@ -734,7 +734,6 @@ hipError_t launch_kv_attention(const void* Q, int64_t ldq, int64_t n_tok, int n_
        ++a.member_bits) {}
   const int64_t chunks = ceil_div(groups, 1 << a.member_bits), gy = chunks < 32768 ? chunks : 32768;
   const int64_t work = (int64_t)p.tiles * p.n_splits, gx = p.prompt ? work << (a.way_bits + a.member_bits) : work;
-  if (gx > 0x7fffffffLL || n_pairs >= (1LL << 31)) return hipErrorInvalidValue;
   const dim3 grid = p.prompt ? dim3((unsigned)gx, (unsigned)gy, (unsigned)ceil_div(chunks, gy))
                              : dim3((unsigned)gx, (unsigned)c.n_kv_heads, (unsigned)b.n_seq);
   auto pick = [&](auto t, auto dh) {

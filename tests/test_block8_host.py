@@ -32,7 +32,7 @@ def test_linear_refusals():
     for k in ("X", "w", "ws", "Y"):
         assert call(**{k: None}) == tlq.ERR_NULL, k
     assert call(par=tlq.params()) == call(ci=65544, ldx=65544, ldw=65664) == tlq.ERR_UNSUPPORTED
-    assert call(n=0) == call(co=0) == call(ci=76, ldx=80) == call(ldw=112) == call(ldw=1 << 22) == call(ldy=4) == call(ldx=64) == tlq.ERR_SHAPE
+    assert call(n=0) == call(co=0) == call(ci=76, ldx=80) == call(ldw=112) == call(ldw=1 << 22) == call(co=1 << 29, ldy=1 << 29) == call(ldy=4) == call(ldx=64) == tlq.ERR_SHAPE
     assert call(X=ODD) == call(w=ODD) == call(ws=ODD) == call(f=ODD) == call(Y=ODD) == call(ldw=136) == call(ldy=12) == tlq.ERR_ALIGN
     assert call(work=None) == call(size=16) == tlq.ERR_WORKSPACE
     assert call(work=ODD) == tlq.ERR_ALIGN
@@ -53,7 +53,7 @@ def test_rope_refusals():
     for bad in (dict(dh=96), dict(dh=512), dict(pairs=2), dict(norm=2), dict(norm=0), dict(norm=0, wq=None), dict(eps=-1.0),
                 dict(eps=float("nan")), dict(eps=float("inf"))):
         assert call(**bad) == tlq.ERR_UNSUPPORTED, bad
-    for bad in (dict(n=0), dict(n=1 << 31), dict(h=0), dict(kv=0), dict(h=65536, ldq=1 << 24, ldqo=1 << 24), dict(rot=-16), dict(rot=144),
+    for bad in (dict(n=0), dict(n=1 << 31), dict(n=1 << 26), dict(h=0), dict(kv=0), dict(h=65536, ldq=1 << 24, ldqo=1 << 24), dict(rot=-16), dict(rot=144),
                 dict(rot=24), dict(ldq=248), dict(ldk=120), dict(ldqo=128), dict(ldko=64)):
         assert call(**bad) == tlq.ERR_SHAPE, bad
     for bad in (dict(Q=ODD), dict(K=ODD), dict(qo=ODD), dict(ko=ODD), dict(ldq=260), dict(ldko=132), dict(wq=ODD), dict(wk=ODD),
@@ -101,6 +101,9 @@ def test_cache_refusals():
     assert append(K=ODD) == append(V=ODD) == append(ldk=260) == append(ldv=260) == tlq.ERR_ALIGN
     assert attend(Q=None) == attend(Out=None) == tlq.ERR_NULL
     assert attend(heads=3) == attend(heads=0) == attend(ldq=504) == attend(ldo=256) == attend(heads=65536) == tlq.ERR_SHAPE
+    # more blocks than a launch can have
+    assert append(n=1 << 30, n_seq=1000, max_new=1 << 20, max_len=1 << 20, page=16) == tlq.ERR_SHAPE
+    assert attend(n=1 << 28, heads=4, max_new=1 << 28, max_len=1 << 28, n_kv_heads=4, ldq=512) == tlq.ERR_SHAPE
     assert attend(scale=float("nan")) == attend(scale=float("inf")) == tlq.ERR_UNSUPPORTED
     assert attend(Q=ODD) == attend(Out=ODD) == attend(ldq=516) == attend(ldo=516) == tlq.ERR_ALIGN
     long = dict(max_len=100000, max_pages=2000, ld_table=2000, n=3)
