@@ -403,7 +403,7 @@ class _Torch:
         import torch
         self.torch, self.i8, self.i32, self.f32, self.f64 = torch, torch.int8, torch.int32, torch.float32, torch.float64
         self.of = (torch.float16, torch.bfloat16, torch.float32)
-        self.device = torch._C._cuda_getDevice
+        self.device, self.raw_stream, self.in_bad_fork = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, torch._C._cuda_isInBadFork
 
 
 def _types():
@@ -426,6 +426,11 @@ def _current(t):
     return _types().device()
 
 
+def _stream_of(here):
+    """_stream of the current device, which is known here."""
+    return _stream() if _t.in_bad_fork() else _t.raw_stream(here)
+
+
 def _shape(ok, what):
     if not ok:
         raise ValueError(what)
@@ -433,12 +438,20 @@ def _shape(ok, what):
 
 def _rows(t, name):
     """Row stride of a matrix with neighbouring columns."""
-    ld, one = t.stride() if t.dim() == 2 else (0, 0)
-    if one != 1 and t.size(-1) != 1:
+    s = t.stride()
+    if len(s) == 2 and s[1] == 1 and s[0] >= t.size(1):
+        return s[0]
+    if len(s) != 2 or s[1] != 1 and t.size(1) != 1:
         raise ValueError(f"{name}: a row-major matrix with unit column stride")
-    if ld < t.size(-1) and t.size(0) == 1:
-        return -(-t.size(-1) // 128) * 128       # (the stride of a single row is never used and may be anything)
-    return ld
+    # (the stride of a single row is never used and may be anything)
+    return -(-t.size(1) // 128) * 128 if t.size(0) == 1 else s[0]
+
+
+def _size(t, name):
+    s = t.shape
+    if len(s) != 2:
+        raise ValueError(f"{name}: a matrix")
+    return s
 
 
 def row_codes(X, bits, p, codes, steps, factor=None):
@@ -447,13 +460,13 @@ def row_codes(X, bits, p, codes, steps, factor=None):
     for t, want, name in ((X, ty.of[p.x_dtype], "X"), (codes, ty.i8, "codes"), (steps, ty.f32, "steps"), (factor, ty.f32, "factor")):
         if t is not None and (t.dtype is not want or t.get_device() != here):
             _wrong(t, want, name, here)
-    n, c = X.size(0), X.size(1)
+    n, c = _size(X, "X")
     ldc = _rows(codes, "codes")
     _shape(codes.size(0) == n and ldc >= codes.size(1) >= -(-c // 128) * 128, "codes: n rows, zeros behind c up to a multiple of 128")
     _shape(steps.numel() == n and steps.is_contiguous(), "steps: one a row")
     _shape(factor is None or factor.numel() == c and factor.is_contiguous(), "factor: one a channel")
     _check(lib().tlq_row_codes(X.data_ptr(), n, c, _rows(X, "X"), None if factor is None else factor.data_ptr(), bits, C.byref(p),
-                               codes.data_ptr(), ldc, steps.data_ptr(), _stream()), "tlq_row_codes")
+                               codes.data_ptr(), ldc, steps.data_ptr(), _stream_of(here)), "tlq_row_codes")
 
 
 def linear_i8_workspace_bytes(n_tok, c_in):
@@ -467,16 +480,16 @@ def linear_i8(X, w_codes, w_steps, p, Y, factor=None, workspace=None):
                           (Y, ty.of[p.yref_dtype], "Y"), (factor, ty.f32, "factor")):
         if t is not None and (t.dtype is not want or t.get_device() != here):
             _wrong(t, want, name, here)
-    n, ci, co = X.size(0), X.size(1), w_codes.size(0)
-    _shape(w_codes.size(1) >= -(-ci // 128) * 128, "w_codes: rows with zeros behind c_in up to a multiple of 128")
+    (n, ci), (co, wide) = _size(X, "X"), _size(w_codes, "w_codes")
+    _shape(wide >= -(-ci // 128) * 128, "w_codes: rows with zeros behind c_in up to a multiple of 128")
     _shape(w_steps.numel() == co and w_steps.is_contiguous(), "w_steps: one an output")
-    _shape(Y.size(0) == n and Y.size(1) == co, "Y: [n_tok, c_out]")
+    _shape(Y.shape == (n, co), "Y: [n_tok, c_out]")
     _shape(factor is None or factor.numel() == ci and factor.is_contiguous(), "factor: one a channel")
     ws = workspace if workspace is not None else _ws(linear_i8_workspace_bytes(n, ci), X)
     _shape(ws.get_device() == here, "workspace: not on the current device")
     _check(lib().tlq_linear_i8(X.data_ptr(), n, ci, _rows(X, "X"), None if factor is None else factor.data_ptr(), w_codes.data_ptr(), co,
                                _rows(w_codes, "w_codes"), w_steps.data_ptr(), C.byref(p), Y.data_ptr(), _rows(Y, "Y"), ws.data_ptr(),
-                               ws.numel(), _stream()), "tlq_linear_i8")
+                               ws.numel(), _stream_of(here)), "tlq_linear_i8")
     return Y
 
 
@@ -489,8 +502,8 @@ def qk_norm_rope(Q, K, head_dim, pos, inv_freq, p, Q_out, K_out, wq=None, wk=Non
                           (inv_freq, ty.f64, "inv_freq"), (wq, f32, "wq"), (wk, f32, "wk")):
         if t is not None and (t.dtype is not want or t.get_device() != here):
             _wrong(t, want, name, here)
-    n, nq, nk = Q.size(0), Q.size(1), K.size(1)
-    _shape(K.size(0) == n == Q_out.size(0) == K_out.size(0) and Q_out.size(1) == nq and K_out.size(1) == nk, "outputs of the inputs' shapes")
+    (n, nq), (rows, nk) = _size(Q, "Q"), _size(K, "K")
+    _shape(rows == n and Q_out.shape == (n, nq) and K_out.shape == (n, nk), "outputs of the inputs' shapes")
     _shape(head_dim > 0 and nq % head_dim == 0 and nk % head_dim == 0, "whole heads")
     _shape(pos.numel() == n and pos.is_contiguous() and (inv_freq is None or inv_freq.is_contiguous()), "pos: one a row")
     for w in (wq, wk):
@@ -499,7 +512,7 @@ def qk_norm_rope(Q, K, head_dim, pos, inv_freq, p, Q_out, K_out, wq=None, wk=Non
                                   0 if inv_freq is None else 2 * inv_freq.numel(), 1 if interleaved else 0, 1 if norm else 0, eps,
                                   None if wq is None else wq.data_ptr(), None if wk is None else wk.data_ptr(), pos.data_ptr(),
                                   None if inv_freq is None else inv_freq.data_ptr(), C.byref(p), Q_out.data_ptr(),
-                                  _rows(Q_out, "Q_out"), K_out.data_ptr(), _rows(K_out, "K_out"), _stream()), "tlq_qk_norm_rope")
+                                  _rows(Q_out, "Q_out"), K_out.data_ptr(), _rows(K_out, "K_out"), _stream_of(here)), "tlq_qk_norm_rope")
     return Q_out, K_out
 
 
@@ -533,15 +546,16 @@ def _kv_tensors(p, batch, cache, x, y, names):
                           *zip(cache.parts, (i8, i8, f32, f32), ("k", "v", "k_step", "v_step"))):
         if t.dtype is not want or t.get_device() != here:
             _wrong(t, want, name, here)
+    return here
 
 
 def kv_append(K, V, batch, cache, p):
     """New rows of keys and values [n_tok, n_kv_heads * head_dim] into the cache's pages."""
-    _kv_tensors(p, batch, cache, K, V, "KV")
-    n, width = K.size(0), K.size(1)
-    _shape(V.size(0) == n and V.size(1) == width == cache.n_kv_heads * cache.head_dim, "K, V: [n_tok, n_kv_heads * head_dim]")
+    here = _kv_tensors(p, batch, cache, K, V, "KV")
+    n, width = _size(K, "K")
+    _shape(V.shape == (n, width) and width == cache.n_kv_heads * cache.head_dim, "K, V: [n_tok, n_kv_heads * head_dim]")
     _check(lib().tlq_kv_append(K.data_ptr(), _rows(K, "K"), V.data_ptr(), _rows(V, "V"), n, C.byref(batch), C.byref(cache), C.byref(p),
-                               _stream()), "tlq_kv_append")
+                               _stream_of(here)), "tlq_kv_append")
 
 
 def kv_attention_workspace_bytes(n_tok, n_heads, batch, cache):
@@ -550,13 +564,13 @@ def kv_attention_workspace_bytes(n_tok, n_heads, batch, cache):
 
 def kv_attention(Q, n_heads, batch, cache, p, Out, scale=0.0, workspace=None):
     """Causal attention of the new rows Q [n_tok, n_heads * head_dim] over the cache, their own tokens among it."""
-    _kv_tensors(p, batch, cache, Q, Out, ("Q", "Out"))
-    n, width = Q.size(0), Q.size(1)
-    _shape(Out.size(0) == n and Out.size(1) == width == n_heads * cache.head_dim, "Q, Out: [n_tok, n_heads * head_dim]")
+    here = _kv_tensors(p, batch, cache, Q, Out, ("Q", "Out"))
+    n, width = _size(Q, "Q")
+    _shape(Out.shape == (n, width) and width == n_heads * cache.head_dim, "Q, Out: [n_tok, n_heads * head_dim]")
     ws = workspace if workspace is not None else _ws(kv_attention_workspace_bytes(n, n_heads, batch, cache), Q)
-    _shape(ws.get_device() == Q.get_device(), "workspace: not on the current device")
+    _shape(ws.get_device() == here, "workspace: not on the current device")
     _check(lib().tlq_kv_attention(Q.data_ptr(), _rows(Q, "Q"), n, n_heads, scale, C.byref(batch), C.byref(cache), C.byref(p),
-                                  Out.data_ptr(), _rows(Out, "Out"), ws.data_ptr(), ws.numel(), _stream()), "tlq_kv_attention")
+                                  Out.data_ptr(), _rows(Out, "Out"), ws.data_ptr(), ws.numel(), _stream_of(here)), "tlq_kv_attention")
     return Out
 
 
