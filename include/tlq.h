@@ -339,8 +339,8 @@ tlq_status tlq_residual_add(const void* H, int64_t ldh, const void* Z, int64_t l
  *   code = clip(rint(xt / step_r), -2^(bits-1), 2^(bits-1) - 1).
  * X [n, c] x_dtype; factor: float [c], 16-byte aligned, or NULL (ones) - the searched scales for weight rows, their
  * reciprocals for tokens; bits 2..8; codes: out int8 [n, ldc], ldc (bytes) a multiple of 16 and at least c rounded up
- * to 128 (zeros are written behind c up to there, nothing beyond); 16-byte aligned; steps: out float [n].  A NaN has the lowest code and no
- * part in the step; an infinity makes the step infinite. */
+ * to 128 (zeros are written behind c up to there, nothing beyond); 16-byte aligned; steps: out float [n].  A NaN has the
+ * lowest code and no part in the step; an infinity makes the step infinite. */
 tlq_status tlq_row_codes(const void* X, int64_t n, int64_t c, int64_t ldx, const float* factor, int32_t bits,
                          const tlq_params* p, int8_t* codes, int64_t ldc, float* steps, void* stream);
 /* tlq_linear_i8: Y[t,o] = step_t * w_step[o] * sum_c code[t,c] * w_codes[o,c], with the codes and steps that
@@ -359,8 +359,8 @@ tlq_status tlq_linear_i8(const void* X, int64_t n_tok, int64_t c_in, int64_t ldx
  * d >= rot is not rotated.  Float arithmetic, one rounding to x_dtype at the end.
  * Q [n_tok, n_heads * head_dim], K [n_tok, n_kv_heads * head_dim] x_dtype, n_tok < 2^26, 16-byte aligned, strides multiples of 8
  * (both may be column slices of one matrix); head_dim 64, 128 or 256 (TLQ_ERR_UNSUPPORTED otherwise); rot a multiple
- * of 16, 0 <= rot <= head_dim; eps >= 0 (with 0 a head of zeros gives NaN); pos int32 [n_tok] (any sign), inv_freq double [rot/2]; wq, wk float [head_dim], 16-byte
- * aligned, or NULL (ones; both have to be NULL without norm).  Q_out may be Q with the same stride, K_out likewise K; no
+ * of 16, 0 <= rot <= head_dim; eps >= 0 (with 0 a head of zeros gives NaN); pos int32 [n_tok] (any sign), inv_freq
+ * double [rot/2]; wq, wk float [head_dim], 16-byte aligned, or NULL (ones; both have to be NULL without norm).  Q_out may be Q with the same stride, K_out likewise K; no
  * other overlap. */
 tlq_status tlq_qk_norm_rope(const void* Q, int64_t ldq, int32_t n_heads, const void* K, int64_t ldk, int32_t n_kv_heads,
                             int64_t n_tok, int32_t head_dim, int32_t rot, int32_t interleaved, int32_t norm, float eps,

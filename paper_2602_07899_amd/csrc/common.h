@@ -259,7 +259,8 @@ hipError_t launch_rmsnorm_mul(const void* Z, int64_t ldz, const void* Zb, int64_
                               int64_t c, bool bf16, const float* m_a, const float* m_b, int period,
                               int split, void* out, int64_t ldo, hipStream_t stream);
 
-// products of tokens' codes with stored codes: few tokens (linear.hip, up to 64), up to kLinearMidTokens (there, too), any (launch_gemm_store).  K = row length in codes, a multiple of 128
+// products of tokens' codes with stored codes: few tokens or outputs (linear.hip), up to kLinearMidTokens (there, too), any
+// (launch_gemm_store).  K = row length in codes, a multiple of 128
 struct LinearI8Args {
   const int8_t* xc; int64_t n_tok, ldx; const float* xs;    // token codes and steps
   const int8_t* wc; int64_t c_out, ldw, K; const float* ws;

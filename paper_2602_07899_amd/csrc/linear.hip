@@ -22,7 +22,8 @@ __device__ __forceinline__ void write4(const LinearI8Args& a, int64_t t, int64_t
 // any order).  16x16x64 MFMA with the weights as rows: a lane holds 16 codes of output lane % 16 (32 neighbouring ones in two
 // products, so that four lanes read a whole line), which it reads from memory as they are; nothing passes through LDS
 // before the sums.
-// Bound by the bytes of the weights: every one is read once per 16 NT tokens.
+// Bound by the bytes of the weights, every one is read once per 16 NT tokens, and by latency where they are few: 1 x 4096 x 4096
+// 5.4 us, 3.1 TB/s.
 template <int NT, int NW>
 __global__ __launch_bounds__(NW * 64) void linear_few_kernel(LinearI8Args a) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -92,7 +93,9 @@ hipError_t launch_linear_few(const LinearI8Args& a, hipStream_t stream) {
 // memory to registers, 512 codes ahead.  Waves 0 - 3 and 4 - 7 have the same four groups of 32 outputs and every second 128
 // codes.  Sums of one part are whole numbers; with several parts they go to the workspace and linear_join_kernel adds them.
 // Reading the tokens' codes from memory in every wave, as above, costs as much as the weights for each 16 tokens (see
-// linear_kind for both sides).
+// linear_kind for both sides).  48 x 11008 x 4096 13.9 us, 3.2 TB/s of weights (weights that are in the caches take 13: two and
+// a half stages a block, so the first loads and the meeting count), and 4.0 for the sums of eight parts.  Weights two stages
+// ahead instead of one: calls of 48 x 11008 x 4096 23.1 25.4, 64 x 4096 x 11008 24.3 26.6.
 constexpr int kMidStage = 512;
 template <int NT>
 __global__ __launch_bounds__(512) void linear_mid_kernel(LinearI8Args a, int splits, int* __restrict__ partial) {
@@ -221,13 +224,17 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinearI8Args a, int sp
 //   16 x 5120 x 13824   30.5 26.5 31.6     64 x 11008 x 4096  34.6 24.9 54.4     128 x 4096 x 11008   -  32.4 28.3
 //   32 x 4096 x 4096    12.0 15.3 22.1     64 x 4096 x 11008  39.0 23.6 26.8     256 x 4096 x 4096    -  24.9 24.1
 //   32 x 4096 x 11008   26.0 21.4 24.9     64 x 5120 x 13824  64.1 30.7 38.3     256 x 11008 x 4096   -  43.4 58.6
-//   16 x 1096 x 1399     6.2 10.0 11.2     300 x 1096 x 1399   -   15.1 15.1     256 x 4096 x 11008   -  48.0 29.5
-// Up to 64 tokens the few kernel's bytes decide, the weights once for each 16 tokens; beyond, whether the tiles of 128 x 128
-// are so few that most CUs have none, and their contraction long.
+//   16 x 1096 x 1399     6.2 10.0 11.2     300 x 1096 x 1399  12.5 15.1 15.1     256 x 4096 x 11008   -  48.0 29.5
+// Up to 64 tokens the few kernel's bytes decide, the weights once for each 16 tokens; beyond, whether its blocks run in one round
+// and are short, then whether the tiles of 128 x 128 are so few that most CUs have none, and their contraction long.  Few
+// and the better of the others: 128 x 1096 x 1399 8.3 14.8, 128 x 2048 x 2048 10.7 14.5, 300 x 1096 x 1399 12.5 15.0, 300 x 2048 x
+// 1399 16.7 19.1, 1000 x 128 x 500 8.7 10.3, 400 x 1096 x 1000 13.2 14.2, 128 x 2048 x 4096 (512 blocks) 16.8 16.9, 4000 x 2048 x 128
+// (504) 25.2 23.2, 613 x 1096 x 1399 (880) 21.4 15.8, 96 x 3000 x 4000 19.9 18.4, 100 x 8192 x 1024 25.4 19.7.
 // (Codes and product of up to four tokens in one launch, every block making the codes for itself: 1 x 4096 x 4096 9.0 -> 12.9,
 // 1 x 11008 x 4096 16.1 -> 18.6.)
 LinearKind linear_kind(int64_t n_tok, int64_t c_out, int64_t K) {
   if (n_tok <= 64) return (double)ceil_div(n_tok, 16) * (double)c_out * (double)K <= 70e6 ? kLinearFew : kLinearMid;
+  if (K <= 2048 && ceil_div(n_tok, 64) * ceil_div(c_out, 16) <= 448) return kLinearFew;
   return n_tok <= kLinearMidTokens && ceil_div(n_tok, 128) * ceil_div(c_out, 128) <= 64 && K >= 2048 ? kLinearMid : kLinearTiles;
 }
 

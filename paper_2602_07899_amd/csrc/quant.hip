@@ -771,8 +771,8 @@ hipError_t launch_row_codes(const void* X, int64_t n, int64_t c_in, int64_t ldx,
     kern<<<(unsigned)(waves == 1 ? ceil_div(n, 4) : n), (waves == 1 ? 256 : waves * 64), 0, stream>>>(
         (const uint16_t*)X, n, c_in, ldx, factor, qa, steps, codes, ldc);
   };
-  // (us eight waves a row and four: 1 x 5120 3.5 3.7, 1024 x 5120 8.3 7.3, 10,240 x 4104 50 36, x 5120 54 42, x 8192 68 61: 3.7 - 4.1
-  // TB/s; one wave: 40,960 x 1024 28)
+  // (bound by latency for few rows, 1 x 4096 3.0 us, by bytes for many.  us eight waves a row and four: 1 x 5120 3.5 3.7, 1024 x
+  // 5120 8.3 7.3, 10,240 x 4104 50 36, x 5120 54 42, x 8192 68 61: 3.7 - 4.1 TB/s; one wave: 40,960 x 1024 28)
   auto pick = [&](auto t) {
     using T = decltype(t);
     if (c_in <= 1024) go(row_codes_kernel<T, 1, 2>, 1);

@@ -83,6 +83,20 @@ def test_row_codes_zeros_behind_infinite_factors(gpu):
     assert bool((codes[:, 136:] == 0).all())
 
 
+def test_row_codes_of_more_rows_than_a_launch_has_blocks(gpu):
+    """Four million rows at once are those of their halves."""
+    import torch
+    n, p = (1 << 22) + 9, tlq.params()
+    X = torch.randn((n, 8), device=gpu).half()
+    f = torch.rand(8, device=gpu) + 0.5
+    codes, steps = torch.empty((n, 128), dtype=torch.int8, device=gpu), torch.empty(n, device=gpu)
+    tlq.row_codes(X, 8, p, codes, steps, factor=f)
+    c, s = torch.empty((n // 2 + 1, 128), dtype=torch.int8, device=gpu), torch.empty(n // 2 + 1, device=gpu)
+    for r0 in (0, n - n // 2 - 1):
+        tlq.row_codes(X[r0:r0 + n // 2 + 1], 8, p, c, s, factor=f)
+        assert torch.equal(codes[r0:r0 + n // 2 + 1], c) and torch.equal(steps[r0:r0 + n // 2 + 1], s)
+
+
 def test_row_codes_of_weights_are_the_channel_quantiser(gpu):
     """The codes are those of fake_quant with symmetric rows."""
     import torch
@@ -124,7 +138,9 @@ def _padded(wc, gpu, extra=0):
     (1, 13824, 24, 8), (3, 11008, 70, 2), (257, 512, 257, 8),
     # tokens shared through LDS: parts of the row of codes and one part, odd numbers of 128 codes, ragged outputs and tokens
     (16, 8200, 9001, 8), (17, 4104, 9001, 8), (40, 2568, 13000, 6), (64, 1096, 20001, 8), (65, 2048, 130, 8), (130, 4104, 1003, 8),
-    (256, 2056, 129, 4), (33, 136, 70001, 8)])
+    (256, 2056, 129, 4), (33, 136, 70001, 8),
+    # beyond 64 tokens: few outputs, a long row of codes, tiles
+    (448, 136, 1009, 8), (65, 2176, 130, 8), (300, 4104, 263, 8), (520, 1096, 1399, 6), (1000, 72, 1003, 8)])
 def test_linear_i8(gpu, dt, out, n, ci, co, bits):
     import torch
     g = np.random.default_rng([23, n, ci, co])
