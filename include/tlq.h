@@ -413,7 +413,8 @@ tlq_status tlq_kv_append(const void* K, int64_t ldk, const void* V, int64_t ldv,
  * probabilities times the page's step in fp16, which the softmax's sum takes as well; Out is rounded to x_dtype.  Steps have to
  * be positive, and scores below 2^21 in size (beyond, a float holds them to a quarter at best); other rows are undefined.
  * Q, Out [n_tok, n_heads * head_dim] x_dtype, 16-byte aligned, strides multiples of 8; n_heads a multiple of n_kv_heads;
- * n_tok * (n_heads / n_kv_heads) and n_seq * n_kv_heads below 2^31 - 256, max_new * (n_heads / n_kv_heads) below 2^28.
+ * n_tok * (n_heads / n_kv_heads) and n_seq * n_kv_heads below 2^31 - 256, max_new * (n_heads / n_kv_heads) below 2^28,
+ * that over 128 (rounded up) times n_seq * n_kv_heads below 2^30.
  * The workspace query reads sizes only, no pointer; the result does not depend on the workspace's contents. */
 size_t tlq_kv_attention_workspace_bytes(int64_t n_tok, int32_t n_heads, const tlq_kv_batch* b, const tlq_kv_cache* c);
 tlq_status tlq_kv_attention(const void* Q, int64_t ldq, int64_t n_tok, int32_t n_heads, float scale, const tlq_kv_batch* b,

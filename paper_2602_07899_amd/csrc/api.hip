@@ -969,7 +969,8 @@ tlq_status tlq_kv_append(const void* K, int64_t ldk, const void* V, int64_t ldv,
 static tlq_status check_kv_heads(int64_t n_tok, int32_t n_heads, const tlq_kv_batch* b, const tlq_kv_cache* c) {
   if (n_tok <= 0 || n_tok >= (1LL << 31) || n_heads <= 0 || n_heads > 65535 || (n_heads % c->n_kv_heads) != 0 ||
       n_tok * (n_heads / c->n_kv_heads) >= (1LL << 31) - 256 ||      // (rows are counted in 32 bits; a launch has 2^24 blocks)
-      (b->max_new < n_tok ? b->max_new : n_tok) * (n_heads / c->n_kv_heads) >= (1LL << 28))
+      (b->max_new < n_tok ? b->max_new : n_tok) * (n_heads / c->n_kv_heads) >= (1LL << 28) ||
+      ceil_div((b->max_new < n_tok ? b->max_new : n_tok) * (n_heads / c->n_kv_heads), 128) * b->n_seq * c->n_kv_heads >= (1LL << 30))
     return TLQ_ERR_SHAPE;
   return TLQ_OK;
 }

@@ -40,7 +40,8 @@ struct KvAttnDev {
   tlq_kv_batch b; tlq_kv_cache c; int page_bits;
   uint16_t* Out; int64_t ldo;
   int n_splits, chunk;          // keys of a split
-  int tiles; unsigned way_bits, member_bits, n_pairs; KvDiv by_heads;      // kv_prompt_kernel: row tiles, and the order of its blocks
+  // kv_prompt_kernel: row tiles; pairs of sequence and key head, blocks of a pair, and of the pairs that an XCD has to itself
+  int tiles; uint32_t n_pairs, own_blocks, together_bits; KvDiv by_heads, by_work;
   float2* ml; float* acc;       // per (row, head, split): reference and sum; [head_dim] sums of codes
 };
 
@@ -140,7 +141,7 @@ __device__ __forceinline__ float load_queries(const uint16_t* p, f16x8 (&qf)[N],
 // The 16 rows of a tile (a query and head each: the heads that share a key head are rows side by side) against one split of
 // the keys.  Four waves take 64 keys each in turn and meet in LDS at the end; keys and values go from memory to registers,
 // where they are widened: no LDS, no barrier in the loop, the next 64 keys in flight while these are worked on.
-// For few rows, bound by the bytes of the cache: 64 sequences of 4096 - 8192 tokens x 8 key heads of 128, four queries each,
+// For few rows (see kFewWork), bound by the bytes of the cache: 64 sequences of 4096 - 8192 tokens x 8 key heads of 128, four queries each,
 // 157 us, 5.1 TB/s of codes (a large copy reaches 5.06); one of 131,072 x 4 27 us, 5.0 TB/s; one of 1200 x 32 6.8 us, latency.
 template <typename T, int DH>
 __global__ __launch_bounds__(256, 3) void kv_few_kernel(KvAttnDev a) {
@@ -312,7 +313,7 @@ __global__ __launch_bounds__(256, 3) void kv_few_kernel(KvAttnDev a) {
 // 4 of 2400 297 us, 9600 tokens x 40 heads 1031 us, 916 TFLOP/s; a library product of halves reaches 1130.
 // Not kept, us before and with it for the first: 256 rows with eight waves 427 457, staging held in registers by hand no gain;
 // P through LDS is not needed, S^T's columns are P^T's.
-// All row tiles of a sequence and key head run on one XCD, as many of those together as fill it, the longest tiles first.
+// All row tiles of a sequence and key head run on one XCD, the longest first, as far as the pairs can be dealt out evenly.
 template <typename T, int DH>
 __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -322,12 +323,29 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
   __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * STAGE];
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, fq = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // blockIdx.x = ways * (members * (split, tile) + member) + pair
-  const unsigned pair = blockIdx.x & ((1u << a.way_bits) - 1), rest = blockIdx.x >> a.way_bits;
-  const unsigned which = rest >> a.member_bits, member = rest & ((1u << a.member_bits) - 1);
-  const unsigned sh = ((((blockIdx.z * gridDim.y + blockIdx.y) << a.member_bits) + member) << a.way_bits) + pair;
-  if (sh >= a.n_pairs) return;
-  const unsigned turn = a.n_splits == 1 ? which : which / (unsigned)a.n_splits;
+  // block 8 j + x runs on XCD x.  It has pair x of each eight: 2^together_bits such pairs at a time, then those that are left of
+  // them, the longest tiles of all first.  The pairs that are no eight come last, their blocks one XCD after the other.
+  const uint32_t block = blockIdx.y * gridDim.x + blockIdx.x, x = block & 7;
+  uint32_t j = block >> 3, sh, which;
+  if (j < a.own_blocks) {
+    const uint32_t own = a.n_pairs >> 3, full = own >> a.together_bits << a.together_bits;
+    if (j < full * a.by_work.d) {
+      const uint32_t g = a.by_work.of(j >> a.together_bits);
+      which = (j >> a.together_bits) - g * a.by_work.d;
+      sh = ((g << a.together_bits) + (j & ((1u << a.together_bits) - 1))) * 8 + x;
+    } else {
+      j -= full * a.by_work.d;
+      which = j / (own - full);
+      sh = (full + j - which * (own - full)) * 8 + x;
+    }
+  } else {
+    j = (j - a.own_blocks) * 8 + x;
+    const uint32_t g = a.by_work.of(j);
+    which = j - g * a.by_work.d;
+    sh = (a.n_pairs & ~7u) + g;
+    if (sh >= a.n_pairs) return;
+  }
+  const uint32_t turn = a.n_splits == 1 ? which : which / (uint32_t)a.n_splits;
   const int tile = a.tiles - 1 - (int)turn, split = (int)(which - turn * a.n_splits);
   const int s = (int)a.by_heads.of(sh), hk = (int)(sh - s * a.by_heads.d);
   const int k0 = split * a.chunk;
@@ -683,9 +701,14 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnDev a, uint32_t tile
 #endif
 }
 
-// Rows of a sequence and key head up to which they go in one tile of 16: beyond, the keys are read again for each 16 rows and
-// the tile of 128, though mostly empty, is as fast (2048 keys, us 16 and 128: 16 rows 57 70, 24 69 71, 32 71 71, 48 95 86, 64 128 86).
-constexpr int64_t kFewRows = 16;
+// Tiles of 16 rows times pairs of sequence and key head times 256 keys up to which the few kernel is taken, also for more than 16
+// rows: it has eight times as many, shorter blocks, which decides until they fill the chip several times; then reading the
+// keys again for each 16 rows does.  us few and prompt, by that number (heads of 128): 32 rows x 16 pairs x 5000 keys (640) 19
+// 27, x 64 x 2000 (1024) 22 28, x 64 x 5000 (2560) 36 34; 56 x 6 x 5000 (480) 15 28, x 16 x 5000 (1280) 23 29, x 64 x 2000 (2048) 26 31,
+// x 16 x 16,000 (4032) 48 41; 128 x 1 x 16,000 (504) 18 30, x 16 x 2000 (1024) 22 30, x 16 x 5000 (2560) 36 33; 256 x 4 x 5000 (1280)
+// 22 30, x 64 x 500 (2048) 22 20; whole prompts 300 x 8 pairs (304) 13.1 13.4, 600 x 4 (456) 14 21, 1000 x 1 (252) 11 30, 2400 x 1 (1500) 24
+// 30, 100 x 32 with four rows a token (800) 11.9 11.0.
+constexpr int64_t kFewWork = 1536;
 
 namespace {
 struct KvPlan { bool prompt; int rows, tiles, n_splits, chunk; size_t acc_at, bytes; };
@@ -693,20 +716,33 @@ KvPlan kv_plan(int64_t n_tok, int n_heads, const tlq_kv_batch& b, const tlq_kv_c
   KvPlan p;
   const int group = n_heads / c.n_kv_heads;
   const int64_t most = b.max_new < n_tok ? b.max_new : n_tok;
-  p.prompt = most * group > kFewRows;
+  const int64_t room = (int64_t)b.max_pages * c.page, keys = b.max_len < room ? b.max_len : room;
+  p.prompt = most * group > 16 && ceil_div(most * group, 16) * c.n_kv_heads * b.n_seq * ceil_div(keys, 256) > kFewWork;
   p.rows = p.prompt ? 128 : 16;
   p.tiles = (int)ceil_div(most * group, p.rows);
-  const int64_t room = (int64_t)b.max_pages * c.page, keys = b.max_len < room ? b.max_len : room;
   const int64_t base = (int64_t)p.tiles * c.n_kv_heads * b.n_seq;
-  // Split until there are about two blocks a CU, a part of 256 keys or, where many rows have sums to be joined, of 512 at
-  // least (us unsplit, for 256, 512 and 1024 blocks: single tokens, 131,072 keys x 4 key heads - 35 32 35, 8 x 4096 x 32 44 44 45
-  // 47, 32 x 1024 x 8 18 18 20 22, 64 x 8192 x 8 160 160 159 171; 64 tokens behind 16,320 x 4 477 50 44 44, 4 x 100 behind
-  // 3900 x 8 122 79 61 75, 4096 x 8 122 121 104 107; 600 x 8 in parts of 300 24 35).  Beyond two blocks a CU a second round of
-  // them and the joining cost more than their evenness gives.
-  const int64_t units = ceil_div(keys, 256), most_splits = p.prompt ? keys / 512 : units;
+  // Split until there are about two blocks a CU, into parts of 256 keys at least.  Beyond two blocks a CU a second round of them
+  // and the joining cost more than their evenness gives (us unsplit, for 256, 512 and 1024 blocks: single tokens, 131,072 keys x 4
+  // key heads - 35 32 35, 8 x 4096 x 32 44 44 45 47, 32 x 1024 x 8 18 18 20 22, 64 x 8192 x 8 160 160 159 171; 64 tokens behind
+  // 16,320 x 4 477 50 44 44, 4 x 100 behind 3900 x 8 122 79 61 75).
+  // With the tiles of 128 rows a split costs: for 64 keys 1.6 us, with two blocks a CU 2.2, and the joined sums' way to memory
+  // and back, at 4 TB/s behind another launch's 4 us.  The least by that, against parts of 512 and of 256 keys (us): 128 rows x 4
+  // pairs x 16,000 keys 33 28, 256 x 6 x 16,000 38 41, x 32 x 2000 37 32, 400 x 10 x 5000 44 38, 600-token prompts x 32 heads 22
+  // (unsplit) 36.
+  const int64_t units = ceil_div(keys, 256);
   int64_t splits = 511 / base;
-  if (splits > most_splits) splits = most_splits;
+  if (splits > units) splits = units;
   if (splits < 1) splits = 1;
+  if (p.prompt) {
+    double least = 0.0;
+    const int64_t most_splits = splits;
+    for (int64_t n = splits = 1; n <= most_splits; ++n) {
+      const int64_t part = ceil_div(units, n), parts = ceil_div(units, part);
+      const double joined = (double)n_tok * n_heads * (double)parts * c.head_dim * 8.0 / 4e6;
+      const double us = (double)part * 4.0 * (base * parts > 256 ? 2.2 : 1.6) + (parts > 1 ? 4.0 + joined : 0.0);
+      if (n == 1 || us < least) { least = us; splits = n; }
+    }
+  }
   p.chunk = (int)(ceil_div(units, splits) * 256);
   p.n_splits = (int)ceil_div(keys, p.chunk);
   p.acc_at = align_up((size_t)n_tok * n_heads * p.n_splits * sizeof(float2), 256);
@@ -732,19 +768,20 @@ hipError_t launch_kv_attention(const void* Q, int64_t ldq, int64_t n_tok, int n_
   a.tiles = p.tiles;
   a.by_group = kv_div((uint32_t)a.group);
   a.by_heads = kv_div((uint32_t)c.n_kv_heads);
-  const int64_t n_pairs = (int64_t)b.n_seq * c.n_kv_heads;
-  a.n_pairs = (unsigned)n_pairs;
-  // (powers of two: up to eight pairs side by side, and up to eight of an XCD together)
-  for (a.way_bits = 0; a.way_bits < 3 && (2 << a.way_bits) <= n_pairs; ++a.way_bits) {}
-  const int64_t groups = ceil_div(n_pairs, 1 << a.way_bits);
-  // (an XCD has 64 blocks at a time: more pairs than fill them only push each other's keys out of its cache.  us with eight
-  // pairs always and by this rule: 2 x 4800 x 40 heads 600 547, 9600 x 40 1452 1031, 16 x 1200 x 40 389 391)
-  for (a.member_bits = 0; a.member_bits < 3 && (2 << a.member_bits) <= groups && ((int64_t)p.tiles * p.n_splits << a.member_bits) < 64;
-       ++a.member_bits) {}
-  const int64_t chunks = ceil_div(groups, 1 << a.member_bits), gy = chunks < 32768 ? chunks : 32768;
-  const int64_t work = (int64_t)p.tiles * p.n_splits, gx = p.prompt ? work << (a.way_bits + a.member_bits) : work;
-  const dim3 grid = p.prompt ? dim3((unsigned)gx, (unsigned)gy, (unsigned)ceil_div(chunks, gy))
-                             : dim3((unsigned)gx, (unsigned)c.n_kv_heads, (unsigned)b.n_seq);
+  const int64_t n_pairs = (int64_t)b.n_seq * c.n_kv_heads, work = (int64_t)p.tiles * p.n_splits;
+  a.n_pairs = (uint32_t)n_pairs;
+  a.by_work = kv_div((uint32_t)work);
+  a.own_blocks = (uint32_t)(n_pairs / 8 * work);
+  // (an XCD has 64 blocks at a time: more pairs than fill them only push each other's keys out of its cache, fewer leave the
+  // longest tiles of the last to the end.  us with eight pairs always and by this rule: 2 x 4800 x 40 heads 600 547, 9600 x 40 1452
+  // 1031; one pair always and by this rule: 16 x 1200 x 40 398 377, 4 x 2400 x 40 359 346.  Pairs that are no eight, all on XCDs of
+  // their own and dealt out: 9600 x 9 heads with two rows a token 740 585, 256 tokens of two rows behind 15,744 x 9 112 68,
+  // 1200 x 25 56 58)
+  for (a.together_bits = 0; a.together_bits < 3 && (16 << a.together_bits) <= n_pairs && work << a.together_bits < 64; ++a.together_bits) {}
+  const int64_t blocks = 8 * ((int64_t)a.own_blocks + ceil_div(n_pairs % 8 * work, 8));
+  const int64_t gx = blocks < (1 << 20) ? blocks : (1 << 20);
+  const dim3 grid = p.prompt ? dim3((unsigned)gx, (unsigned)ceil_div(blocks, gx))
+                             : dim3((unsigned)work, (unsigned)c.n_kv_heads, (unsigned)b.n_seq);
   auto pick = [&](auto t, auto dh) {
     using T = decltype(t);
     constexpr int DH = decltype(dh)::value;

@@ -104,6 +104,7 @@ def test_cache_refusals():
     # more blocks than a launch can have
     assert append(n=1 << 30, n_seq=1000, max_new=1 << 20, max_len=1 << 20, page=16) == tlq.ERR_SHAPE
     assert attend(n=1 << 28, heads=4, max_new=1 << 28, max_len=1 << 28, n_kv_heads=4, ldq=512) == tlq.ERR_SHAPE
+    assert attend(n=1 << 21, heads=2, max_new=1 << 21, max_len=1 << 21, n_seq=65535, n_kv_heads=2, ldq=256, ldo=256) == tlq.ERR_SHAPE
     assert attend(scale=float("nan")) == attend(scale=float("inf")) == tlq.ERR_UNSUPPORTED
     assert attend(Q=ODD) == attend(Out=ODD) == attend(ldq=516) == attend(ldo=516) == tlq.ERR_ALIGN
     long = dict(max_len=100000, max_pages=2000, ld_table=2000, n=3)

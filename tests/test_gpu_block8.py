@@ -345,6 +345,21 @@ def _attend(gpu, c, heads, dt, q, scale=0.0, rows=None, poison=True):
     return got[:, 8:8 + q.shape[1]]
 
 
+def _bounds(c, heads, q, kind):
+    """Host's bounds under which the tiles of 128 rows are taken (they need work for many blocks): rows behind the last sequence
+    ("tiles"), or, for more than 16 rows, longer sequences than there are ("parts": many parts, most of them empty)."""
+    group, pairs = heads // c.kv, len(c.lens) * c.kv
+    if kind == "tiles":
+        q = np.concatenate([q, np.full((1540 * 16 // (group * pairs) + 16, q.shape[1]), np.nan)])
+        c.max_new = q.shape[0]
+        c.max_len = max(c.max_len, c.max_new)
+    if kind == "parts":
+        units = 1540 // (max(-(-c.max_new * group // 16), 1) * pairs) + 1
+        c.max_len = max(c.max_len, units * 256)
+        c.table = np.concatenate([c.table, np.full((len(c.lens), max(0, -(-c.max_len // c.page) - c.table.shape[1])), -1, np.int32)], 1)
+    return q
+
+
 def _check_attention(gpu, c, heads, dt, q, scale=0.0):
     got = _attend(gpu, c, heads, dt, q, scale)
     want, mag, sens = ob.kv_attention(q, heads, c.kc, c.ks, c.vc, c.vs, c.cu, c.lens, c.table, c.max_len, scale or None)
@@ -357,7 +372,7 @@ def _check_attention(gpu, c, heads, dt, q, scale=0.0):
     # weights in 16 bits, above the line and below it: sum_j p_j e_j (v_j - out), |e_j| <= 2^-11, at most 2^-11 (mag + |out|);
     # those below 2^-21 of the largest to 2^-32 of it; scores as sums of dh products (a relative error of e^(2 ds) in p and in
     # the sum of p), sums over the keys in 32 bits, the output
-    n = c.max_len
+    n = min(c.max_len, max(c.lens))
     ds = ((c.dh + 6) * sens + 64) * U
     bound = (mag + np.abs(want)) * 2.0 ** -11 + mag * (2.1 * ds + (n / 4 + 64) * U) + n * 2.0 ** -32 * 127 * c.vs.max() + np.abs(want) * HALF[dt] * 1.001 + TINY[dt] * 1.01
     within(got, want, bound)
@@ -378,17 +393,19 @@ ATTENTION = [   # lens, new, kv heads, group, dh, page
 
 
 @pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("kind", ["", "tiles", "parts"])
 @pytest.mark.parametrize("lens,new,kv,group,dh,page", ATTENTION)
-def test_kv_attention(gpu, dt, lens, new, kv, group, dh, page):
+def test_kv_attention(gpu, dt, kind, lens, new, kv, group, dh, page):
     g = np.random.default_rng([51, sum(lens), group, dh])
     c = Pool(g, gpu, lens, new, kv, dh, page, dt)
     q = rnd(1.5 * g.standard_normal((c.rows + 2, kv * group * dh)), dt)
     q[c.rows:] = np.nan
-    _check_attention(gpu, c, kv * group, dt, q)
+    _check_attention(gpu, c, kv * group, dt, _bounds(c, kv * group, q, kind))
 
 
+@pytest.mark.parametrize("kind", ["", "tiles", "parts"])
 @pytest.mark.parametrize("dt", ["f16", "bf16"])
-def test_kv_attention_of_wild_steps_and_loud_queries(gpu, dt):
+def test_kv_attention_of_wild_steps_and_loud_queries(gpu, dt, kind):
     """Pages whose steps lie five orders of magnitude apart; queries of very different size, zeros among them; scores large
     enough that one key has nearly all of the weight; a scale of the caller's."""
     g = np.random.default_rng(52)
@@ -397,13 +414,15 @@ def test_kv_attention_of_wild_steps_and_loud_queries(gpu, dt):
     q[2] = 0.0
     if dt == "bf16":
         q[3] = rnd(q[3] * 2.0 ** -100, dt)
+    q = _bounds(c, 4, q, kind)
     _check_attention(gpu, c, 4, dt, q)
     _check_attention(gpu, c, 4, dt, q, scale=-0.31)
     c.ks[:] *= 20
     _check_attention(gpu, c, 4, dt, q)
 
 
-def test_kv_attention_of_pages_that_are_not_there(gpu):
+@pytest.mark.parametrize("kind", ["", "tiles", "parts"])
+def test_kv_attention_of_pages_that_are_not_there(gpu, kind):
     """Entries outside the pool stand for tokens that do not exist, wherever they are; a row that sees none gives zeros; steps and
     codes of pages that no sequence names are never used."""
     g = np.random.default_rng(53)
@@ -413,13 +432,15 @@ def test_kv_attention_of_pages_that_are_not_there(gpu):
         named = {int(i) for i in c.table.ravel() if 0 <= i < c.n}
         for i in set(range(c.n)) - named:
             c.ks[i], c.vs[i] = np.nan, np.inf
-        q = rnd(g.standard_normal((c.rows, 4 * 128)), dt)
+        q = _bounds(c, 4, rnd(g.standard_normal((c.rows, 4 * 128)), dt), kind)
         keep = c.vs.copy()
         c.vs[~np.isfinite(c.vs)] = 0.0                        # (the bound takes the largest step; put back below)
         top = c.vs.max()
         c.vs = keep
         got = _attend(gpu, c, 4, dt, q)
+        assert (got[c.rows:] == 3.0).all()
         want, mag, sens = ob.kv_attention(q, 4, c.kc, c.ks, c.vc, c.vs, c.cu, c.lens, c.table, c.max_len)
+        got, want, mag, sens = (t[:c.rows] for t in (got, want, mag, sens))
         ds = ((128 + 6) * np.repeat(sens, 128, 1) + 64) * U
         within(got, want, (mag + np.abs(want)) * 2.0 ** -11 + mag * (2.1 * ds + 200 * U) + 200 * 2.0 ** -32 * 127 * top + np.abs(want) * HALF[dt] * 1.001 + TINY[dt] * 1.01)
         assert (want == 0).all(axis=1).any()
@@ -521,8 +542,8 @@ def test_kv_attention_of_a_long_sequence(gpu):
     _check_attention(gpu, c, 2, "f16", np.ones((1, 128), np.float32))
 
 
-@pytest.mark.parametrize("new", [1, 20])
-def test_kv_attention_of_many_keys_far_below_one(gpu, new):
+@pytest.mark.parametrize("new,kind", [(1, ""), (20, ""), (20, "tiles"), (20, "parts")])
+def test_kv_attention_of_many_keys_far_below_one(gpu, new, kind):
     """One key 2^22 times as heavy as each of 40,000 others, whose weights are no normal halves: together one percent of the sum,
     in the numerator and in the denominator alike."""
     g = np.random.default_rng(57)
@@ -534,7 +555,7 @@ def test_kv_attention_of_many_keys_far_below_one(gpu, new):
         c.vc[c.table[0, page], 0, :, 5] = 0                  # what is left is the others' alone
         c.vc[:] = np.abs(c.vc)
         c.vs[:] = np.float32(0.03)
-        got = _attend(gpu, c, 2, "f16", np.ones((new, 128), np.float32))
+        got = _attend(gpu, c, 2, "f16", _bounds(c, 2, np.ones((new, 128), np.float32), kind))[:new]
         want, mag, _ = ob.kv_attention(np.ones((new, 128)), 2, c.kc, c.ks, c.vc, c.vs, c.cu, c.lens, c.table, c.max_len)
         # weights of 2^-15 and 2^7, exact halves; the score to 2^-17 of itself, sums in 32 bits, a half of a small output
         within(got, want, want * (22 * 64 * U + 2.0 ** -11 * 1.01 + 40000 / 16 * U) + TINY["f16"])
@@ -555,8 +576,8 @@ def test_kv_attention_of_queries_near_the_types_largest(gpu):
 
 
 @pytest.mark.parametrize("dt", ["f16", "bf16"])
-@pytest.mark.parametrize("new", [1, 20, 150])
-def test_kv_attention_of_queries_that_are_not_finite(gpu, dt, new):
+@pytest.mark.parametrize("new,kind", [(1, ""), (20, ""), (20, "tiles"), (20, "parts"), (150, ""), (150, "tiles"), (150, "parts")])
+def test_kv_attention_of_queries_that_are_not_finite(gpu, dt, new, kind):
     """An infinity or a NaN anywhere in a query makes its head NaN, whichever sign the keys have there, and no other head; a row
     that sees no key gives zeros still.  Split and unsplit."""
     g = np.random.default_rng(59)
@@ -564,15 +585,15 @@ def test_kv_attention_of_queries_that_are_not_finite(gpu, dt, new):
         c = Pool(g, gpu, [length, 40], [new, 1], 2, 64, 32, dt)
         c.kc[:, 0] = np.abs(c.kc[:, 0])
         c.table[1, :] = -1
-        q = rnd(g.standard_normal((c.rows, 4 * 64)), dt)
+        q = _bounds(c, 4, rnd(g.standard_normal((c.rows, 4 * 64)), dt), kind)
         clean = _attend(gpu, c, 4, dt, q)
         bad = q.copy()
         bad[0, 3], bad[0, 64 * 2 + 50] = -np.inf, np.nan       # heads 0 and 2
         bad[new // 2, 64 + 63], bad[new // 2, 64 * 3] = np.inf, -np.inf
         bad[c.rows - 1, 0] = np.nan
         got = _attend(gpu, c, 4, dt, bad)
-        lost = np.repeat(~np.isfinite(bad).reshape(c.rows, 4, 64).all(2), 64, 1)
-        lost[c.rows - 1] = False
+        lost = np.repeat(~np.isfinite(bad).reshape(len(bad), 4, 64).all(2), 64, 1)
+        lost[c.rows - 1:] = False                              # (rows behind the last sequence stay as they were)
         assert np.isfinite(clean).all() and (clean[c.rows - 1] == 0.0).all()
         assert np.isnan(got[lost]).all() and np.array_equal(got[~lost], clean[~lost])
 
