@@ -496,6 +496,18 @@ def test_kv_tables_that_are_part_of_a_wider_one(gpu, lens, new):
         assert np.array_equal(got.cpu().numpy(), want)
 
 
+def test_kv_attention_of_very_many_sequences(gpu):
+    """More blocks than one row of a grid has here, nearly all of them of sequences without tokens."""
+    g = np.random.default_rng(62)
+    lens, new = np.zeros(65535, np.int64), np.zeros(65535, np.int64)
+    lens[[0, 40000, 65527, 65534]], new[[0, 40000, 65527, 65534]] = [70, 33, 20, 150], [70, 1, 20, 20]
+    c = Pool(g, gpu, lens.tolist(), new.tolist(), 1, 64, 16, "f16")
+    q = np.full((2300, 64), np.nan, np.float32)                # (18 tiles a sequence by the host's bound)
+    q[:c.rows] = rnd(g.standard_normal((c.rows, 64)), "f16")
+    c.max_new, c.max_len = 2300, 2300
+    _check_attention(gpu, c, 1, "f16", q)
+
+
 def test_kv_attention_of_more_splits_than_lanes(gpu):
     """Parts of 256 keys of one sequence, and of a short one beside it."""
     g = np.random.default_rng(61)
