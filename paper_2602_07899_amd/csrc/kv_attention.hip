@@ -9,7 +9,13 @@
 // is set, and is set again when a z lies 15 above it: weights stay between 2^15 and, as normal halves, 2^-21 of the largest
 // at least (with the largest at 1, 2^-14: over 10^5 keys what falls below would show), and sums are rescaled a few times a
 // row instead of at every new maximum.  The denominator sums the rounded weights, in 32 bits: where one key has nearly all
-// of the weight its rounding cancels.  Both products run on fp16 matrix instructions whatever x_dtype is: codes are exact in
+// of the weight its rounding cancels.  But a page whose step lies far below the others' has small weights 2^(z - m) whatever
+// its probabilities are, and in the denominator they are divided by that step: such halves would be subnormal or zero.  Where a
+// lane's page has a step below 2^-3 of those that the reference was set among, and the largest of the lane's 16 weights is
+// below 2^-7, it sums sum_j 2^(scale log2(e) ks (q . kcode_j) - m) from unrounded exponentials.  What the denominator can lose
+// otherwise, next to the roundings to 2^-12: 15 times 2^-25 beside a weight of 2^-7 at least (2^-14 of itself), and 2^-25 a key
+// at 2^3 times the reference's step and weight of 2^7, so 2^-29 a key (2^-12 over 131,072 keys, all of them below the
+// halves).  Both products run on fp16 matrix instructions whatever x_dtype is: codes are exact in
 // fp16; bf16 queries are multiplied with the power of two that brings the largest of the row to [2^14, 2^15).
 // The products are transposed, S^T = K Q^T and O^T = V^T P^T, so that a lane owns one query column and P stays in
 // registers; values are stored channel by channel so that V^T's rows are read as they lie.
@@ -54,8 +60,9 @@ __device__ __forceinline__ void static_for(Fn&& f) {
 }
 
 #if defined(__HIP_DEVICE_COMPILE__)
-constexpr float kSmallStep = 1e-30f;    // (a step of zero: its codes' page counts as zeros)
+constexpr float kSmallStep = 1e-30f;    // (a step of zero: its page's values count as zeros, its keys in the sum as ever)
 constexpr float kTop = 7.0f, kRaise = 15.0f;      // exponents of the largest weight: when the reference is set, at most
+constexpr float kNear = 3.0f, kLow = 7.0f;        // binary orders below the reference's step, below a weight of one (see above)
 // sum of eight weights (rounded already) and c
 __device__ __forceinline__ float add_weights(f16x8 w, float c) {
   const f16x2 one = {(_Float16)1.0f, (_Float16)1.0f};
@@ -86,6 +93,19 @@ __device__ __forceinline__ float column_max(float v) {
   return fmaxf(a, b);
 }
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+// A denominator times 2^d, d <= 0.  Steps of values may lie further apart than floats have exponents: where 2^d has none left the
+// denominator takes the way in two.  With f = 2^d at hand where a launch is a chain of few of them (1200 keys x 32 9.9 us, the other
+// form 10.0), without a branch between the products of prompts (16 of up to 1200 tokens 343 us, the other form 348).
+__device__ __forceinline__ float lower_sum(float l, float d, float f) {
+  const bool far = l != 0.0f && d < -100.0f;
+  float r = l * f;
+  if (__builtin_expect(__any(far), 0)) r = far ? l * 0x1p-100f * exp2_fast(d + 100.0f) : r;
+  return r;
+}
+__device__ __forceinline__ float lower_sum(float l, float d) {
+  const float c = fmaxf(d, -100.0f);
+  return l * exp2_fast(c) * exp2_fast(d - c);      // (the last is one down to there)
+}
 
 // A query with an infinity or NaN is not to end as a row without keys (all of its scores -inf, or none above the maximum so far):
 // a lane that holds such a number makes a NaN of it, and with it the products with every key.
@@ -174,6 +194,7 @@ __global__ __launch_bounds__(256, 3) void kv_few_kernel(KvAttnDev a) {
 #pragma unroll
   for (int d = 0; d < ND; ++d) acc[d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   float ref = -INFINITY, l_run = 0.0f;      // the row's reference, this lane's share of its sum
+  float quiet = -INFINITY;                  // kNear below the largest step (its logarithm) among the keys that set the reference
 
   uint4 kr[4][LW], vr[ND];
   float ks = 0.0f, vs = 1.0f;
@@ -240,19 +261,31 @@ __global__ __launch_bounds__(256, 3) void kv_few_kernel(KvAttnDev a) {
         sc[j][r] = 4 * j + r <= limit ? z : -INFINITY;
         mx = fmaxf(mx, sc[j][r]);
       }
+    const float own = mx;
     mx = column_max(mx);
-    if (mx > ref + kRaise) {
-      const float next = mx - kTop, alpha = exp2_fast(ref - next);       // (0 at the first visible key)
-      ref = next;
-      l_run *= alpha;
+    float per = rv;                       // of the rounded weights' sum, in the denominator
+    if (__any(mx > ref + kRaise || lg < quiet)) {
+      const float lg_top = column_max(seen ? lg : -INFINITY);
+      if (mx > ref + kRaise) {
+        const float next = mx - kTop, alpha = exp2_fast(ref - next);       // (0 at the first visible key)
+        l_run = lower_sum(l_run, ref - next, alpha);
+        ref = next;
+        quiet = lg_top - kNear;
 #pragma unroll
-      for (int d = 0; d < ND; ++d) acc[d] *= alpha;
+        for (int d = 0; d < ND; ++d) acc[d] *= alpha;
+      }
+      if (lg < quiet && own < ref - kLow) {
+        const float less = ref + lg;
+        per = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) l_run += exp2_fast(sc[e >> 2][e & 3] - less);
+      }
     }
     const float from = ref == -INFINITY ? 0.0f : ref;
     f16x8 pf[2];
 #pragma unroll
     for (int e = 0; e < 16; ++e) pf[e >> 3][e & 7] = (_Float16)exp2_fast(sc[e >> 2][e & 3] - from);
-    l_run = __builtin_fmaf(add_weights(pf[1], add_weights(pf[0], 0.0f)), rv, l_run);
+    l_run = __builtin_fmaf(add_weights(pf[1], add_weights(pf[0], 0.0f)), per, l_run);
 #pragma unroll
     for (int d = 0; d < ND; ++d) {
       acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen_codes8(vr[d].x, vr[d].y), pf[0], acc[d], 0, 0, 0);
@@ -279,7 +312,7 @@ __global__ __launch_bounds__(256, 3) void kv_few_kernel(KvAttnDev a) {
   for (int w = 0; w < 4; ++w) m = fmaxf(m, ml[w][r].x);
 #pragma unroll
   for (int w = 0; w < 4; ++w)
-    l += ml[w][r].y * (ml[w][r].x == -INFINITY ? 0.0f : exp2_fast(ml[w][r].x - m));      // (NaN stays)
+    l += lower_sum(ml[w][r].y, ml[w][r].x - m, ml[w][r].x == -INFINITY ? 0.0f : exp2_fast(ml[w][r].x - m));      // (NaN stays)
 #pragma unroll
   for (int e = 0; e < PER; ++e) o[e] = (part[0][r][d0 + e] + part[1][r][d0 + e]) + (part[2][r][d0 + e] + part[3][r][d0 + e]);
   const uint32_t oq = a.by_group.of(first_row + r);
@@ -315,7 +348,7 @@ __global__ __launch_bounds__(256, 3) void kv_few_kernel(KvAttnDev a) {
 // P through LDS is not needed, S^T's columns are P^T's.
 // All row tiles of a sequence and key head run on one XCD, the longest first, as far as the pairs can be dealt out evenly.
 template <typename T, int DH>
-__global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
+__global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kv_prompt_kernel(KvAttnDev a) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int NS = DH / 32, ND = DH / 16, CPK = DH / 8;   // k32 steps of a score, channel tiles, 16-byte chunks of a key
   constexpr int KB = DH * 2, VB = 128;                      // bytes of a row of K, of V^T in LDS
@@ -380,6 +413,7 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
 #pragma unroll
   for (int d = 0; d < ND; ++d) acc[d][0] = acc[d][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   float ref[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.0f, 0.0f};
+  float quiet = -INFINITY;                 // as in kv_few_kernel, the larger of the two columns'
 
   // what a thread moves: K rows tid / (CPK / 2) and further ones, 16 codes; V channels 16 wave + l16 and 64 further, the 16 keys
   // that it has the scores of.
@@ -515,25 +549,38 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
       }
     }
     const float lg = __builtin_amdgcn_logf(vst), rv = __builtin_amdgcn_rcpf(vst);
-    float f[2], mx[2];
+    float f[2], mx[2], own[2];
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
       f[n] = fmaxf(fac[n] * kst, 1e-37f);       // (zero times a masked product would not be -inf)
       mx[n] = sc[0][n][0];
 #pragma unroll
       for (int e = 1; e < 16; ++e) mx[n] = fmaxf(mx[n], sc[e >> 2][n][e & 3]);
-      mx[n] = column_max(mx[n] == -INFINITY ? mx[n] : __builtin_fmaf(mx[n], f[n], lg));
+      own[n] = mx[n] == -INFINITY ? mx[n] : __builtin_fmaf(mx[n], f[n], lg);
+      mx[n] = column_max(own[n]);
     }
-    if (__any(mx[0] > ref[0] + kRaise || mx[1] > ref[1] + kRaise)) {
+    float per = rv;
+    if (__any(mx[0] > ref[0] + kRaise || mx[1] > ref[1] + kRaise || lg < quiet)) {
+      const float lg_top = column_max(now_seen ? lg : -INFINITY);
 #pragma unroll
       for (int n = 0; n < 2; ++n)
         if (mx[n] > ref[n] + kRaise) {
           const float next = mx[n] - kTop, alpha = exp2_fast(ref[n] - next);
+          l_run[n] = lower_sum(l_run[n], ref[n] - next);
           ref[n] = next;
-          l_run[n] *= alpha;
+          quiet = fmaxf(quiet, lg_top - kNear);
 #pragma unroll
           for (int d = 0; d < ND; ++d) acc[d][n] *= alpha;
         }
+      if (lg < quiet && (own[0] < ref[0] - kLow || own[1] < ref[1] - kLow)) {
+        per = 0.0f;
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+          const float less = ref[n] != -INFINITY ? -ref[n] : 0.0f;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) l_run[n] += exp2_fast(__builtin_fmaf(sc[e >> 2][n][e & 3], f[n], less));
+        }
+      }
     }
     float off[2];
 #pragma unroll
@@ -563,7 +610,7 @@ __global__ __launch_bounds__(256, 2) void kv_prompt_kernel(KvAttnDev a) {
       __builtin_amdgcn_sched_barrier(0);
     });
 #pragma unroll
-    for (int n = 0; n < 2; ++n) l_run[n] = __builtin_fmaf(add_weights(pf[1][n], add_weights(pf[0][n], 0.0f)), rv, l_run[n]);
+    for (int n = 0; n < 2; ++n) l_run[n] = __builtin_fmaf(add_weights(pf[1][n], add_weights(pf[0][n], 0.0f)), per, l_run[n]);
   }
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
@@ -621,7 +668,7 @@ __global__ __launch_bounds__(256) void kv_join_few_kernel(KvAttnDev a, uint32_t 
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
   const float f = p.x == -INFINITY ? 0.0f : exp2_fast(p.x - m);
-  float l = p.y * f;
+  float l = lower_sum(p.y, p.x - m, f);
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) l += __shfl_xor(l, off, 64);
   vec o = {};
@@ -671,7 +718,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnDev a, uint32_t tile
   for (int k = 0; k < kMaxSplits / 256; ++k) {
     const float f = p[k].x == -INFINITY ? 0.0f : exp2_fast(p[k].x - m);
     if (k * 256 + tid < n) factor[k * 256 + tid] = f;
-    l += p[k].y * f;
+    l += lower_sum(p[k].y, p[k].x - m, f);
   }
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) l += __shfl_xor(l, off, 64);

@@ -555,6 +555,41 @@ def test_kv_attention_of_a_long_sequence(gpu):
 
 
 @pytest.mark.parametrize("new,kind", [(1, ""), (20, ""), (20, "tiles"), (20, "parts")])
+@pytest.mark.parametrize("dt,length,page,at,heavy,high,low", [
+    # one key of the page with values has half of the weight, zeros elsewhere (the step that an append gives them)
+    ("f16", 4096, 64, 0, True, 30 / 127, 1e-5 / 127), ("f16", 4096, 64, 40, True, 4 / 127, 1e-5 / 127),
+    # equal scores: a page of zeros, or all but one, beside pages with values up to the type's largest; few keys, and many
+    ("f16", 32, 16, 0, False, 1000 / 127, 1e-5 / 127), ("f16", 32, 16, 1, False, 16000 / 127, 1e-5 / 127),
+    ("f16", 200, 16, 5, False, 65504 / 127, 1e-5 / 127), ("bf16", 3000, 32, 90, False, 1e6, 1e-5 / 127),
+    ("bf16", 40000, 64, 0, True, 0.3, 1e-3 / 127), ("f16", 40000, 64, 600, True, 500.0, 1e-3 / 127),
+    # further apart than a float's exponents, in one part of the keys and in two; a step of zero
+    ("bf16", 200, 16, 0, False, 2.0 ** 118, 2.0 ** -60), ("bf16", 3000, 64, 45, False, 2.0 ** 118, 2.0 ** -60),
+    ("bf16", 3000, 64, 0, False, 2.0 ** 118, 2.0 ** -60), ("f16", 600, 64, 3, False, 0.02, 0.0)])
+def test_kv_attention_of_quiet_pages_beside_a_loud_one(gpu, new, kind, dt, length, page, at, heavy, high, low):
+    """Keys whose values have a step far below that of the loudest page count in the softmax's sum with all of their weight."""
+    g = np.random.default_rng([66, length, at])
+    c = Pool(g, gpu, [length + new - 1], [new], 1, 64, page, dt)
+    c.vs[:] = np.float32(low)
+    c.vs[c.table[0, at]] = np.float32(high)
+    c.vc[c.table[0, at]] = np.abs(c.vc[c.table[0, at]])      # (their mean is no zero)
+    if heavy:
+        c.kc[:] = 0
+        c.kc[c.table[0, at], 0, 5, :] = 127
+        c.ks[:] = np.float32(np.log(length) / (127 * 8))
+        q = np.ones((new, 128), np.float32)
+    else:
+        q = rnd(0.1 * g.standard_normal((new, 128)), dt)
+    got = _attend(gpu, c, 2, dt, _bounds(c, 2, q, kind))[:new]
+    want, mag, sens = ob.kv_attention(q, 2, c.kc, c.ks, c.vc, c.vs, c.cu, c.lens, c.table, c.max_len)
+    # as in _check_attention; the sum of the weights may lose 2^-14 of itself and 2^-29 for each key
+    ds = ((64 + 6) * np.repeat(sens, 64, 1) + 64) * U
+    n = length + new
+    bound = ((mag + np.abs(want)) * 2.0 ** -11 + mag * (2.1 * ds + (n / 4 + 64) * U) + n * 2.0 ** -32 * 127 * c.vs.max() +
+             np.abs(want) * (2.0 ** -14 + n * 2.0 ** -29 + HALF[dt] * 1.001) + TINY[dt] * 1.01)
+    within(got, want, bound)
+
+
+@pytest.mark.parametrize("new,kind", [(1, ""), (20, ""), (20, "tiles"), (20, "parts")])
 def test_kv_attention_of_many_keys_far_below_one(gpu, new, kind):
     """One key 2^22 times as heavy as each of 40,000 others, whose weights are no normal halves: together one percent of the sum,
     in the numerator and in the denominator alike."""
