@@ -265,7 +265,7 @@ __global__ __launch_bounds__(256, 3) void kv_few_kernel(KvAttnDev a) {
     mx = column_max(mx);
     float per = rv;                       // of the rounded weights' sum, in the denominator
     if (__any(mx > ref + kRaise || lg < quiet)) {
-      const float lg_top = column_max(seen ? lg : -INFINITY);
+      const float lg_top = column_max(own != -INFINITY ? lg : -INFINITY);
       if (mx > ref + kRaise) {
         const float next = mx - kTop, alpha = exp2_fast(ref - next);       // (0 at the first visible key)
         l_run = lower_sum(l_run, ref - next, alpha);
@@ -503,7 +503,8 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kv_prompt_kernel(KvAttn
     __syncthreads();
     const unsigned char* kv = lds + cur * STAGE;
     const bool work = unit < wend, now_seen = seen;
-    const float kst = ks, vst = vs;
+    const float kst = ks;
+    float vst = vs;
     f32x4 sc[4][2];
     unsigned char* next = lds + (cur ^ 1) * STAGE;
     if (work) {
@@ -547,6 +548,8 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kv_prompt_kernel(KvAttn
 #pragma unroll
         for (int e = 0; e < 16; ++e) sc[e >> 2][n][e & 3] = e <= limit ? sc[e >> 2][n][e & 3] : -INFINITY;
       }
+      // (a page behind the last key may never have been written: an infinite step would make a NaN of the masked scores)
+      if (unit + fq * 16 >= k1) vst = 1.0f;
     }
     const float lg = __builtin_amdgcn_logf(vst), rv = __builtin_amdgcn_rcpf(vst);
     float f[2], mx[2], own[2];
@@ -561,7 +564,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kv_prompt_kernel(KvAttn
     }
     float per = rv;
     if (__any(mx[0] > ref[0] + kRaise || mx[1] > ref[1] + kRaise || lg < quiet)) {
-      const float lg_top = column_max(now_seen ? lg : -INFINITY);
+      const float lg_top = column_max(own[0] != -INFINITY || own[1] != -INFINITY ? lg : -INFINITY);
 #pragma unroll
       for (int n = 0; n < 2; ++n)
         if (mx[n] > ref[n] + kRaise) {

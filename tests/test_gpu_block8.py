@@ -446,6 +446,26 @@ def test_kv_attention_of_pages_that_are_not_there(gpu, kind):
         assert (want == 0).all(axis=1).any()
 
 
+@pytest.mark.parametrize("kind", ["", "tiles", "parts"])
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("page,dh", [(16, 128), (16, 64), (32, 128)])
+def test_kv_attention_of_pages_named_ahead(gpu, kind, dt, page, dh):
+    """Pages that the table names behind a sequence's last token, never written: their steps have no part in anything."""
+    g = np.random.default_rng([67, page, dh])
+    lens, new = [33, 70, 17, 272, 300], [33, 50, 1, 20, 16]
+    c = Pool(g, gpu, lens, new, 2, dh, page, dt, spare=8)
+    c.table = np.concatenate([c.table, np.full((5, 4), -1, np.int32)], 1)
+    spare = [i for i in range(c.n) if i not in set(c.table.ravel().tolist())]
+    q = _bounds(c, 4, rnd(g.standard_normal((c.rows, 4 * dh)), dt), kind)
+    want = _attend(gpu, c, 4, dt, q)
+    assert np.isfinite(want).all()
+    for s, n in enumerate(lens):
+        c.table[s, -(-n // page):][:4] = np.array(spare)[[s, (s + 3) % 8, 0, 1]]
+    for k, v in ((np.nan, np.inf), (np.inf, np.nan), (0.0, np.inf), (np.inf, 0.0), (-1.0, -np.inf), (3e38, 3e38)):
+        c.ks[spare], c.vs[spare] = np.float32(k), np.float32(v)
+        assert np.array_equal(_attend(gpu, c, 4, dt, q), want), (k, v)
+
+
 def test_kv_lengths_that_no_batch_should_have(gpu):
     """Lengths beyond the table, beyond the host's bound, negative ones and new rows beyond a length: held to what is there."""
     g = np.random.default_rng(54)
