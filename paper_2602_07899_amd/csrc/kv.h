@@ -6,9 +6,9 @@ namespace tlq {
 
 struct KvSeq {
   int64_t row0;      // first of its new rows in the call's matrices
-  int n_new;         // new rows, those before the sequence's first token among them
+  int n_new;         // new rows within the host's bound, those before the sequence's first token among them
   int first;         // position of row row0 (negative: that many rows lie before the first token)
-  int len;           // tokens, those beyond the table or the host's bound left out
+  int len;           // tokens, those beyond the table or the host's bounds left out
 };
 // Values that no valid batch has are held to what is addressable.
 __device__ __forceinline__ KvSeq kv_sequence(const tlq_kv_batch& b, int page, int64_t n_tok, int s) {
@@ -18,10 +18,12 @@ __device__ __forceinline__ KvSeq kv_sequence(const tlq_kv_batch& b, int page, in
   r1 = r1 < r0 ? r0 : (r1 > n_tok ? n_tok : r1);
   const int len = b.lens[s] < 0 ? 0 : b.lens[s];
   q.row0 = r0;
-  q.n_new = (int)(r1 - r0);
-  q.first = len - q.n_new;
+  const int rows = (int)(r1 - r0);
+  q.n_new = rows < b.max_new ? rows : b.max_new;
+  q.first = len - rows;
   const int64_t room = (int64_t)b.max_pages * page;
-  q.len = len > b.max_len ? b.max_len : len;
+  q.len = q.first + q.n_new;       // (negative where all of those rows lie before the first token)
+  if (q.len > b.max_len) q.len = b.max_len;
   if (q.len > room) q.len = (int)room;
   return q;
 }

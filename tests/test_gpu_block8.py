@@ -485,6 +485,43 @@ def test_kv_lengths_that_no_batch_should_have(gpu):
         assert np.array_equal(got.cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("lens,new,most,group,page,kind", [
+    ([40, 30], [5, 3], 1, 1, 16, ""), ([700, 40], [5, 20], 3, 2, 16, ""), ([3000, 2], [9, 2], 1, 4, 64, ""),
+    ([300, 260, 9], [150, 260, 9], 40, 1, 64, "parts"), ([1500, 30], [200, 7], 130, 2, 32, "parts"), ([90, 70], [70, 70], 17, 2, 128, ""),
+    ([10, 33], [20, 33], 12, 1, 16, "")])                    # (the first with rows before its first token)
+def test_kv_more_new_tokens_than_the_hosts_bound(gpu, dt, lens, new, most, group, page, kind):
+    """Tokens behind a sequence's first max_new: their rows of Out stay as they were, the cache takes none of them."""
+    g = np.random.default_rng([68, sum(lens), most])
+    c = Pool(g, gpu, lens, new, 2, 64, page, dt)
+    heads = 2 * group
+    q = rnd(g.standard_normal((c.rows, heads * 64)), dt)
+    whole = _attend(gpu, c, heads, dt, q)
+    c.max_new = most
+    if kind == "parts":
+        q = _bounds(c, heads, q, kind)
+    got = _attend(gpu, c, heads, dt, q)
+    taken = np.concatenate([np.arange(n) < most for n in new])
+    assert (got[~taken] == 3.0).all() and not (got[taken] == 3.0).all(axis=1).any()
+    want, mag, sens = ob.kv_attention(q, heads, c.kc, c.ks, c.vc, c.vs, c.cu, c.lens, c.table, c.max_len)
+    ds = ((64 + 6) * np.repeat(sens, 64, 1) + 64) * U
+    n = max(lens)
+    bound = (mag + np.abs(want)) * 2.0 ** -11 + mag * (2.1 * ds + (n / 4 + 64) * U) + n * 2.0 ** -32 * 127 * c.vs.max() + np.abs(want) * HALF[dt] * 1.01 + TINY[dt] * 1.01
+    within(got[taken], want[taken], bound[taken])
+    within(got[taken], whole[taken], 2 * bound[taken])
+    # the oracle's append of the first max_new of each alone
+    rows = np.flatnonzero(taken)
+    x = rnd(g.standard_normal((c.rows, 2 * 64)), dt)
+    b, cache = c.load()
+    tlq.kv_append(dev(x, gpu, dt), dev(x, gpu, dt), b, cache, tlq.params(x_dtype=CODE[dt]))
+    cu = np.concatenate([[0], np.cumsum(np.minimum(new, most))]).astype(np.int32)
+    end = [n - m + min(m, most) for n, m in zip(lens, new)]
+    ob.kv_append(x[rows], c.kc, c.ks, cu, end, c.table, c.max_len, False)
+    ob.kv_append(x[rows], c.vc, c.vs, cu, end, c.table, c.max_len, True)
+    for got, want in zip(c.t, (c.kc, c.ks, c.vc, c.vs)):
+        assert np.array_equal(got.cpu().numpy(), want)
+
+
 def test_kv_attention_of_a_shared_prefix(gpu):
     """Two sequences that hold the same first pages give what they give alone."""
     import torch
