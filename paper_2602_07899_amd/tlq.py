@@ -533,8 +533,9 @@ def kv_batch(cu_new, lens, table, max_new, max_len):
     n = lens.numel()
     _shape(table.dim() == 2 and table.size(0) == n and cu_new.numel() == n + 1, "cu_new [n + 1], lens [n], table [n, pages]")
     _shape(cu_new.is_contiguous() and lens.is_contiguous(), "cu_new and lens are dense")
-    pages = table.size(1)
-    b = KvBatch(_KV_BATCH_BYTES, n, cu_new.data_ptr(), lens.data_ptr(), table.data_ptr(), max(_rows(table, "table"), pages), pages, max_new, max_len, 0)
+    pages, apart = table.size(1), _rows(table, "table")
+    _shape(apart >= pages, "table: rows that do not overlap")
+    b = KvBatch(_KV_BATCH_BYTES, n, cu_new.data_ptr(), lens.data_ptr(), table.data_ptr(), apart, pages, max_new, max_len, 0)
     b.parts = (cu_new, lens, table)
     return b
 

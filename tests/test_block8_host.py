@@ -154,6 +154,18 @@ def test_binding_refusals():
             bad()
 
 
+def test_tables_whose_rows_overlap_are_refused():
+    """Rows that lie on each other (an expanded table) would be read a row's length apart, behind the table's end."""
+    import torch
+    i = lambda *n: torch.zeros(n, dtype=torch.int32)
+    for table in (i(1, 5).expand(2, 5), torch.as_strided(i(9), (2, 5), (4, 1)), i(1, 1).expand(2, 1)):
+        with pytest.raises(ValueError):
+            tlq.kv_batch(i(3), i(2), table, 1, 40)
+    b = tlq.kv_batch(i(2), i(1), torch.as_strided(i(9), (1, 5), (0, 1)), 1, 40)      # (of a single row the stride is never used)
+    assert b.max_pages == 5 <= b.ld_table
+    assert tlq.kv_batch(i(3), i(2), i(2, 1), 1, 16).ld_table == 1
+
+
 # ------------------------------------------------------------------ pins of the oracle
 def test_oracle_attention_by_hand():
     """One key head, two tokens, weights 1 / 3 and 2 / 3 by hand; the first row sees itself only."""
