@@ -535,6 +535,7 @@ def kv_batch(cu_new, lens, table, max_new, max_len):
     _shape(cu_new.is_contiguous() and lens.is_contiguous(), "cu_new and lens are dense")
     pages, apart = table.size(1), _rows(table, "table")
     _shape(apart >= pages, "table: rows that do not overlap")
+    _shape(-(1 << 31) <= max_new < 1 << 31 and -(1 << 31) <= max_len < 1 << 31, "max_new, max_len: 32-bit numbers")
     b = KvBatch(_KV_BATCH_BYTES, n, cu_new.data_ptr(), lens.data_ptr(), table.data_ptr(), apart, pages, max_new, max_len, 0)
     b.parts = (cu_new, lens, table)
     return b

@@ -166,6 +166,16 @@ def test_tables_whose_rows_overlap_are_refused():
     assert tlq.kv_batch(i(3), i(2), i(2, 1), 1, 16).ld_table == 1
 
 
+def test_bounds_beyond_32_bits_are_refused():
+    """A bound of tokens that the structure cannot hold is not cut to its low bits."""
+    import torch
+    i = lambda *n: torch.zeros(n, dtype=torch.int32)
+    for new, most in ((1, (1 << 32) + 40), ((1 << 32) + 1, 40), (1, 1 << 31), (1 - (1 << 32), 40), (1, 40 - (1 << 32))):
+        with pytest.raises(ValueError):
+            tlq.kv_batch(i(3), i(2), i(2, 5), new, most)
+    assert tlq.kv_batch(i(3), i(2), i(2, 5), 1, (1 << 31) - 1).max_len == (1 << 31) - 1      # (the call refuses it)
+
+
 # ------------------------------------------------------------------ pins of the oracle
 def test_oracle_attention_by_hand():
     """One key head, two tokens, weights 1 / 3 and 2 / 3 by hand; the first row sees itself only."""
