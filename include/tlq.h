@@ -339,7 +339,8 @@ tlq_status tlq_residual_add(const void* H, int64_t ldh, const void* Z, int64_t l
  *   code = clip(rint(xt / step_r), -2^(bits-1), 2^(bits-1) - 1).
  * X [n, c] x_dtype; factor: float [c], 16-byte aligned, or NULL (ones) - the searched scales for weight rows, their
  * reciprocals for tokens; bits 2..8; codes: out int8 [n, ldc], ldc (bytes) a multiple of 16 and at least c rounded up
- * to 128 (zeros are written behind c up to there, nothing beyond); 16-byte aligned; steps: out float [n].  A NaN has the
+ * to 128 (zeros are written behind c up to there, nothing beyond); 16-byte aligned; steps: out float [n]; n + 8 times the
+ * smaller of 8 and c / 512 (rounded up) at most 2^29, here and in tlq_linear_i8.  A NaN has the
  * lowest code and no part in the step; an infinity makes the step infinite. */
 tlq_status tlq_row_codes(const void* X, int64_t n, int64_t c, int64_t ldx, const float* factor, int32_t bits,
                          const tlq_params* p, int8_t* codes, int64_t ldc, float* steps, void* stream);
@@ -357,7 +358,7 @@ tlq_status tlq_linear_i8(const void* X, int64_t n_tok, int64_t c_in, int64_t ldx
  *   u = x / sqrt(mean_d x^2 + eps) * w[d];  angle = pos[t] * inv_freq[i] (in double), i < rot / 2;
  *   (u_a, u_b) -> (u_a cos - u_b sin, u_b cos + u_a sin), (a, b) = (i, i + rot/2), or (2i, 2i+1) with interleaved = 1;
  * d >= rot is not rotated.  Float arithmetic, one rounding to x_dtype at the end.
- * Q [n_tok, n_heads * head_dim], K [n_tok, n_kv_heads * head_dim] x_dtype, n_tok < 2^26, 16-byte aligned, strides multiples of 8
+ * Q [n_tok, n_heads * head_dim], K [n_tok, n_kv_heads * head_dim] x_dtype, n_tok <= 2^26 - 4, 16-byte aligned, strides multiples of 8
  * (both may be column slices of one matrix); head_dim 64, 128 or 256 (TLQ_ERR_UNSUPPORTED otherwise); rot a multiple
  * of 16, 0 <= rot <= head_dim; eps >= 0 (with 0 a head of zeros gives NaN); pos int32 [n_tok] (any sign), inv_freq
  * double [rot/2]; wq, wk float [head_dim], 16-byte aligned, or NULL (ones; both have to be NULL without norm).  Q_out may be Q with the same stride, K_out likewise K; no

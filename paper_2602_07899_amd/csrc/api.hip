@@ -859,19 +859,24 @@ tlq_status tlq_residual_add(const void* H, int64_t ldh, const void* Z, int64_t l
 
 
 // ------------------------------------------------------------ a decoder block in 8 bits
+// rows of codes: eight to a block, a wave of it for each 512 channels up to eight, and fewer than 2^32 threads a launch
+static bool row_codes_fit(int64_t n, int64_t c) {
+  const int64_t waves = ceil_div(c, 512);
+  return (n + 8) * (waves < 8 ? waves : 8) <= (1LL << 29);
+}
 tlq_status tlq_row_codes(const void* X, int64_t n, int64_t c, int64_t ldx, const float* factor, int32_t bits,
                          const tlq_params* p, int8_t* codes, int64_t ldc, float* steps, void* stream) {
   if (!X || !codes || !steps) return TLQ_ERR_NULL;
   TLQ_TRY(check_params(p));
   if (bits < 2 || bits > 8) return TLQ_ERR_UNSUPPORTED;
-  if (!dims_ok(n, c, ldx) || (c % 8) != 0 || ldc < int8_row(c) || ldc >= (1LL << 31)) return TLQ_ERR_SHAPE;
+  if (!dims_ok(n, c, ldx) || (c % 8) != 0 || !row_codes_fit(n, c) || ldc < int8_row(c) || ldc >= (1LL << 31)) return TLQ_ERR_SHAPE;
   if (!mat16_aligned(X, ldx) || !aligned(codes, 16) || (ldc % 16) != 0 || (factor && !aligned(factor, 16)) || !aligned(steps, 4))
     return TLQ_ERR_ALIGN;
   return hip_status(launch_row_codes(X, n, c, ldx, p->x_dtype == TLQ_BF16, factor, bits, codes, ldc, steps, (hipStream_t)stream));
 }
 
 size_t tlq_linear_i8_workspace_bytes(int64_t n_tok, int64_t c_in) {
-  if (n_tok <= 0 || c_in <= 0 || n_tok >= (1LL << 31) || c_in > kMaxLinearI8) return 0;
+  if (n_tok <= 0 || c_in <= 0 || n_tok >= (1LL << 31) || c_in > kMaxLinearI8 || !row_codes_fit(n_tok, c_in)) return 0;
   return align_up((size_t)n_tok * int8_row(c_in), 256) + align_up((size_t)n_tok * sizeof(float), 256) +
          (n_tok <= kLinearMidTokens ? (size_t)(n_tok < 64 ? n_tok : 64) * kLinearMidInts * sizeof(int) : 0);
 }
@@ -883,7 +888,7 @@ tlq_status tlq_linear_i8(const void* X, int64_t n_tok, int64_t c_in, int64_t ldx
   TLQ_TRY(check_params(p));
   if (p->act_bits == 0 || c_in > kMaxLinearI8) return TLQ_ERR_UNSUPPORTED;
   if (!dims_ok(n_tok, c_in, ldx) || (c_in % 8) != 0 || !dims_ok(c_out, int8_row(c_in), ldw) || ldw >= (1LL << 22) || c_out >= (1LL << 29) ||
-      !dims_ok(n_tok, c_out, ldy))
+      !dims_ok(n_tok, c_out, ldy) || !row_codes_fit(n_tok, c_in))
     return TLQ_ERR_SHAPE;
   if (!mat16_aligned(X, ldx) || !aligned(w_codes, 16) || (ldw % 16) != 0 || !aligned(w_steps, 16) ||
       (factor && !aligned(factor, 16)) || !mat_aligned(Y, ldy, p->yref_dtype))
@@ -919,7 +924,7 @@ tlq_status tlq_qk_norm_rope(const void* Q, int64_t ldq, int32_t n_heads, const v
   if ((head_dim != 64 && head_dim != 128 && head_dim != 256) || (interleaved != 0 && interleaved != 1) ||
       (norm != 0 && norm != 1) || (norm == 0 && (wq || wk)) || !(eps >= 0.0f) || eps > 3.0e38f)
     return TLQ_ERR_UNSUPPORTED;
-  if (n_tok <= 0 || n_tok >= (1LL << 26) || n_heads <= 0 || n_heads > 65535 || n_kv_heads <= 0 || n_kv_heads > 65535 || rot < 0 ||
+  if (n_tok <= 0 || n_tok > (1LL << 26) - 4 || n_heads <= 0 || n_heads > 65535 || n_kv_heads <= 0 || n_kv_heads > 65535 || rot < 0 ||
       rot > head_dim || (rot % 16) != 0)
     return TLQ_ERR_SHAPE;
   const int64_t wide = (int64_t)n_heads * head_dim, narrow = (int64_t)n_kv_heads * head_dim;

@@ -61,6 +61,20 @@ def test_rope_refusals():
         assert call(**bad) == tlq.ERR_ALIGN, bad
 
 
+def test_rows_beyond_the_threads_of_a_launch_are_refused():
+    """A launch has fewer than 2^32 threads: rows of codes go eight to a block of up to eight waves, tokens' heads four tokens to
+    a block of four."""
+    l, p, a = tlq.lib(), tlq.params(), tlq.params(act_bits=8)
+    for n, c in (((1 << 29) - 7, 8), ((1 << 29) - 7, 512), ((1 << 28) - 7, 520), ((1 << 26) - 7, 4096), ((1 << 26) - 7, 65536)):
+        assert l.tlq_row_codes(FAKE, n, c, c, None, 8, C.byref(p), FAKE, -(-c // 128) * 128, FAKE, None) == tlq.ERR_SHAPE, (n, c)
+        assert l.tlq_linear_i8(FAKE, n, c, c, None, FAKE, 8, -(-c // 128) * 128, FAKE, C.byref(a), FAKE, 8, FAKE, 1 << 60, None) == tlq.ERR_SHAPE
+        assert tlq.linear_i8_workspace_bytes(n, c) == 0 < tlq.linear_i8_workspace_bytes(n - 1, c)
+        # one row less is none of these (an address that is out of line is found behind the sizes)
+        assert l.tlq_row_codes(ODD, n - 1, c, c, None, 8, C.byref(p), FAKE, -(-c // 128) * 128, FAKE, None) == tlq.ERR_ALIGN
+    rope = lambda Q, n: l.tlq_qk_norm_rope(Q, 64, 1, FAKE, 64, 1, n, 64, 64, 0, 1, 1e-6, None, None, FAKE, FAKE, C.byref(p), FAKE, 64, FAKE, 64, None)
+    assert rope(FAKE, (1 << 26) - 3) == rope(FAKE, (1 << 26) - 1) == tlq.ERR_SHAPE and rope(ODD, (1 << 26) - 4) == tlq.ERR_ALIGN
+
+
 def _kv(**k):
     c = tlq.KvCache(C.sizeof(tlq.KvCache), 2, 128, 64, 10, 0x1000, 0x1000, 0x1000, 0x1000)
     b = tlq.KvBatch(C.sizeof(tlq.KvBatch), 3, 0x1000, 0x1000, 0x1000, 4, 4, 2, 200, 0)
