@@ -194,6 +194,87 @@ def test_linear_i8_extreme_sums(gpu):
         within(host(y), want, np.abs(want) * 4 * U)
 
 
+def _kernels(call):
+    """Names of the library's launches of a call, other than the codes'."""
+    tlq.profile_reset()
+    tlq.profile_enable(True)
+    try:
+        call()
+        return {k.name for k in tlq.profile_read() if k.launches} - {"row_codes", "act_quant"}
+    finally:
+        tlq.profile_enable(False)
+        tlq.profile_reset()
+
+
+FEW, MID, TILES = {"linear_few"}, {"linear_mid", "linear_join"}, {"gemm_store"}
+
+
+@pytest.mark.parametrize("dt,out", [("f16", "x"), ("bf16", "f32"), ("bf16", "x")])
+@pytest.mark.parametrize("n,ci,co,kernels", [
+    (300, 1096, 263, FEW), (64, 8200, 2203, MID), (200, 4104, 1003, MID), (300, 4104, 263, TILES),
+    # tiles of 128 x 128, at most one a CU and more; of 256 outputs x 256, 192 and 320 tokens; ragged outputs and tokens
+    (1000, 264, 2051, TILES), (2501, 136, 2050, TILES), (6391, 136, 2557, TILES), (4001, 136, 2051, TILES), (8001, 136, 2051, TILES),
+    # rows longer than the search's
+    (300, 20008, 70, TILES), (520, 65536, 262, TILES)])
+def test_linear_i8_by_kernel(gpu, dt, out, n, ci, co, kernels):
+    """Every kernel of the product, each named, against the oracle."""
+    import torch
+    g = np.random.default_rng([25, n, ci, co])
+    x, f, wc, ws = _linear_case(g, n, ci, co, dt, 8)
+    od = dt if out == "x" else "f32"
+    p = tlq.params(act_bits=8, x_dtype=CODE[dt], yref_dtype=CODE[od])
+    xt, _ = spread(x, gpu, dt)
+    y, wide = spread(np.zeros((n, co), np.float32), gpu, od)
+    work = torch.full((tlq.linear_i8_workspace_bytes(n, ci),), 0xAB, dtype=torch.uint8, device=gpu)
+    w, s, ft = _padded(wc, gpu, 16), dev(ws, gpu), dev(f, gpu)
+    assert _kernels(lambda: tlq.linear_i8(xt, w, s, p, y, factor=ft, workspace=work)) == kernels
+    want = ob.linear_i8(x, 8, wc, ws, f)
+    within(host(y), want, np.abs(want) * (HALF[od] + 3.1 * U) + TINY[od] + 1e-44)
+    keep = torch.ones(wide.shape[1], dtype=torch.bool)
+    keep[8:8 + co] = False
+    assert bool((wide[:, keep.to(gpu)] == 3.0).all())
+
+
+def test_linear_i8_is_the_propagation_of_the_search_in_every_kernel(gpu):
+    """What apply_best gives, by the kernels for few tokens, for shared tokens and by tiles."""
+    import torch
+    g = np.random.default_rng(26)
+    for n, ci, co, cases in ((700, 384, 1003, ((700, TILES), (300, FEW), (20, FEW))), (300, 4104, 200, ((300, TILES), (256, MID), (50, FEW))),
+                             (64, 8200, 2400, ((64, MID),))):
+        x, W = rnd(g.standard_normal((n, ci)), "bf16"), rnd(g.standard_normal((co, ci)) * 0.02, "bf16")
+        s = np.exp(0.5 * g.standard_normal(ci)).astype(np.float32)
+        p = tlq.params(bits=8, group=0, symmetric=1, act_bits=8, x_dtype=tlq.BF16, yref_dtype=tlq.BF16)
+        X, Wt, st = dev(x, gpu, "bf16"), dev(W, gpu, "bf16"), dev(s, gpu)
+        a, y = (torch.empty((n, -(-co // 8) * 8), dtype=torch.bfloat16, device=gpu)[:, :co] for _ in range(2))
+        tlq.apply_best(X, Wt, st, p, a)
+        codes, steps = torch.empty((co, -(-ci // 128) * 128), dtype=torch.int8, device=gpu), torch.empty(co, device=gpu)
+        tlq.row_codes(Wt, 8, p, codes, steps, factor=st)
+        inv = dev(np.float32(1) / s, gpu)
+        for rows, kernels in cases:
+            assert _kernels(lambda: tlq.linear_i8(X[:rows], codes, steps, p, y[:rows], factor=inv)) == kernels, rows
+            d = (y[:rows].float() - a[:rows].float()).abs()
+            assert bool((d <= 2 * HALF["bf16"] * a[:rows].float().abs() * 1.01).all())    # (either may round the last bit the other way)
+
+
+@pytest.mark.parametrize("rows,co,kernels", [(300, 5, TILES), (700, 262, TILES), (66, 300, MID)])
+def test_linear_i8_extreme_sums_in_tiles(gpu, rows, co, kernels):
+    """The largest sums that the codes allow, 2^30, of either sign: exact in 32 bits."""
+    import torch
+    ci = 65536
+    x = torch.ones((rows, ci), dtype=torch.float16, device=gpu)
+    x[1::2] = -1.0
+    # (127 times -128 each; a token of -1 and weights of 127 to -128 in turn meet the other sign)
+    wc = torch.full((co, ci), -128, dtype=torch.int8, device=gpu)
+    wc[1::3] = 127
+    ws = torch.ones(co, device=gpu)
+    p = tlq.params(act_bits=8, yref_dtype=tlq.F32)
+    y = torch.empty((rows, -(-co // 8) * 8), device=gpu)[:, :co]
+    assert _kernels(lambda: tlq.linear_i8(x, wc, ws, p, y)) == kernels
+    row = np.where(np.arange(co) % 3 == 1, 127.0, -128.0) * 127.0 * ci
+    want = np.where(np.arange(rows) % 2 == 0, 1.0, -1.0)[:, None] * row[None, :] * float(np.float32(1) / np.float32(127))
+    within(host(y), want, np.abs(want) * 4 * U)
+
+
 # ------------------------------------------------------------------ queries and keys
 @pytest.mark.parametrize("dt", ["f16", "bf16"])
 @pytest.mark.parametrize("n,h,kv,dh,rot,pairs,norm,far", [
