@@ -120,9 +120,21 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkRopeArgs a, int wpt
       float ss = 0.0f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) ss = __builtin_fmaf(u[j], u[j], ss);
-      const float mean = head_sum<LPH>(ss) * (1.0f / DH) + a.eps;
-      float inv = __builtin_amdgcn_rsqf(mean);
-      if (mean < 1e-30f) inv = 1.0f / sqrtf(mean);
+      float mean = head_sum<LPH>(ss) * (1.0f / DH) + a.eps;
+      // (bf16 heads whose squares are no floats, beside ordinary ones of the wave: taken times a power of two; what is not
+      // finite stays so)
+      const bool fits = mean >= 1e-30f && mean <= 1e37f;
+      if (__builtin_expect(__any(!fits), 0)) {
+        const float times = fits ? 1.0f : mean < 1e-30f ? 0x1p100f : 0x1p-80f;
+        ss = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          u[j] *= times;
+          ss = __builtin_fmaf(u[j], u[j], ss);
+        }
+        mean = head_sum<LPH>(ss) * (1.0f / DH) + a.eps * times * times;
+      }
+      const float inv = __builtin_amdgcn_rsqf(mean);
 #pragma unroll
       for (int j = 0; j < 8; ++j) u[j] = u[j] * inv * (key ? wk[j] : wq[j]);
     }

@@ -319,6 +319,35 @@ def test_qk_norm_rope(gpu, dt, n, h, kv, dh, rot, pairs, norm, far):
     assert torch.equal(both[:, :h * dh], qo) and torch.equal(both[:, h * dh:], ko)
 
 
+@pytest.mark.parametrize("dh,rot,pairs", [(64, 64, False), (128, 64, False), (256, 256, True), (128, 128, False)])
+def test_qk_norm_of_heads_whose_squares_are_no_floats(gpu, dh, rot, pairs):
+    """Heads near bf16's largest and smallest numbers, beside ordinary ones: squares beyond a float's range on either side."""
+    g = np.random.default_rng([32, dh])
+    n, h = 12, 5
+    size = np.concatenate([2.0 ** np.array([120, 64, 63, 50, 0, -40, -50, -75, -110, -126]), [1.0, 1.0]])
+    x = rnd(g.standard_normal((n, h * dh)) * size[:, None], "bf16")
+    x[10, dh:2 * dh] *= np.float32(2.0 ** 100)                # (one head of a token)
+    x[11, :dh] = rnd(x[11, :dh] * np.float32(2.0 ** -120), "bf16")
+    x[3, 0] = rnd(np.array([3e38]), "bf16")[0]                # (one channel of a head)
+    pos = g.integers(0, 1000, n).astype(np.int32)
+    inv = 1e4 ** (-np.arange(rot // 2) / (rot // 2))
+    w = np.exp(0.3 * g.standard_normal(dh)).astype(np.float32)
+    for eps in (0.0, 1e-6):
+        X = dev(x, gpu, "bf16")
+        qo, ko = X.clone(), X.clone()
+        tlq.qk_norm_rope(X, X, dh, dev(pos, gpu), dev(inv, gpu), tlq.params(x_dtype=tlq.BF16), qo, ko, wq=dev(w, gpu), wk=dev(w, gpu),
+                         eps=eps, interleaved=pairs)
+        want = ob.qk_norm_rope(x, dh, pos, inv, w, eps, True, pairs).reshape(n, h, dh)
+        u = np.abs(ob.qk_norm_rope(x, dh, pos, inv[:0], w, eps)).reshape(n, h, dh)
+        both_of = u.copy()
+        for i in range(rot // 2):
+            a, b = (2 * i, 2 * i + 1) if pairs else (i, i + rot // 2)
+            both_of[:, :, a] = both_of[:, :, b] = u[:, :, a] + u[:, :, b]
+        delta = (dh + 8) * U + 2 * np.pi * 2.0 ** -26 + 4 * U + pos[:, None, None] * 2.0 ** -51
+        for got in (qo, ko):
+            within(host(got).reshape(n, h, dh), want, both_of * delta + np.abs(want) * HALF["bf16"] * 1.001 + 2.0 ** -126 * 1.01)
+
+
 # ------------------------------------------------------------------ the cache
 class Pool:
     """A pool of pages with sequences in it, on the host and on the device."""
