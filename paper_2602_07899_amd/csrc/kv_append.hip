@@ -47,7 +47,7 @@ struct KvStep {
 #endif
 
 // A few new tokens a sequence: a block owns one page of one head, for K (blockIdx.z = 0) or V, and nobody else writes there.
-// Bound by latency: the table's entry, the rows, the step, the codes one after the other: 64 sequences x 8 heads of 128 5.7 us.
+// Bound by latency: the table's entry, the rows, the step, the codes one after the other: 64 sequences x 8 heads of 128 5.9 us.
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void kv_append_few_kernel(const uint16_t* __restrict__ K, int64_t ldk, const uint16_t* __restrict__ V,
                                                         int64_t ldv, int64_t n_tok, tlq_kv_batch b, tlq_kv_cache c, int max_touch) {
@@ -135,7 +135,7 @@ __global__ __launch_bounds__(256) void kv_append_few_kernel(const uint16_t* __re
 // there, so no atomics on memory.  A thread has pieces of four tokens x eight channels (up to U: half of them K's, the others
 // V's), which stay in registers between the maximum and the codes, so that rows are read once.  V's codes turn in LDS, where a
 // piece is eight words of four tokens.  Codes of tokens that the page held before are stored again where the step has grown.
-// Bound by bytes: 16 x 613 tokens x 32 heads of 128 in pages of 32 54 - 66 us, 3.7 - 4.5 TB/s (with divisions throughout, rows
+// Bound by bytes: 16 x 613 tokens x 32 heads of 128 in pages of 32 60 - 66 us, 3.7 - 4.0 TB/s (with divisions throughout, rows
 // read twice and V two bytes at a time 108).
 template <typename T, int DH, int U>
 __global__ __launch_bounds__(256) void kv_append_kernel(const uint16_t* __restrict__ K, int64_t ldk, const uint16_t* __restrict__ V,

@@ -30,7 +30,7 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
 
-// r / d for 0 <= r < 2^31, 1 <= d < 2^31, as a product: m = ceil(2^(31+s) / d), s = ceil(log2 d)
+// r / d for 0 <= r < 2^31, 1 <= d < 2^31, as a product (Granlund and Montgomery, 1994): m = ceil(2^(31+s) / d), s = ceil(log2 d)
 struct KvDiv {
   uint32_t m, s, d;
   __device__ __forceinline__ uint32_t of(uint32_t r) const { return __umulhi(r << 1, m) >> s; }
@@ -162,7 +162,7 @@ __device__ __forceinline__ float load_queries(const uint16_t* p, f16x8 (&qf)[N],
 // the keys.  Four waves take 64 keys each in turn and meet in LDS at the end; keys and values go from memory to registers,
 // where they are widened: no LDS, no barrier in the loop, the next 64 keys in flight while these are worked on.
 // For few rows (see kFewWork), bound by the bytes of the cache: 64 sequences of 4096 - 8192 tokens x 8 key heads of 128, four queries each,
-// 157 us, 5.1 TB/s of codes (a large copy reaches 5.06); one of 131,072 x 4 27 us, 5.0 TB/s; one of 1200 x 32 6.8 us, latency.
+// 158 us, 5.1 TB/s of codes (a large copy reaches 5.06); one of 131,072 x 4 26 us, 5.1 TB/s; one of 1200 x 32 6.9 us, latency.
 template <typename T, int DH>
 __global__ __launch_bounds__(256, 3) void kv_few_kernel(KvAttnDev a) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -341,9 +341,11 @@ __global__ __launch_bounds__(256, 3) void kv_few_kernel(KvAttnDev a) {
 // the next into the stage that nobody reads (one barrier a step).  A lane has 16 neighbouring keys of two queries: they lie
 // in one page, so its steps are two numbers, and the largest exponent is found on the bare products.
 // Bound by the issue of vector instructions (an exponential, a conversion and a fused product for each score, beside them the
-// widening) and, where sequences are long, by power: 16 prompts of up to 1200 tokens x 40 heads of 128 337 - 377 us, 570 - 640
-// TFLOP/s of what the mask leaves (a quarter more is computed on the diagonal's tiles, and a block has only 19 steps at most),
-// 4 of 2400 297 us, 9600 tokens x 40 heads 1031 us, 916 TFLOP/s; a library product of halves reaches 1130.
+// widening) and, where sequences are long, by power: 16 prompts of up to 1200 tokens x 40 heads of 128 343 - 361 us (one launch
+// after the other; 380 - 391 under the profiler), 600 - 630 TFLOP/s of what the mask leaves (a quarter more is computed on the
+// diagonal's tiles, and a block has only 19 steps at most), 4 of 2400 292 - 303 us, 9600 tokens x 40 heads 1000 - 1033 us, 915 -
+// 945 TFLOP/s; a library product of halves reaches 1130.  Sums of unrounded weights in every second page: the first 364 us for
+// 343.
 // Not kept, us before and with it for the first: 256 rows with eight waves 427 457, staging held in registers by hand no gain;
 // P through LDS is not needed, S^T's columns are P^T's.
 // All row tiles of a sequence and key head run on one XCD, the longest first, as far as the pairs can be dealt out evenly.

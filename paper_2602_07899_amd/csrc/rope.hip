@@ -51,8 +51,9 @@ __device__ __forceinline__ float half_head(float v, bool upper) {
 // of them, through LDS) and uses them for all heads it takes.  Angles are reduced to a fraction of a turn in double: at
 // position 2^31 a float product would be off by whole turns.
 // FORM: pairs half a head apart (their lanes trade by lane permutations), half of fewer rotated channels (by LDS), neighbours.
-// Bound by the bytes of Q and K, read and written once: 40,800 tokens x 80 heads of 128 332 - 348 us, 4.8 - 5.0 TB/s where a copy
-// of as many bytes reaches 3.9 - 5.1; by latency for few tokens: 16 x 40 heads 5.0 us.
+// Bound by the bytes of Q and K, read and written once: 40,800 tokens x 80 heads of 128 332 - 335 us one launch after the other, 337
+// - 351 under the profiler, 4.8 - 5.0 TB/s where a copy of as many bytes reaches 3.9 - 5.1; by latency for few tokens: 16 x 40
+// heads 5.0 us.
 enum { kHalfHead, kHalfRot, kNeighbours };
 template <typename T, int DH, int FORM>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkRopeArgs a, int wpt, bool nts) {
