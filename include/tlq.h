@@ -413,7 +413,7 @@ tlq_status tlq_kv_append(const void* K, int64_t ldk, const void* V, int64_t ldv,
  * below 2^-31 of its largest are rounded to 2^-39 of it) and
  * probabilities times the page's step in fp16, which the softmax's sum takes as well unless a page's step lies so far below the
  * others' that halves would lose its keys (their weights are then summed as floats); Out is rounded to x_dtype.  Steps have to
- * be positive, and scores below 2^21 in size (beyond, a float holds them to a quarter at best); other rows are undefined.
+ * be positive and finite in pages that a row sees (others may hold anything), and scores below 2^21 in size (beyond, a float holds them to a quarter at best); other rows are undefined.
  * Q, Out [n_tok, n_heads * head_dim] x_dtype, 16-byte aligned, strides multiples of 8; n_heads a multiple of n_kv_heads;
  * n_tok * (n_heads / n_kv_heads) and n_seq * n_kv_heads below 2^31 - 256, max_new * (n_heads / n_kv_heads) below 2^28,
  * that over 128 (rounded up) times n_seq * n_kv_heads below 2^30.
