@@ -423,6 +423,89 @@ tlq_status tlq_kv_attention(const void* Q, int64_t ldq, int64_t n_tok, int32_t n
                             const tlq_kv_cache* c, const tlq_params* p, void* Out, int64_t ldo, void* workspace,
                             size_t workspace_bytes, void* stream);
 
+/* ---- the block's other calls in low bits: what stands between its products, products of codes that are there already,
+ * positions of images and video, and a cache in 4 bits.  Forward only; forms for single tokens and for whole prompts; no call
+ * synchronises, allocates or keeps anything, all can be captured into a graph.
+ *
+ * tlq_add_norm_codes: the residual's addition, a root-mean-square norm and the codes of the normalised rows in one pass:
+ *   h = round16(H + Z) (Z NULL: h = H);  r = float(1 / sqrt(mean_c h^2 + eps)) with the mean and the root in double;
+ *   u = (h * r) * w[c];  step = max(max_c |u|, 1e-5) / (2^(bits-1) - 1);  code = clip(rint(u / step), -2^(bits-1), 2^(bits-1) - 1)
+ * (float arithmetic, one rounding an operation, half to even; the double sum makes r the same in any order of its terms).  The
+ * norm's weight and the searched scales' reciprocals are one factor w: float [c], 16-byte aligned, or NULL (ones).
+ * H, Z, H_out [n, c] x_dtype, 16-byte aligned, strides multiples of 8; H_out may be NULL (not wanted), or H or Z with the same
+ * stride; no other overlap.  c a multiple of 8, at most 65536; bits 2..8; eps >= 0 (with 0 a row of zeros gives NaN).  codes, ldc and steps as
+ * in tlq_row_codes.  A row with h that is not finite, or whose mean with eps is 0, has a NaN step (and with it every product of the row)
+ * and undefined codes.  n at most 2^21. */
+tlq_status tlq_add_norm_codes(const void* H, int64_t ldh, const void* Z, int64_t ldz, int64_t n, int64_t c, const float* w,
+                              float eps, int32_t bits, const tlq_params* p, void* H_out, int64_t ldho, int8_t* codes,
+                              int64_t ldc, float* steps, void* stream);
+
+/* tlq_linear_codes: tlq_linear_i8 on codes and steps that are there (tlq_add_norm_codes, tlq_row_codes), with an epilogue:
+ *   y = act(step_t * w_step[o] * sum_c code[t,c] * w_codes[o,c] + bias[o]);  Y[t,o] = y + R[t,o], or y * R[t,o] with mul = 1.
+ * codes int8 [n_tok, ldx] and w_codes with zeros behind c_in up to the next multiple of 128, 16-byte aligned, strides (bytes)
+ * multiples of 16 and below 2^22; steps float [n_tok].  bias: float [c_out], 16-byte aligned, or NULL.  act: one of tlq_act.
+ * R [n_tok, c_out] yref_dtype, aligned as Y, or NULL (mul has to be 0 then); Y may be R with the same stride; no other
+ * overlap.  Float arithmetic, one rounding to yref_dtype at the end.  c_in, c_out, w_steps, Y as in tlq_linear_i8; of p the
+ * type of Y is read.  Workspace from the query. */
+typedef enum {
+  TLQ_ACT_NONE = 0,
+  TLQ_ACT_SILU = 1,       /* v / (1 + exp(-v)) */
+  TLQ_ACT_GELU_TANH = 2,  /* v / 2 (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) */
+  TLQ_ACT_GELU_ERF = 3    /* v / 2 (1 + erf(v / sqrt(2))) */
+} tlq_act;
+size_t tlq_linear_codes_workspace_bytes(int64_t n_tok, int64_t c_in);
+tlq_status tlq_linear_codes(const int8_t* codes, int64_t ldx, const float* steps, int64_t n_tok, int64_t c_in, const int8_t* w_codes,
+                            int64_t c_out, int64_t ldw, const float* w_steps, const float* bias, int32_t act, const void* R,
+                            int64_t ldr, int32_t mul, const tlq_params* p, void* Y, int64_t ldy, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/* tlq_qk_norm_rope_axes: tlq_qk_norm_rope with a position for each of n_axes axes (1..4; time, height and width of image and
+ * video patches):  angle of frequency i = pos[axis[i] * ld_pos + t] * inv_freq[i].  pos int32 [n_axes, ld_pos], ld_pos >= n_tok; axis
+ * int32 [rot/2] on the device, its values are held to [0, n_axes).  Everything else as there, and the same bits where a
+ * token's positions agree. */
+tlq_status tlq_qk_norm_rope_axes(const void* Q, int64_t ldq, int32_t n_heads, const void* K, int64_t ldk, int32_t n_kv_heads,
+                                 int64_t n_tok, int32_t head_dim, int32_t rot, int32_t interleaved, int32_t norm, float eps,
+                                 const float* wq, const float* wk, const int32_t* pos, int64_t ld_pos, int32_t n_axes,
+                                 const int32_t* axis, const double* inv_freq, const tlq_params* p, void* Q_out, int64_t ldqo,
+                                 void* K_out, int64_t ldko, void* stream);
+
+/* ---- a cache in 4 bits: pages as above, with a step for each token, head and 32 channels (4.5 bits a value), so that a token's
+ * codes hang on nothing but the token and never change once they are written, however the tokens are dealt to calls.
+ * Codes are words of eight: element e of a word lies in the four bits from 4 (e / 2) + 16 (e % 2) up, as code + 8.
+ *   k uint32 [n_pages, n_kv_heads, page, head_dim / 8];  k_step half [n_pages, n_kv_heads, page, head_dim / 32];
+ *   v uint32 [n_pages, n_kv_heads, head_dim, page / 8] (the tokens of a channel are contiguous);
+ *   v_step half [n_pages, n_kv_heads, head_dim / 32, page];   key and value = (nibble - 8) * step, which halves hold
+ * exactly (appends write nibbles 1..15 and steps up to 9344; a nibble of 0 beside a step above 8188 would be none).
+ * All four 16-byte aligned; head_dim and page as above.  Batches are the same tlq_kv_batch, and device values as little trusted. */
+typedef struct tlq_kv4_cache {
+  uint32_t struct_size; /* = sizeof(tlq_kv4_cache) */
+  int32_t n_kv_heads, head_dim, page;
+  int64_t n_pages;
+  uint32_t* k; uint16_t* k_step;
+  uint32_t* v; uint16_t* v_step;
+} tlq_kv4_cache;
+/* tlq_kv4_append: the new tokens' keys and values as codes.  For a token, head and 32 neighbouring channels (float arithmetic):
+ *   step = max(max |x|, 1e-5) / 7 rounded to bf16 and then to half (its 8 significant bits keep code * step exact), 9344 at most;
+ *   code = clip(rint(x / step), -7, 7).
+ * Infinities count as +-7 and NaN as 0, neither has a part in the step.  Everything that is not a new token's stays as it was.
+ * K, V and pages that are shared as in tlq_kv_append; n_seq (n_kv_heads head_dim (max_new / 8 + 2) / 2048 + 1) below 2^23, here and in
+ * tlq_kv4_read (max_new at most n_tok there). */
+tlq_status tlq_kv4_append(const void* K, int64_t ldk, const void* V, int64_t ldv, int64_t n_tok, const tlq_kv_batch* b,
+                          const tlq_kv4_cache* c, const tlq_params* p, void* stream);
+/* tlq_kv4_read: what the tokens of a batch's rows stand for: row r of K_out and V_out [n_tok, n_kv_heads * head_dim] x_dtype, 16-byte aligned, strides
+ * multiples of 8, is the token that a tlq_kv4_append of the same batch writes from row r (cu_new from whole lengths reads whole
+ * sequences).  Rows before a sequence's first token, beyond its bounds or in a page that there is not give zeros; rows behind
+ * the last sequence, or behind a sequence's first max_new, are not written.  Exact in half, rounded to bf16.  K_out or V_out may be NULL. */
+tlq_status tlq_kv4_read(const tlq_kv_batch* b, const tlq_kv4_cache* c, const tlq_params* p, int64_t n_tok, void* K_out, int64_t ldk,
+                        void* V_out, int64_t ldv, void* stream);
+/* tlq_kv4_attention: tlq_kv_attention over a cache in 4 bits: the same rows, masks, limits and workspace rules.  Keys and values
+ * enter the matrix products exactly, queries as there, and softmax weights rounded to halves, which the softmax's sum takes as well; scores,
+ * softmax and sums are float.  Steps have to be finite in tokens that a row sees; others may hold anything. */
+size_t tlq_kv4_attention_workspace_bytes(int64_t n_tok, int32_t n_heads, const tlq_kv_batch* b, const tlq_kv4_cache* c);
+tlq_status tlq_kv4_attention(const void* Q, int64_t ldq, int64_t n_tok, int32_t n_heads, float scale, const tlq_kv_batch* b,
+                             const tlq_kv4_cache* c, const tlq_params* p, void* Out, int64_t ldo, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
 /* ---- host-side self check (no GPU work, no device memory): walks the block -> tile map that
  * the contraction kernels (S3/S4, f_fp, S6) would use for this problem shape, in both of its
  * orders (candidates inside every patch row / candidate-outermost), both patch shapes and all tile

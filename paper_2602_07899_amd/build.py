@@ -22,13 +22,14 @@ LIB = os.path.join(HERE, "libtlq.so")
 CEILING = os.path.join(HERE, "mfma_ceiling")
 
 SOURCES = ["api.hip", "stats.hip", "quant.hip", "gemm.hip", "gemm_width.hip", "gemm_tok.hip", "gemm_half.hip", "gemm_i8.hip", "glue.hip", "block.hip", "select.hip", "profile.hip", "noalloc.hip", "gram.hip",
-           "linear.hip", "rope.hip", "kv_append.hip", "kv_attention.hip"]
+           "linear.hip", "rope.hip", "kv_append.hip", "kv_attention.hip", "norm_codes.hip", "gemm_i8_finish.hip",
+           "kv4_cache.hip", "kv4_attention.hip"]
 COMMON = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-I", os.path.join(ROOT, "include"),
           "-I", CSRC, "-Wall", "-Wno-unused-function",
           # keep hipcc from forming packed-fp32 instructions on its own
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 # the quantiser's float arithmetic must round once per written operation
-PER_FILE = {"quant.hip": ["-ffp-contract=off"]}
+PER_FILE = {"quant.hip": ["-ffp-contract=off"], "norm_codes.hip": ["-ffp-contract=off"]}
 
 
 def hipcc() -> str:

@@ -901,7 +901,7 @@ tlq_status tlq_linear_i8(const void* X, int64_t n_tok, int64_t c_in, int64_t ldx
   float* steps = c.take<float>((size_t)n_tok);
   int* partial = c.take<int>(0);
   const bool bf16 = p->x_dtype == TLQ_BF16;
-  const LinearI8Args l{codes, n_tok, ld8, steps, w_codes, c_out, ldw, ld8, w_steps, Y, ldy, p->yref_dtype};
+  const LinearI8Args l{codes, n_tok, ld8, steps, w_codes, c_out, ldw, ld8, w_steps, Y, ldy, p->yref_dtype, false, {}};
   TLQ_HIP(launch_row_codes(X, n_tok, c_in, ldx, bf16, factor, p->act_bits, codes, ld8, steps, st));
   const LinearKind kind = linear_kind(n_tok, c_out, ld8);
   if (kind == kLinearFew) return hip_status(launch_linear_few(l, st));
@@ -915,32 +915,49 @@ tlq_status tlq_linear_i8(const void* X, int64_t n_tok, int64_t c_in, int64_t ldx
   return hip_status(launch_gemm_store(g, st));
 }
 
-tlq_status tlq_qk_norm_rope(const void* Q, int64_t ldq, int32_t n_heads, const void* K, int64_t ldk, int32_t n_kv_heads,
+static tlq_status norm_rope(const void* Q, int64_t ldq, int32_t n_heads, const void* K, int64_t ldk, int32_t n_kv_heads,
                             int64_t n_tok, int32_t head_dim, int32_t rot, int32_t interleaved, int32_t norm, float eps,
                             const float* wq, const float* wk, const int32_t* pos, const double* inv_freq,
-                            const tlq_params* p, void* Q_out, int64_t ldqo, void* K_out, int64_t ldko, void* stream) {
-  if (!Q || !K || !Q_out || !K_out || !pos || (!inv_freq && rot > 0)) return TLQ_ERR_NULL;
+                            const tlq_params* p, void* Q_out, int64_t ldqo, void* K_out, int64_t ldko, void* stream,
+                            bool axes, const int32_t* axis, int64_t ld_pos, int32_t n_axes) {
+  if (!Q || !K || !Q_out || !K_out || !pos || ((!inv_freq || (axes && !axis)) && rot > 0)) return TLQ_ERR_NULL;
   TLQ_TRY(check_params(p));
   if ((head_dim != 64 && head_dim != 128 && head_dim != 256) || (interleaved != 0 && interleaved != 1) ||
-      (norm != 0 && norm != 1) || (norm == 0 && (wq || wk)) || !(eps >= 0.0f) || eps > 3.0e38f)
+      (norm != 0 && norm != 1) || (norm == 0 && (wq || wk)) || !(eps >= 0.0f) || eps > 3.0e38f || (axes && (n_axes < 1 || n_axes > 4)))
     return TLQ_ERR_UNSUPPORTED;
   if (n_tok <= 0 || n_tok > (1LL << 26) - 4 || n_heads <= 0 || n_heads > 65535 || n_kv_heads <= 0 || n_kv_heads > 65535 || rot < 0 ||
-      rot > head_dim || (rot % 16) != 0)
+      rot > head_dim || (rot % 16) != 0 || (axes && (ld_pos < n_tok || ld_pos >= (1LL << 40))))
     return TLQ_ERR_SHAPE;
   const int64_t wide = (int64_t)n_heads * head_dim, narrow = (int64_t)n_kv_heads * head_dim;
   if (ldq < wide || ldqo < wide || ldk < narrow || ldko < narrow) return TLQ_ERR_SHAPE;
   if (!mat16_aligned(Q, ldq) || !mat16_aligned(K, ldk) || !mat16_aligned(Q_out, ldqo) || !mat16_aligned(K_out, ldko) ||
-      (wq && !aligned(wq, 16)) || (wk && !aligned(wk, 16)) || !aligned(pos, 4) || !aligned(inv_freq, 8))
+      (wq && !aligned(wq, 16)) || (wk && !aligned(wk, 16)) || !aligned(pos, 4) || !aligned(inv_freq, 8) || (axis && !aligned(axis, 4)))
     return TLQ_ERR_ALIGN;
   return hip_status(launch_qk_norm_rope({Q, K, ldq, ldk, n_heads, n_kv_heads, n_tok, head_dim, rot, interleaved != 0, norm != 0,
-                                         p->x_dtype == TLQ_BF16, eps, wq, wk, pos, inv_freq, Q_out, K_out, ldqo, ldko},
+                                         p->x_dtype == TLQ_BF16, eps, wq, wk, pos, inv_freq, Q_out, K_out, ldqo, ldko, axis, ld_pos, n_axes},
                                         (hipStream_t)stream));
+}
+tlq_status tlq_qk_norm_rope(const void* Q, int64_t ldq, int32_t n_heads, const void* K, int64_t ldk, int32_t n_kv_heads,
+                            int64_t n_tok, int32_t head_dim, int32_t rot, int32_t interleaved, int32_t norm, float eps,
+                            const float* wq, const float* wk, const int32_t* pos, const double* inv_freq,
+                            const tlq_params* p, void* Q_out, int64_t ldqo, void* K_out, int64_t ldko, void* stream) {
+  return norm_rope(Q, ldq, n_heads, K, ldk, n_kv_heads, n_tok, head_dim, rot, interleaved, norm, eps, wq, wk, pos, inv_freq, p, Q_out, ldqo,
+                   K_out, ldko, stream, false, nullptr, 0, 1);
+}
+tlq_status tlq_qk_norm_rope_axes(const void* Q, int64_t ldq, int32_t n_heads, const void* K, int64_t ldk, int32_t n_kv_heads,
+                                 int64_t n_tok, int32_t head_dim, int32_t rot, int32_t interleaved, int32_t norm, float eps,
+                                 const float* wq, const float* wk, const int32_t* pos, int64_t ld_pos, int32_t n_axes,
+                                 const int32_t* axis, const double* inv_freq, const tlq_params* p, void* Q_out, int64_t ldqo,
+                                 void* K_out, int64_t ldko, void* stream) {
+  return norm_rope(Q, ldq, n_heads, K, ldk, n_kv_heads, n_tok, head_dim, rot, interleaved, norm, eps, wq, wk, pos, inv_freq, p, Q_out, ldqo,
+                   K_out, ldko, stream, true, axis, ld_pos, n_axes);
 }
 
 // sizes of a cache and a batch (no pointer); then the rest
-static tlq_status check_kv_sizes(const tlq_kv_batch* b, const tlq_kv_cache* c) {
+extern "C++" template <typename Cache>
+static tlq_status check_kv_sizes(const tlq_kv_batch* b, const Cache* c) {
   if (!b || !c) return TLQ_ERR_NULL;
-  if (b->struct_size != sizeof(tlq_kv_batch) || c->struct_size != sizeof(tlq_kv_cache) || b->reserved != 0) return TLQ_ERR_UNSUPPORTED;
+  if (b->struct_size != sizeof(tlq_kv_batch) || c->struct_size != sizeof(Cache) || b->reserved != 0) return TLQ_ERR_UNSUPPORTED;
   if (c->head_dim != 64 && c->head_dim != 128) return TLQ_ERR_UNSUPPORTED;
   if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128 && c->page != 256) return TLQ_ERR_UNSUPPORTED;
   if (c->n_kv_heads <= 0 || c->n_kv_heads > 65535 || c->n_pages <= 0 || c->n_pages >= (1LL << 31) || b->n_seq <= 0 ||
@@ -971,7 +988,8 @@ tlq_status tlq_kv_append(const void* K, int64_t ldk, const void* V, int64_t ldv,
   return hip_status(launch_kv_append(K, ldk, V, ldv, n_tok, *b, *c, p->x_dtype == TLQ_BF16, (hipStream_t)stream));
 }
 
-static tlq_status check_kv_heads(int64_t n_tok, int32_t n_heads, const tlq_kv_batch* b, const tlq_kv_cache* c) {
+extern "C++" template <typename Cache>
+static tlq_status check_kv_heads(int64_t n_tok, int32_t n_heads, const tlq_kv_batch* b, const Cache* c) {
   if (n_tok <= 0 || n_tok >= (1LL << 31) || n_heads <= 0 || n_heads > 65535 || (n_heads % c->n_kv_heads) != 0 ||
       n_tok * (n_heads / c->n_kv_heads) >= (1LL << 31) - 256 ||      // (rows are counted in 32 bits; a launch has 2^24 blocks)
       (b->max_new < n_tok ? b->max_new : n_tok) * (n_heads / c->n_kv_heads) >= (1LL << 28) ||
@@ -1000,6 +1018,119 @@ tlq_status tlq_kv_attention(const void* Q, int64_t ldq, int64_t n_tok, int32_t n
   if (scale == 0.0f) scale = c->head_dim == 128 ? 0.08838834764831845f : 0.125f;
   return hip_status(launch_kv_attention(Q, ldq, n_tok, n_heads, scale, *b, *c, p->x_dtype == TLQ_BF16, Out, ldo, workspace,
                                         (hipStream_t)stream));
+}
+
+// ------------------------------------------------------------ the block's other calls in low bits
+tlq_status tlq_add_norm_codes(const void* H, int64_t ldh, const void* Z, int64_t ldz, int64_t n, int64_t c, const float* w,
+                              float eps, int32_t bits, const tlq_params* p, void* H_out, int64_t ldho, int8_t* codes,
+                              int64_t ldc, float* steps, void* stream) {
+  if (!H || !codes || !steps) return TLQ_ERR_NULL;
+  TLQ_TRY(check_params(p));
+  if (bits < 2 || bits > 8 || !(eps >= 0.0f) || eps > 3.0e38f || c > kMaxLinearI8) return TLQ_ERR_UNSUPPORTED;
+  // (a block of up to 1024 threads a row, fewer than 2^32 threads a launch)
+  if (!dims_ok(n, c, ldh) || (c % 8) != 0 || n > (1 << 21) || (Z && ldz < c) || (H_out && ldho < c) || ldc < int8_row(c) || ldc >= (1LL << 31))
+    return TLQ_ERR_SHAPE;
+  if (!mat16_aligned(H, ldh) || (Z && !mat16_aligned(Z, ldz)) || (H_out && !mat16_aligned(H_out, ldho)) || !aligned(codes, 16) ||
+      (ldc % 16) != 0 || (w && !aligned(w, 16)) || !aligned(steps, 4))
+    return TLQ_ERR_ALIGN;
+  return hip_status(launch_add_norm_codes(H, ldh, Z, ldz, n, c, w, eps, bits, p->x_dtype == TLQ_BF16, H_out, ldho, codes, ldc, steps,
+                                          (hipStream_t)stream));
+}
+
+size_t tlq_linear_codes_workspace_bytes(int64_t n_tok, int64_t c_in) {
+  if (n_tok <= 0 || c_in <= 0 || n_tok >= (1LL << 31) || c_in > kMaxLinearI8) return 0;
+  return n_tok <= kLinearMidTokens ? (size_t)(n_tok < 64 ? n_tok : 64) * kLinearMidInts * sizeof(int) : 0;
+}
+
+tlq_status tlq_linear_codes(const int8_t* codes, int64_t ldx, const float* steps, int64_t n_tok, int64_t c_in, const int8_t* w_codes,
+                            int64_t c_out, int64_t ldw, const float* w_steps, const float* bias, int32_t act, const void* R,
+                            int64_t ldr, int32_t mul, const tlq_params* p, void* Y, int64_t ldy, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+  if (!codes || !steps || !w_codes || !w_steps || !Y) return TLQ_ERR_NULL;
+  TLQ_TRY(check_params(p));
+  if (c_in > kMaxLinearI8 || act < TLQ_ACT_NONE || act > TLQ_ACT_GELU_ERF || (mul != 0 && mul != 1) || (mul != 0 && !R)) return TLQ_ERR_UNSUPPORTED;
+  if (!dims_ok(n_tok, c_in, ldx) || (c_in % 8) != 0 || ldx < int8_row(c_in) || ldx >= (1LL << 22) || !dims_ok(c_out, int8_row(c_in), ldw) ||
+      ldw >= (1LL << 22) || c_out >= (1LL << 29) || !dims_ok(n_tok, c_out, ldy) || (R && ldr < c_out))
+    return TLQ_ERR_SHAPE;
+  if (!aligned(codes, 16) || (ldx % 16) != 0 || !aligned(steps, 4) || !aligned(w_codes, 16) || (ldw % 16) != 0 || !aligned(w_steps, 16) ||
+      (bias && !aligned(bias, 16)) || !mat_aligned(Y, ldy, p->yref_dtype) || (R && !mat_aligned(R, ldr, p->yref_dtype)))
+    return TLQ_ERR_ALIGN;
+  TLQ_TRY(check_ws(workspace, workspace_bytes, tlq_linear_codes_workspace_bytes(n_tok, c_in)));
+  hipStream_t st = (hipStream_t)stream;
+  const int64_t k = int8_row(c_in);
+  const bool tanh_form = act == TLQ_ACT_GELU_TANH;
+  const Finish fin{bias, R, ldr, act, mul, tanh_form ? 1.59576912f : 1.0f, tanh_form ? 0.0713548163f : 0.0f};
+  const bool finish = bias || R || act != TLQ_ACT_NONE;
+  const LinearI8Args l{codes, n_tok, ldx, steps, w_codes, c_out, ldw, k, w_steps, Y, ldy, p->yref_dtype, finish, fin};
+  const LinearKind kind = linear_kind(n_tok, c_out, k);
+  if (kind == kLinearFew) return hip_status(launch_linear_few(l, st));
+  if (kind == kLinearMid) return hip_status(launch_linear_mid(l, linear_mid_splits(n_tok, c_out, k), (int*)workspace, st));
+  GemmArgs g{};
+  g.X = codes; g.n_tok = n_tok; g.tok_scale = steps; g.Wh = w_codes; g.c_out = c_out; g.n_cand = 1; g.row_scale = w_steps;
+  g.i8_k = c_in; g.c_in = k / 2; g.ldx = ldx / 2; g.ldw = ldw / 2;      // (in units of 16 bits)
+  g.Yout = Y; g.ldo = ldy; g.yout_dtype = p->yref_dtype;
+  g.wide_patch = true;
+  g.tile() = gemm_tile(g, kTileAll, INT64_MAX);
+  g.fin = fin;
+  return hip_status(finish ? launch_gemm_finish(g, st) : launch_gemm_store(g, st));
+}
+
+static tlq_status check_kv4(const tlq_kv_batch* b, const tlq_kv4_cache* c) {
+  TLQ_TRY(check_kv_sizes(b, c));
+  if (!b->cu_new || !b->lens || !b->table || !c->k || !c->k_step || !c->v || !c->v_step) return TLQ_ERR_NULL;
+  if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->k_step, 16) || !aligned(c->v_step, 16) || !aligned(b->cu_new, 4) ||
+      !aligned(b->lens, 4) || !aligned(b->table, 4))
+    return TLQ_ERR_ALIGN;
+  return TLQ_OK;
+}
+// blocks of 256 threads, each with eight tokens of eight channels, for K and for V: fewer than 2^32 threads a launch
+static bool kv4_rows_fit(int64_t n_tok, const tlq_kv_batch& b, const tlq_kv4_cache& c) {
+  const int64_t most = b.max_new < n_tok ? b.max_new : n_tok;
+  return ((int64_t)c.n_kv_heads * c.head_dim * (most / 8 + 2) / 2048 + 1) * b.n_seq < (1LL << 23);
+}
+
+tlq_status tlq_kv4_append(const void* K, int64_t ldk, const void* V, int64_t ldv, int64_t n_tok, const tlq_kv_batch* b,
+                          const tlq_kv4_cache* c, const tlq_params* p, void* stream) {
+  if (!K || !V) return TLQ_ERR_NULL;
+  TLQ_TRY(check_params(p));
+  TLQ_TRY(check_kv4(b, c));
+  const int64_t width = (int64_t)c->n_kv_heads * c->head_dim;
+  if (n_tok <= 0 || n_tok >= (1LL << 31) || ldk < width || ldv < width || !kv4_rows_fit(n_tok, *b, *c)) return TLQ_ERR_SHAPE;
+  if (!mat16_aligned(K, ldk) || !mat16_aligned(V, ldv)) return TLQ_ERR_ALIGN;
+  return hip_status(launch_kv4_append(K, ldk, V, ldv, n_tok, *b, *c, p->x_dtype == TLQ_BF16, (hipStream_t)stream));
+}
+
+tlq_status tlq_kv4_read(const tlq_kv_batch* b, const tlq_kv4_cache* c, const tlq_params* p, int64_t n_tok, void* K_out, int64_t ldk,
+                        void* V_out, int64_t ldv, void* stream) {
+  if (!K_out && !V_out) return TLQ_ERR_NULL;
+  TLQ_TRY(check_params(p));
+  TLQ_TRY(check_kv4(b, c));
+  const int64_t width = (int64_t)c->n_kv_heads * c->head_dim;
+  if (n_tok <= 0 || n_tok >= (1LL << 31) || (K_out && ldk < width) || (V_out && ldv < width) || !kv4_rows_fit(n_tok, *b, *c)) return TLQ_ERR_SHAPE;
+  if ((K_out && !mat16_aligned(K_out, ldk)) || (V_out && !mat16_aligned(V_out, ldv))) return TLQ_ERR_ALIGN;
+  return hip_status(launch_kv4_read(K_out, ldk, V_out, ldv, n_tok, *b, *c, p->x_dtype == TLQ_BF16, (hipStream_t)stream));
+}
+
+size_t tlq_kv4_attention_workspace_bytes(int64_t n_tok, int32_t n_heads, const tlq_kv_batch* b, const tlq_kv4_cache* c) {
+  if (check_kv_sizes(b, c) != TLQ_OK || check_kv_heads(n_tok, n_heads, b, c) != TLQ_OK) return 0;
+  return kv4_attention_workspace(n_tok, n_heads, *b, *c);
+}
+
+tlq_status tlq_kv4_attention(const void* Q, int64_t ldq, int64_t n_tok, int32_t n_heads, float scale, const tlq_kv_batch* b,
+                             const tlq_kv4_cache* c, const tlq_params* p, void* Out, int64_t ldo, void* workspace,
+                             size_t workspace_bytes, void* stream) {
+  if (!Q || !Out) return TLQ_ERR_NULL;
+  TLQ_TRY(check_params(p));
+  TLQ_TRY(check_kv4(b, c));
+  TLQ_TRY(check_kv_heads(n_tok, n_heads, b, c));
+  if (!(scale - scale == 0.0f)) return TLQ_ERR_UNSUPPORTED;
+  const int64_t width = (int64_t)n_heads * c->head_dim;
+  if (ldq < width || ldo < width) return TLQ_ERR_SHAPE;
+  if (!mat16_aligned(Q, ldq) || !mat16_aligned(Out, ldo)) return TLQ_ERR_ALIGN;
+  TLQ_TRY(check_ws(workspace, workspace_bytes, kv4_attention_workspace(n_tok, n_heads, *b, *c)));
+  if (scale == 0.0f) scale = c->head_dim == 128 ? 0.08838834764831845f : 0.125f;
+  return hip_status(launch_kv4_attention(Q, ldq, n_tok, n_heads, scale, *b, *c, p->x_dtype == TLQ_BF16, Out, ldo, workspace,
+                                         (hipStream_t)stream));
 }
 
 }  // extern "C"

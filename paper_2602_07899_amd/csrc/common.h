@@ -197,6 +197,9 @@ struct FinalDev {
 // gemm_tile says which is the fastest.
 struct GemmTile { bool small; int tok_blocks; };
 // S3+S4 / plain GEMM with store epilogue.
+// What follows a product's scaling (finish.h): y = act(y + bias[o]), then + or * R[t, o] of the output's type.  k1, k3: of the
+// logistic activations
+struct Finish { const float* bias; const void* R; int64_t ldr; int act, mul; float k1, k3; };
 struct GemmArgs : GemmTile {
   GemmTile& tile() { return *this; }
   const void* X; int64_t n_tok, c_in, ldx;     // tokens  [n_tok, c_in]
@@ -220,6 +223,7 @@ struct GemmArgs : GemmTile {
   int64_t i8_k; const float* row_scale; int64_t row_scale_stride;
   // store epilogue: Y[t,o]; with Yref given Yref - Y (float output and one candidate only, else an error)
   void* Yout; int64_t ldo; int yout_dtype;
+  Finish fin;   // launch_gemm_finish
 };
 void gemm_tile_counts(int64_t n_tok, int64_t c_out, GemmTile tile, int64_t* tiles_o, int64_t* tiles_t);
 // The tile for a launch of g's sizes, candidates and order.  kinds: tiles besides 256 x 256 that the launch has (stores and
@@ -234,6 +238,8 @@ int64_t gemm_blocks(const GemmArgs& g);   // workgroups of the launch (sizes, ti
 int64_t tile_map_defects(int64_t n_tok, int64_t c_in, int64_t c_out, int n_cand);
 hipError_t launch_gemm_loss(const GemmArgs& a, hipStream_t stream);
 hipError_t launch_gemm_store(const GemmArgs& a, hipStream_t stream);
+// the store of one product of integer codes with g.fin behind it (any tile but 128 x 64)
+hipError_t launch_gemm_finish(const GemmArgs& a, hipStream_t stream);
 // partial[k, tile] = sum over the tile of (X_k Wh^T)[t,o] * Y_k[t,o]  (no token weights), fp16, for a symmetric
 // Wh (sym_k): about half the flops, same partial sums
 hipError_t launch_gemm_dot(const GemmArgs& a, hipStream_t stream);
@@ -265,6 +271,7 @@ struct LinearI8Args {
   const int8_t* xc; int64_t n_tok, ldx; const float* xs;    // token codes and steps
   const int8_t* wc; int64_t c_out, ldw, K; const float* ws;
   void* Y; int64_t ldy; int ydt;
+  bool finish; Finish fin;      // finish: fin follows
 };
 enum LinearKind { kLinearFew, kLinearMid, kLinearTiles };
 constexpr int64_t kLinearMidTokens = 256;
@@ -281,6 +288,7 @@ struct QkRopeArgs {
   int head_dim, rot; bool interleaved, norm, bf16; float eps;
   const float *wq, *wk; const int32_t* pos; const double* inv_freq;
   void *Qo, *Ko; int64_t ldqo, ldko;
+  const int32_t* axis; int64_t ld_pos; int n_axes;      // axis NULL: one position a token
 };
 hipError_t launch_qk_norm_rope(const QkRopeArgs& a, hipStream_t stream);
 
@@ -291,6 +299,19 @@ hipError_t launch_kv_append(const void* K, int64_t ldk, const void* V, int64_t l
 size_t kv_attention_workspace(int64_t n_tok, int n_heads, const tlq_kv_batch& b, const tlq_kv_cache& c);
 hipError_t launch_kv_attention(const void* Q, int64_t ldq, int64_t n_tok, int n_heads, float scale, const tlq_kv_batch& b,
                                const tlq_kv_cache& c, bool bf16, void* Out, int64_t ldo, void* workspace, hipStream_t stream);
+
+// the 4-bit cache (kv4_cache.hip, kv4_attention.hip)
+hipError_t launch_kv4_append(const void* K, int64_t ldk, const void* V, int64_t ldv, int64_t n_tok, const tlq_kv_batch& b,
+                             const tlq_kv4_cache& c, bool bf16, hipStream_t stream);
+hipError_t launch_kv4_read(void* K, int64_t ldk, void* V, int64_t ldv, int64_t n_tok, const tlq_kv_batch& b,
+                           const tlq_kv4_cache& c, bool bf16, hipStream_t stream);
+size_t kv4_attention_workspace(int64_t n_tok, int n_heads, const tlq_kv_batch& b, const tlq_kv4_cache& c);
+hipError_t launch_kv4_attention(const void* Q, int64_t ldq, int64_t n_tok, int n_heads, float scale, const tlq_kv_batch& b,
+                                const tlq_kv4_cache& c, bool bf16, void* Out, int64_t ldo, void* workspace, hipStream_t stream);
+
+// residual, norm and codes (norm_codes.hip); Z, w and out may be NULL
+hipError_t launch_add_norm_codes(const void* H, int64_t ldh, const void* Z, int64_t ldz, int64_t n, int64_t c, const float* w, float eps,
+                                 int bits, bool bf16, void* out, int64_t ldo, int8_t* codes, int64_t ldc, float* steps, hipStream_t stream);
 
 // decoder-block glue (block.hip): head width 128, rows in blocks of seq_len
 hipError_t launch_causal_attention(const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V,

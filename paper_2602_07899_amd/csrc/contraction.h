@@ -41,7 +41,7 @@
 #include <type_traits>
 #include <utility>
 
-#include "common.h"
+#include "finish.h"
 
 namespace tlq {
 
@@ -125,7 +125,8 @@ template <int IA, int JB> struct Acc16 {   // acc[IA][JB] of f32x4 (16x16x32)
 
 // EPI_DOT: partial = sum over the tile of acc * Y (Y read like Y_ref, one matrix per candidate, no
 // token weights): the quadratic form of the second-moment search.
-enum { EPI_LOSS = 0, EPI_LOSS_TOK = 1, EPI_STORE = 2, EPI_DOT = 3 };
+// EPI_FINISH + an activation's class (finish.h): a store with GemmDev::fin behind the scaling.
+enum { EPI_LOSS = 0, EPI_LOSS_TOK = 1, EPI_STORE = 2, EPI_DOT = 3, EPI_FINISH = 4 };
 constexpr int BK = 64;        // halves per k-tile
 constexpr int ROWB = BK * 2;  // bytes per LDS row
 // An L2 patch (one per XCD at a time) is po x pt tiles = 32 workgroups: 4 x 8 by default (4 operand
@@ -149,6 +150,7 @@ struct GemmDev {
   int cpt;          // token patches per chunk (see make_dev)
   int rag, rag_pt;  // tile rows of the last, incomplete patch row (0 = none) and its patch width in tiles
   int po, pt;       // patch shape in tiles (po * pt <= PATCH_SLOTS)
+  Finish fin;       // EPI_FINISH
   int rot;          // XCD rotation from one round of patches to the next (see make_dev)
   int64_t strips;   // > 0: no patches, the launch has this many tiles (see decode_tile)
   const float* row_scale; int64_t row_scale_stride;   // integer codes: steps of the output rows per candidate
@@ -405,6 +407,76 @@ __device__ __forceinline__ void store_rows_lds(const GemmDev& a, void* Yout, con
   });
 }
 
+#if defined(__HIP_DEVICE_COMPILE__)
+// The same with GemmDev::fin behind the scaling; the second matrix comes in whole lines through the same piece of LDS.
+template <typename YT, int CLASS, typename L, typename Acc>
+__device__ __forceinline__ void finish_rows_lds(const GemmDev& a, void* Yout, const Acc& acc, const float* tsc,
+                                                int64_t ow, int64_t tw, unsigned char* ylds) {
+  using S = Staged<L>;
+  const int lane = threadIdx.x & 63;
+  const Finish& f = a.fin;
+  static_for<0, S::GROUPS>([&](auto gc) {
+    constexpr int G = decltype(gc)::value;
+    if (f.R) S::template fill<G>(f.R, f.ldr, ow, tw, ylds);
+    else if (G > 0) wave_lds_order();
+#pragma unroll
+    for (int b = 0; b < S::template blocks<G>(); ++b) {
+      const int tb = G * L::STG + b;
+      const float sg = tsc[tw + L::tok(tb, lane)];
+#pragma unroll
+      for (int q = 0; q < L::NQ; ++q) {
+        float y[4], r[4];
+        float4 bias = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (f.bias) bias = *reinterpret_cast<const float4*>(f.bias + ow + L::row(q, lane));
+        y[0] = act_of<CLASS>(__builtin_fmaf(sg, L::get(acc, q, tb, 0), bias.x), f);
+        y[1] = act_of<CLASS>(__builtin_fmaf(sg, L::get(acc, q, tb, 1), bias.y), f);
+        y[2] = act_of<CLASS>(__builtin_fmaf(sg, L::get(acc, q, tb, 2), bias.z), f);
+        y[3] = act_of<CLASS>(__builtin_fmaf(sg, L::get(acc, q, tb, 3), bias.w), f);
+        if (f.R) {
+          unpack4<YT>(*S::at4(ylds, b, q), r);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = f.mul ? y[e] * r[e] : y[e] + r[e];
+        }
+        *S::at4(ylds, b, q) = make_uint2((uint32_t)YT::from_float(y[0]) | (uint32_t)YT::from_float(y[1]) << 16,
+                                         (uint32_t)YT::from_float(y[2]) | (uint32_t)YT::from_float(y[3]) << 16);
+      }
+    }
+    wave_lds_order();
+    S::template drain<G>(Yout, a.ldo, ow, tw, ylds);
+  });
+}
+// four neighbouring outputs of a token behind the scaling, stored
+template <typename Act>
+__device__ __forceinline__ void finish4(const Finish& f, void* Y, int ydt, int64_t ldy, int64_t t, int64_t o, int64_t c_out, float (&y)[4],
+                                        Act act) {
+  if (o + 3 < c_out) {
+    if (f.bias) {
+      const float4 b = *reinterpret_cast<const float4*>(f.bias + o);
+      y[0] += b.x; y[1] += b.y; y[2] += b.z; y[3] += b.w;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = act(y[e]);
+    if (f.R) {
+      float r[4];
+      load_y4(f.R, ydt, t * f.ldr + o, r);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = f.mul ? y[e] * r[e] : y[e] + r[e];
+    }
+    store_y4(Y, ydt, t * ldy + o, y);
+    return;
+  }
+  for (int e = 0; e < 3; ++e) {
+    if (o + e >= c_out) return;
+    float v = act(f.bias ? y[e] + f.bias[o + e] : y[e]);
+    if (f.R) {
+      const float r = load_y(f.R, ydt, t * f.ldr + o + e);
+      v = f.mul ? v * r : v + r;
+    }
+    store_y1(Y, ydt, t * ldy + o + e, v);
+  }
+}
+#endif
+
 // ---------------------------------------------------------------------------
 // Tile epilogue shared by both kernels; L is the accumulator layout (Acc32 / Acc16).  The block's
 // waves form an NWO x NWT grid; wave (wo, wt) owns output rows [wo*WO, +WO) and tokens
@@ -418,6 +490,32 @@ __device__ __forceinline__ void tile_epilogue(const GemmDev& a, const Acc& acc, 
   constexpr int kStage = WO * L::STG * (WT / L::NTB) * 2;   // bytes of LDS per wave, see Staged
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const float* tsc = a.tok_scale ? a.tok_scale + (int64_t)cand * a.n_tok : nullptr;
+#if defined(__HIP_DEVICE_COMPILE__)
+  if constexpr (EPI >= EPI_FINISH) {      // (one candidate, tokens' steps)
+    constexpr int CLASS = EPI - EPI_FINISH;
+    if constexpr (YLDS) {
+      if (a.odt != TLQ_F32 && (o0 + NWO * WO <= a.c_out) && (t0 + BT <= a.n_tok)) {
+        unsigned char* ylds = reinterpret_cast<unsigned char*>(rows) + wave * kStage;
+        if (a.odt == TLQ_F16) finish_rows_lds<F16, CLASS, L>(a, a.Yout, acc, tsc, o0 + wo * WO, t0 + wt * WT, ylds);
+        else finish_rows_lds<BF16, CLASS, L>(a, a.Yout, acc, tsc, o0 + wo * WO, t0 + wt * WT, ylds);
+        return;
+      }
+    }
+    static_for<0, L::NTB>([&](auto tbc) {
+      constexpr int tb = decltype(tbc)::value;
+      const int64_t t = t0 + wt * WT + L::tok(tb, lane);
+      if (t >= a.n_tok) return;
+      const float sg = tsc[t];
+#pragma unroll
+      for (int q = 0; q < L::NQ; ++q) {
+        float y[4] = {sg * L::get(acc, q, tb, 0), sg * L::get(acc, q, tb, 1), sg * L::get(acc, q, tb, 2), sg * L::get(acc, q, tb, 3)};
+        const int64_t o = o0 + wo * WO + L::row(q, lane);
+        if (o < a.c_out) finish4(a.fin, a.Yout, a.odt, a.ldo, t, o, a.c_out, y, [&](float v) { return act_of<CLASS>(v, a.fin); });
+      }
+    });
+    return;
+  }
+#endif
   if (EPI == EPI_STORE) {
     void* Yo = (unsigned char*)a.Yout + (int64_t)cand * a.o_cand_stride * (a.odt == TLQ_F32 ? 4 : 2);
     if constexpr (YLDS) {
@@ -962,5 +1060,6 @@ hipError_t launch_dma_width(const GemmDev& d, int epi, bool bf16, int tok_blocks
 hipError_t launch_dma_half(const GemmDev& d, int epi, bool bf16, unsigned blocks, hipStream_t stream);
 hipError_t launch_dma_small_tok(const GemmDev& d, bool deep, unsigned blocks, hipStream_t stream);
 hipError_t launch_dma_i8(const GemmDev& d, int epi, GemmTile tile, unsigned blocks, hipStream_t stream);
+hipError_t launch_dma_i8_finish(const GemmDev& d, GemmTile tile, unsigned blocks, hipStream_t stream);      // gemm_i8_finish.hip
 
 }  // namespace tlq

@@ -157,6 +157,7 @@ static GemmDev make_dev(const GemmArgs& g) {
   d.partial = g.partial; d.tok_partial = g.tok_partial;
   d.Yout = g.Yout; d.ldo = g.ldo; d.odt = g.yout_dtype;
   d.row_scale = g.row_scale; d.row_scale_stride = g.row_scale_stride;
+  d.fin = g.fin;
   int64_t to, tt;
   gemm_tile_counts(g.n_tok, g.c_out, g, &to, &tt);
   d.tiles_o = (int)to; d.tiles_t = (int)tt;
@@ -427,6 +428,16 @@ hipError_t launch_gemm_store(const GemmArgs& g, hipStream_t stream) {
   if (g.Yref && (g.yout_dtype != TLQ_F32 || g.n_cand != 1)) return hipErrorInvalidValue;
   const char* name = g.tri ? "gemm_gram" : "gemm_store";
   return g.bf16 ? launch_gemm<BF16, EPI_STORE>(g, name, stream) : launch_gemm<F16, EPI_STORE>(g, name, stream);
+}
+hipError_t launch_gemm_finish(const GemmArgs& g, hipStream_t stream) {
+  if (!g.i8_k || g.n_cand != 1 || g.tri || g.bf16 || !g.tok_scale || g.Yref || (g.small && g.tok_blocks != 0 && g.tok_blocks != 4) || !pipelined_ok(g) ||
+      !g.row_scale || (g.c_in % kDmaBK) != 0)
+    return hipErrorInvalidValue;
+  const GemmDev d = make_dev(g);
+  const int64_t blocks = dev_blocks(d);
+  if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
+  ProfScope ps("gemm_finish", stream, 2.0 * (double)g.n_tok * (double)g.i8_k * (double)g.c_out);
+  return launch_dma_i8_finish(d, g, (unsigned)blocks, stream);
 }
 hipError_t launch_gemm_dot(const GemmArgs& g, hipStream_t stream) {
   // (row strides of 2^21 and more would mean a matrix of 8 TB)

@@ -1,0 +1,221 @@
+// New keys and values into the pages of a 4-bit cache, and what a cache holds as 16-bit rows.
+#include "kv4.h"
+
+namespace tlq {
+
+typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
+
+struct Kv4CacheDev {
+  const uint16_t *K, *V; uint16_t *Ko, *Vo; int64_t ldk, ldv, n_tok;      // rows in, or rows out
+  tlq_kv_batch b; tlq_kv_cache c; Kv4Dev d;      // (c: sizes)
+  int groups;                                     // eights of tokens that a sequence's new ones can lie in
+};
+
+#if defined(__HIP_DEVICE_COMPILE__)
+// A piece of a thread: eight tokens at a multiple of eight, eight channels.  DH / 8 lanes have the channels of a head, four of them
+// a group that shares steps.
+struct Kv4Piece {
+  KvSeq q; int h, d8;          // head, channels 8 d8 and on
+  int64_t p0, row0;            // position of the piece's first token (negative before the sequence), its row (may lie outside the rows)
+  int lo, hi;                  // of its eight tokens those that are rows of the call
+  int id;                      // their page, or -1
+  int in_page;                 // of token 0
+};
+template <int DH>
+__device__ __forceinline__ bool kv4_piece(const Kv4CacheDev& a, Kv4Piece& p) {
+  constexpr int LPH = DH / 8;
+  const int i = (int)(blockIdx.x * 256 + threadIdx.x), s = blockIdx.y;
+  const int u = i / LPH;
+  p.d8 = i % LPH;
+  p.h = u / a.groups;
+  if (p.h >= a.c.n_kv_heads) return false;
+  p.q = kv_sequence(a.b, a.c.page, a.n_tok, s);
+  p.p0 = ((int64_t)(p.q.first >> 3) + u % a.groups) * 8;
+  p.row0 = p.q.row0 + p.p0 - p.q.first;
+  p.lo = p.q.first > p.p0 ? (int)(p.q.first - p.p0) : 0;
+  const int64_t left = (int64_t)p.q.first + p.q.n_new - p.p0;
+  p.hi = left < 8 ? (int)left : 8;
+  if (p.lo >= p.hi) return false;
+  p.in_page = (int)p.p0 & (a.c.page - 1);
+  p.id = p.p0 >= 0 && p.p0 < p.q.len ? kv_page(a.b, a.c, s, (int)p.p0 / a.c.page) : -1;
+  return true;
+}
+__device__ __forceinline__ float finite_abs(float x) { return __builtin_isfinite(x) ? fabsf(x) : 0.0f; }
+// code + 8 in the low bits.  x / step is k + 1/2 exactly or at least 2^-13 away from it: both have few bits (x at least 2^-6 steps: 11
+// and 8).  So the product with the reciprocal, off by 1.5 ulp, is brought to a multiple of 2^-16, which restores the ties
+// and crosses none, and rounded half to even by the addition.
+__device__ __forceinline__ uint32_t kv4_code(float x, float rd) {
+  float q = __builtin_fmaf(x, rd, 192.0f) - 192.0f;
+  q = __builtin_amdgcn_fmed3f(q, -kKv4Top, kKv4Top);
+  q = x != x ? 0.0f : q;
+  return __builtin_bit_cast(uint32_t, q + 12582920.0f) & 15u;      // 1.5 * 2^23 + 8
+}
+#endif
+
+// A token's step for 32 channels is that of its largest value; nothing else has a part in it, so pieces need no meeting but
+// that of four lanes.  V's words hold eight tokens of a channel: a piece has all of them, and takes those that are not new from
+// memory.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void kv4_append_kernel(Kv4CacheDev a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int NG = DH / kKv4Group;
+  Kv4Piece p;
+  if (!kv4_piece<DH>(a, p) || p.id < 0) return;
+  if (p.q.len - p.p0 < p.hi) p.hi = (int)(p.q.len - p.p0);      // (tokens beyond the bounds)
+  if (p.lo >= p.hi) return;
+  const bool val = blockIdx.z != 0;
+  const uint16_t* x = (val ? a.V : a.K) + (int64_t)p.h * DH + p.d8 * 8;
+  const int64_t ld = val ? a.ldv : a.ldk;
+  const int64_t slot = (int64_t)p.id * a.c.n_kv_heads + p.h;
+  u16x8 raw[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    raw[e] = u16x8{0, 0, 0, 0, 0, 0, 0, 0};
+    if (e >= p.lo && e < p.hi) raw[e] = *reinterpret_cast<const u16x8*>(x + (p.row0 + e) * ld);
+  }
+  uint32_t word[8];      // of K: a token's eight channels, of V: a channel's eight tokens
+  uint16_t step[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) word[e] = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float f[8], m = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      f[j] = T::to_float(raw[e][j]);
+      m = fmaxf(m, finite_abs(f[j]));
+    }
+    m = fmaxf(m, __shfl_xor(m, 1, 64));
+    m = fmaxf(m, __shfl_xor(m, 2, 64));
+    const float wide = BF16::to_float(BF16::from_float(fmaxf(m, kRangeFloor) / kKv4Top));
+    step[e] = F16::from_float(fminf(wide, kKv4Most));
+    const float rd = __builtin_amdgcn_rcpf(F16::to_float(step[e]));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t n = kv4_code(f[j], rd);
+      if (val) word[j] |= n << kv4_shift(e);
+      else word[e] |= n << kv4_shift(j);
+    }
+  }
+  const bool first = (p.d8 & 3) == 0;
+  if (!val) {
+    const int64_t token = slot * a.c.page + p.in_page;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (e < p.lo || e >= p.hi) continue;
+      a.d.k[(token + e) * (DH / 8) + p.d8] = word[e];
+      if (first) a.d.k_step[(token + e) * NG + p.d8 / 4] = step[e];
+    }
+    return;
+  }
+  uint32_t* to = a.d.v + ((slot * DH + p.d8 * 8) * a.c.page + p.in_page) / 8;
+  uint16_t* at = a.d.v_step + (slot * NG + p.d8 / 4) * a.c.page + p.in_page;
+  const bool whole = p.lo == 0 && p.hi == 8;
+  uint32_t mask = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) mask |= e >= p.lo && e < p.hi ? 15u << kv4_shift(e) : 0u;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int64_t row = (int64_t)j * (a.c.page / 8);
+    to[row] = whole ? word[j] : (to[row] & ~mask) | (word[j] & mask);
+  }
+  if (first) {
+    if (whole) {
+      *reinterpret_cast<u16x8*>(at) = u16x8{step[0], step[1], step[2], step[3], step[4], step[5], step[6], step[7]};
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e >= p.lo && e < p.hi) at[e] = step[e];
+    }
+  }
+#endif
+}
+
+// The other way.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void kv4_read_kernel(Kv4CacheDev a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int NG = DH / kKv4Group;
+  Kv4Piece p;
+  if (!kv4_piece<DH>(a, p)) return;
+  const bool val = blockIdx.z != 0 || !a.Ko;
+  uint16_t* x = (val ? a.Vo : a.Ko) + (int64_t)p.h * DH + p.d8 * 8;
+  const int64_t ld = val ? a.ldv : a.ldk;
+  const int64_t slot = (int64_t)(p.id < 0 ? 0 : p.id) * a.c.n_kv_heads + p.h;
+  const int there = p.id < 0 ? 0 : p.q.len - p.p0 < 8 ? (int)(p.q.len - p.p0) : 8;      // tokens of the eight that there are
+  uint32_t word[8];
+  uint16_t step[8];
+  if (!val) {
+    const int64_t token = slot * a.c.page + p.in_page;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      word[e] = a.d.k[(token + e) * (DH / 8) + p.d8];
+      step[e] = a.d.k_step[(token + e) * NG + p.d8 / 4];
+    }
+  } else {
+    const uint32_t* from = a.d.v + ((slot * DH + p.d8 * 8) * a.c.page + p.in_page) / 8;
+    const u16x8 s = *reinterpret_cast<const u16x8*>(a.d.v_step + (slot * NG + p.d8 / 4) * a.c.page + p.in_page);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      word[j] = from[(int64_t)j * (a.c.page / 8)];
+      step[j] = s[j];
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if (e < p.lo || e >= p.hi) continue;
+    const float st = F16::to_float(step[e]);
+    uint16_t o[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t n = val ? word[j] >> kv4_shift(e) : word[e] >> kv4_shift(j);
+      o[j] = e < there ? T::from_float((float)((int)(n & 15u) - 8) * st) : 0;
+    }
+    *reinterpret_cast<u16x8*>(x + (p.row0 + e) * ld) = u16x8{o[0], o[1], o[2], o[3], o[4], o[5], o[6], o[7]};
+  }
+#endif
+}
+
+static dim3 kv4_cache_grid(const Kv4CacheDev& a, unsigned z) {
+  return dim3((unsigned)ceil_div((int64_t)a.c.n_kv_heads * a.groups * (a.c.head_dim / 8), 256), (unsigned)a.b.n_seq, z);
+}
+int64_t kv4_cache_groups(int64_t n_tok, const tlq_kv_batch& b) {
+  const int64_t most = b.max_new < n_tok ? b.max_new : n_tok;
+  return (most - 1 + 7) / 8 + 1;
+}
+
+hipError_t launch_kv4_append(const void* K, int64_t ldk, const void* V, int64_t ldv, int64_t n_tok, const tlq_kv_batch& b,
+                             const tlq_kv4_cache& c, bool bf16, hipStream_t stream) {
+  ProfScope ps("kv4_append", stream, 5.125 * (double)n_tok * c.n_kv_heads * c.head_dim);
+  Kv4CacheDev a{};
+  a.K = (const uint16_t*)K; a.V = (const uint16_t*)V; a.ldk = ldk; a.ldv = ldv; a.n_tok = n_tok;
+  a.b = b; a.c = kv4_sizes(c); a.d = {c.k, c.k_step, c.v, c.v_step};
+  a.groups = (int)kv4_cache_groups(n_tok, b);
+  const dim3 grid = kv4_cache_grid(a, 2);
+  auto pick = [&](auto t) {
+    using T = decltype(t);
+    if (c.head_dim == 128) kv4_append_kernel<T, 128><<<grid, 256, 0, stream>>>(a);
+    else kv4_append_kernel<T, 64><<<grid, 256, 0, stream>>>(a);
+  };
+  bf16 ? pick(BF16{}) : pick(F16{});
+  return hipGetLastError();
+}
+
+hipError_t launch_kv4_read(void* K, int64_t ldk, void* V, int64_t ldv, int64_t n_tok, const tlq_kv_batch& b, const tlq_kv4_cache& c,
+                           bool bf16, hipStream_t stream) {
+  ProfScope ps("kv4_read", stream, (K && V ? 5.125 : 2.5625) * (double)n_tok * c.n_kv_heads * c.head_dim);
+  Kv4CacheDev a{};
+  a.Ko = (uint16_t*)K; a.Vo = (uint16_t*)V; a.ldk = ldk; a.ldv = ldv; a.n_tok = n_tok;
+  a.b = b; a.c = kv4_sizes(c); a.d = {c.k, c.k_step, c.v, c.v_step};
+  a.groups = (int)kv4_cache_groups(n_tok, b);
+  const dim3 grid = kv4_cache_grid(a, K && V ? 2 : 1);
+  auto pick = [&](auto t) {
+    using T = decltype(t);
+    if (c.head_dim == 128) kv4_read_kernel<T, 128><<<grid, 256, 0, stream>>>(a);
+    else kv4_read_kernel<T, 64><<<grid, 256, 0, stream>>>(a);
+  };
+  bf16 ? pick(BF16{}) : pick(F16{});
+  return hipGetLastError();
+}
+
+}  // namespace tlq

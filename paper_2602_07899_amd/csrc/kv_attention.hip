@@ -19,57 +19,13 @@
 // fp16; bf16 queries are multiplied with the power of two that brings the largest of the row to [2^14, 2^15).
 // The products are transposed, S^T = K Q^T and O^T = V^T P^T, so that a lane owns one query column and P stays in
 // registers; values are stored channel by channel so that V^T's rows are read as they lie.
-#include <type_traits>
-
-#include "kv.h"
+#include "kv_attention.h"
 
 namespace tlq {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
-
-// r / d for 0 <= r < 2^31, 1 <= d < 2^31, as a product (Granlund and Montgomery, 1994): m = ceil(2^(31+s) / d), s = ceil(log2 d)
-struct KvDiv {
-  uint32_t m, s, d;
-  __device__ __forceinline__ uint32_t of(uint32_t r) const { return __umulhi(r << 1, m) >> s; }
-};
-static KvDiv kv_div(uint32_t d) {
-  uint32_t s = 0;
-  while ((1ull << s) < d) ++s;
-  return {(uint32_t)(((1ull << (31 + s)) + d - 1) / d), s, d};
-}
-
-struct KvAttnDev {
-  const uint16_t* Q; int64_t ldq, n_tok; int n_heads, group; KvDiv by_group; float scale2;    // scale * log2(e)
-  tlq_kv_batch b; tlq_kv_cache c; int page_bits;
-  uint16_t* Out; int64_t ldo;
-  int n_splits, chunk;          // keys of a split
-  // kv_prompt_kernel: row tiles; pairs of sequence and key head, blocks of a pair, and of the pairs that an XCD has to itself
-  int tiles; uint32_t n_pairs, own_blocks, together_bits; KvDiv by_heads, by_work;
-  float2* ml; float* acc;       // per (row, head, split): reference and sum; [head_dim] sums of codes
-};
-
-template <int I, int N, typename Fn>
-__device__ __forceinline__ void static_for(Fn&& f) {
-  if constexpr (I < N) {
-    f(std::integral_constant<int, I>{});
-    static_for<I + 1, N>(f);
-  }
-}
-
 #if defined(__HIP_DEVICE_COMPILE__)
 constexpr float kSmallStep = 1e-30f;    // (a step of zero: its page's values count as zeros, its keys in the sum as ever)
-constexpr float kTop = 7.0f, kRaise = 15.0f;      // exponents of the largest weight: when the reference is set, at most
 constexpr float kNear = 3.0f, kLow = 7.0f;        // binary orders below the reference's step, below a weight of one (see above)
-// sum of eight weights (rounded already) and c
-__device__ __forceinline__ float add_weights(f16x8 w, float c) {
-  const f16x2 one = {(_Float16)1.0f, (_Float16)1.0f};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_fdot2(f16x2{w[2 * i], w[2 * i + 1]}, one, c, false);
-  return c;
-}
 // four codes -> four halves: byte + 128 behind the exponent of 1024, less 1152
 __device__ __forceinline__ void widen_codes(uint32_t w, uint32_t& lo, uint32_t& hi) {
   w ^= 0x80808080u;
@@ -82,79 +38,6 @@ __device__ __forceinline__ f16x8 widen_codes8(uint32_t a, uint32_t b) {
   widen_codes(a, v.x, v.y);
   widen_codes(b, v.z, v.w);
   return __builtin_bit_cast(f16x8, v);
-}
-// the largest of a value that lane ^ 16 and lane ^ 32 hold (as in block.hip: the builtins' two results come out as one; the wait
-// states are what the swaps need behind the write of an operand)
-__device__ __forceinline__ float column_max(float v) {
-  float a = v, b = v;
-  asm("s_nop 1\n\tv_permlane16_swap_b32 %0, %1" : "+v"(a), "+v"(b));
-  a = b = fmaxf(a, b);
-  asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(a), "+v"(b));
-  return fmaxf(a, b);
-}
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
-// A denominator times 2^d, d <= 0.  Steps of values may lie further apart than floats have exponents: where 2^d has none left the
-// denominator takes the way in two.  With f = 2^d at hand where a launch is a chain of few of them (1200 keys x 32 9.9 us, the other
-// form 10.0), without a branch between the products of prompts (16 of up to 1200 tokens 343 us, the other form 348).
-__device__ __forceinline__ float lower_sum(float l, float d, float f) {
-  const bool far = l != 0.0f && d < -100.0f;
-  float r = l * f;
-  if (__builtin_expect(__any(far), 0)) r = far ? l * 0x1p-100f * exp2_fast(d + 100.0f) : r;
-  return r;
-}
-__device__ __forceinline__ float lower_sum(float l, float d) {
-  const float c = fmaxf(d, -100.0f);
-  return l * exp2_fast(c) * exp2_fast(d - c);      // (the last is one down to there)
-}
-
-// A query with an infinity or NaN is not to end as a row without keys (all of its scores -inf, or none above the maximum so far):
-// a lane that holds such a number makes a NaN of it, and with it the products with every key.
-template <int N>
-__device__ __forceinline__ void mark_queries(f16x8 (&qf)[N]) {
-  const f16x2 zero = {(_Float16)0.0f, (_Float16)0.0f};
-  float t = 0.0f;
-#pragma unroll
-  for (int i = 0; i < N; ++i)
-#pragma unroll
-    for (int e = 0; e < 8; e += 2) t = __builtin_amdgcn_fdot2(f16x2{qf[i][e], qf[i][e + 1]}, zero, t, false);
-  qf[0][0] = t == t ? qf[0][0] : (_Float16)t;
-}
-// A lane's channels of its query as halves, eight at a time and STEP apart (negated if asked); the factor that undoes their
-// prescale.  Lanes lane ^ 16 and lane ^ 32 hold the other channels of the same query.
-template <typename T, int N, int STEP>
-__device__ __forceinline__ float load_queries(const uint16_t* p, f16x8 (&qf)[N], bool negate) {
-  u16x8 raw[N];
-  const unsigned short sign = negate ? 0x8000 : 0;
-#pragma unroll
-  for (int i = 0; i < N; ++i) raw[i] = *reinterpret_cast<const u16x8*>(p + STEP * i) ^ sign;
-  if constexpr (std::is_same<T, F16>::value) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) qf[i] = __builtin_bit_cast(f16x8, raw[i]);
-    mark_queries(qf);
-    return 1.0f;
-  }
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < N; ++i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t a = raw[i][e] & 0x7fffu;
-      top = a > top ? a : top;
-    }
-  for (int off = 16; off <= 32; off <<= 1) {
-    const uint32_t o = (uint32_t)__shfl_xor((int)top, off, 64);
-    top = o > top ? o : top;
-  }
-  // exponent field of the largest -> 127 + 14; rows of zeros and subnormals keep factors that are finite, infinities stay
-  int k = 141 - (int)(top >> 7);
-  k = k > 126 ? 126 : k;
-  const float up = __builtin_bit_cast(float, (uint32_t)(127 + k) << 23);
-#pragma unroll
-  for (int i = 0; i < N; ++i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) qf[i][e] = (_Float16)(BF16::to_float(raw[i][e]) * up);
-  mark_queries(qf);
-  return __builtin_bit_cast(float, (uint32_t)(127 - k) << 23);
 }
 #endif
 
@@ -762,8 +645,6 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnDev a, uint32_t tile
 // 30, 100 x 32 with four rows a token (800) 11.9 11.0.
 constexpr int64_t kFewWork = 1536;
 
-namespace {
-struct KvPlan { bool prompt; int rows, tiles, n_splits, chunk; size_t acc_at, bytes; };
 KvPlan kv_plan(int64_t n_tok, int n_heads, const tlq_kv_batch& b, const tlq_kv_cache& c) {
   KvPlan p;
   const int group = n_heads / c.n_kv_heads;
@@ -801,22 +682,20 @@ KvPlan kv_plan(int64_t n_tok, int n_heads, const tlq_kv_batch& b, const tlq_kv_c
   p.bytes = p.n_splits > 1 ? p.acc_at + align_up((size_t)n_tok * n_heads * p.n_splits * c.head_dim * sizeof(float), 256) : 0;
   return p;
 }
-}  // namespace
 
 size_t kv_attention_workspace(int64_t n_tok, int n_heads, const tlq_kv_batch& b, const tlq_kv_cache& c) {
   return kv_plan(n_tok, n_heads, b, c).bytes;
 }
 
-hipError_t launch_kv_attention(const void* Q, int64_t ldq, int64_t n_tok, int n_heads, float scale, const tlq_kv_batch& b,
-                               const tlq_kv_cache& c, bool bf16, void* Out, int64_t ldo, void* workspace, hipStream_t stream) {
-  const KvPlan p = kv_plan(n_tok, n_heads, b, c);
+// What a launch's kernels read besides the cache's codes (c: its sizes are), and its grid.
+KvAttnDev kv_attn_dev(const KvPlan& p, const void* Q, int64_t ldq, int64_t n_tok, int n_heads, float scale, const tlq_kv_batch& b,
+                      const tlq_kv_cache& c, void* Out, int64_t ldo, void* workspace, dim3* grid) {
   KvAttnDev a{};
   a.Q = (const uint16_t*)Q; a.ldq = ldq; a.n_tok = n_tok; a.n_heads = n_heads; a.group = n_heads / c.n_kv_heads;
   a.scale2 = scale * 1.4426950408889634f;
   a.b = b; a.c = c; a.page_bits = __builtin_ctz((unsigned)c.page);
   a.Out = (uint16_t*)Out; a.ldo = ldo; a.n_splits = p.n_splits; a.chunk = p.chunk;
   a.ml = (float2*)workspace; a.acc = (float*)((unsigned char*)workspace + p.acc_at);
-  const int64_t most = b.max_new < n_tok ? b.max_new : n_tok;
   a.tiles = p.tiles;
   a.by_group = kv_div((uint32_t)a.group);
   a.by_heads = kv_div((uint32_t)c.n_kv_heads);
@@ -832,8 +711,34 @@ hipError_t launch_kv_attention(const void* Q, int64_t ldq, int64_t n_tok, int n_
   for (a.together_bits = 0; a.together_bits < 3 && (16 << a.together_bits) <= n_pairs && work << a.together_bits < 64; ++a.together_bits) {}
   const int64_t blocks = 8 * ((int64_t)a.own_blocks + ceil_div(n_pairs % 8 * work, 8));
   const int64_t gx = blocks < (1 << 20) ? blocks : (1 << 20);
-  const dim3 grid = p.prompt ? dim3((unsigned)gx, (unsigned)ceil_div(blocks, gx))
+  *grid = p.prompt ? dim3((unsigned)gx, (unsigned)ceil_div(blocks, gx))
                              : dim3((unsigned)work, (unsigned)c.n_kv_heads, (unsigned)b.n_seq);
+  return a;
+}
+
+// The joining of a launch's splits into Out.
+hipError_t launch_kv_join(const KvPlan& p, const KvAttnDev& a, bool bf16, hipStream_t stream) {
+  const int64_t most = a.b.max_new < a.n_tok ? a.b.max_new : a.n_tok;
+  ProfScope ps("kv_join", stream, 4.0 * (double)a.n_tok * a.n_heads * p.n_splits * a.c.head_dim);
+  auto pick = [&](auto t, auto dh) {
+    using T = decltype(t);
+    constexpr int DH = decltype(dh)::value;
+    if (p.n_splits <= 64)
+      kv_join_few_kernel<T, DH><<<dim3((unsigned)most, (unsigned)ceil_div(a.n_heads, 4), (unsigned)a.b.n_seq), 256, 0, stream>>>(a, (uint32_t)p.rows);
+    else kv_join_kernel<T, DH><<<dim3((unsigned)most, (unsigned)a.n_heads, (unsigned)a.b.n_seq), 256, 0, stream>>>(a, (uint32_t)p.rows);
+    return hipGetLastError();
+  };
+  using W128 = std::integral_constant<int, 128>;
+  using W64 = std::integral_constant<int, 64>;
+  if (a.c.head_dim == 128) return bf16 ? pick(BF16{}, W128{}) : pick(F16{}, W128{});
+  return bf16 ? pick(BF16{}, W64{}) : pick(F16{}, W64{});
+}
+
+hipError_t launch_kv_attention(const void* Q, int64_t ldq, int64_t n_tok, int n_heads, float scale, const tlq_kv_batch& b,
+                               const tlq_kv_cache& c, bool bf16, void* Out, int64_t ldo, void* workspace, hipStream_t stream) {
+  const KvPlan p = kv_plan(n_tok, n_heads, b, c);
+  dim3 grid;
+  const KvAttnDev a = kv_attn_dev(p, Q, ldq, n_tok, n_heads, scale, b, c, Out, ldo, workspace, &grid);
   auto pick = [&](auto t, auto dh) {
     using T = decltype(t);
     constexpr int DH = decltype(dh)::value;
@@ -843,11 +748,7 @@ hipError_t launch_kv_attention(const void* Q, int64_t ldq, int64_t n_tok, int n_
       else kv_few_kernel<T, DH><<<grid, 256, 0, stream>>>(a);
     }
     if (hipError_t e = hipGetLastError(); e != hipSuccess || p.n_splits == 1) return e;
-    ProfScope ps("kv_join", stream, 4.0 * (double)n_tok * n_heads * p.n_splits * c.head_dim);
-    if (p.n_splits <= 64)
-      kv_join_few_kernel<T, DH><<<dim3((unsigned)most, (unsigned)ceil_div(n_heads, 4), (unsigned)b.n_seq), 256, 0, stream>>>(a, (uint32_t)p.rows);
-    else kv_join_kernel<T, DH><<<dim3((unsigned)most, (unsigned)n_heads, (unsigned)b.n_seq), 256, 0, stream>>>(a, (uint32_t)p.rows);
-    return hipGetLastError();
+    return launch_kv_join(p, a, bf16, stream);
   };
   using W128 = std::integral_constant<int, 128>;
   using W64 = std::integral_constant<int, 64>;

@@ -7,10 +7,15 @@ namespace tlq {
 
 #if defined(__HIP_DEVICE_COMPILE__)
 // four neighbouring outputs of a token
+template <bool FIN>
 __device__ __forceinline__ void write4(const LinearI8Args& a, int64_t t, int64_t o, float st, const i32x4& s) {
   float y[4];
 #pragma unroll
   for (int r = 0; r < 4; ++r) y[r] = o + r < a.c_out ? st * (a.ws[o + r] * (float)s[r]) : 0.0f;
+  if constexpr (FIN) {
+    if (o < a.c_out) finish4(a.fin, a.Y, a.ydt, a.ldy, t, o, a.c_out, y, [&](float v) { return act_of(v, a.fin); });
+    return;
+  }
   if (o + 3 < a.c_out) store_y4(a.Y, a.ydt, t * a.ldy + o, y);
   else
     for (int r = 0; r < 3; ++r)
@@ -24,7 +29,7 @@ __device__ __forceinline__ void write4(const LinearI8Args& a, int64_t t, int64_t
 // before the sums.
 // Bound by the bytes of the weights, every one is read once per 16 NT tokens, and by latency where they are few: 1 x 4096 x 4096
 // 5.4 us, 3.1 TB/s.
-template <int NT, int NW>
+template <int NT, int NW, bool FIN>
 __global__ __launch_bounds__(NW * 64) void linear_few_kernel(LinearI8Args a) {
 #if defined(__HIP_DEVICE_COMPILE__)
   __shared__ __attribute__((aligned(16))) i32x4 red[NW][NT][64];
@@ -73,7 +78,7 @@ __global__ __launch_bounds__(NW * 64) void linear_few_kernel(LinearI8Args a) {
 #pragma unroll
   for (int v = 1; v < NW; ++v) s += red[v][wave][lane];
   const int64_t t = t0 + wave * 16 + l16;
-  if (t < a.n_tok) write4(a, t, o0 + fq * 4, a.xs[t], s);
+  if (t < a.n_tok) write4<FIN>(a, t, o0 + fq * 4, a.xs[t], s);
 #endif
 }
 
@@ -81,10 +86,14 @@ hipError_t launch_linear_few(const LinearI8Args& a, hipStream_t stream) {
   ProfScope ps("linear_few", stream, (double)a.c_out * (double)a.K);
   const unsigned bo = (unsigned)ceil_div(a.c_out, 16);
   auto go = [&](auto kern, int waves, int tokens) { kern<<<dim3(bo, (unsigned)ceil_div(a.n_tok, tokens)), waves * 64, 0, stream>>>(a); };
-  if (a.n_tok <= 16) go(linear_few_kernel<1, 16>, 16, 16);
-  else if (a.n_tok <= 32) go(linear_few_kernel<2, 16>, 16, 32);
-  else if (a.n_tok <= 48) go(linear_few_kernel<3, 16>, 16, 48);
-  else go(linear_few_kernel<4, 16>, 16, 64);
+  auto pick = [&](auto fin) {
+    constexpr bool FIN = decltype(fin)::value;
+    if (a.n_tok <= 16) go(linear_few_kernel<1, 16, FIN>, 16, 16);
+    else if (a.n_tok <= 32) go(linear_few_kernel<2, 16, FIN>, 16, 32);
+    else if (a.n_tok <= 48) go(linear_few_kernel<3, 16, FIN>, 16, 48);
+    else go(linear_few_kernel<4, 16, FIN>, 16, 64);
+  };
+  a.finish ? pick(std::true_type{}) : pick(std::false_type{});
   return hipGetLastError();
 }
 
@@ -97,7 +106,7 @@ hipError_t launch_linear_few(const LinearI8Args& a, hipStream_t stream) {
 // a half stages a block, so the first loads and the meeting count), and 4.0 for the sums of eight parts.  Weights two stages
 // ahead instead of one: calls of 48 x 11008 x 4096 23.1 25.4, 64 x 4096 x 11008 24.3 26.6.
 constexpr int kMidStage = 512;
-template <int NT>
+template <int NT, bool FIN>
 __global__ __launch_bounds__(512) void linear_mid_kernel(LinearI8Args a, int splits, int* __restrict__ partial) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int ROWS = 16 * NT, PER = ROWS * kMidStage / 16 / 512;      // 16-byte pieces of a stage for a thread
@@ -198,12 +207,13 @@ __global__ __launch_bounds__(512) void linear_mid_kernel(LinearI8Args a, int spl
         if (o < a.c_out) *reinterpret_cast<i32x4*>(partial + ((int64_t)part * a.n_tok + t) * ((a.c_out + 3) & ~(int64_t)3) + o) = s;
         continue;
       }
-      write4(a, t, o, a.xs[t], s);
+      write4<FIN>(a, t, o, a.xs[t], s);
     }
   }
 #endif
 }
 
+template <bool FIN>
 __global__ __launch_bounds__(256) void linear_join_kernel(LinearI8Args a, int splits, const int* __restrict__ partial) {
 #if defined(__HIP_DEVICE_COMPILE__)
   const int64_t quads = (a.c_out + 3) >> 2, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -212,7 +222,7 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinearI8Args a, int sp
   i32x4 s = *reinterpret_cast<const i32x4*>(partial + i * 4);
 #pragma unroll 8
   for (int p = 1; p < splits; ++p) s += *reinterpret_cast<const i32x4*>(partial + ((int64_t)p * a.n_tok * quads + i) * 4);
-  write4(a, t, (i - t * quads) * 4, a.xs[t], s);
+  write4<FIN>(a, t, (i - t * quads) * 4, a.xs[t], s);
 #endif
 }
 
@@ -252,14 +262,20 @@ hipError_t launch_linear_mid(const LinearI8Args& a, int splits, int* partial, hi
     auto go = [&](auto kern, int tokens) {
       kern<<<dim3((unsigned)ceil_div(a.c_out, 128), (unsigned)ceil_div(a.n_tok, tokens), (unsigned)splits), 512, 0, stream>>>(a, splits, partial);
     };
-    if (a.n_tok <= 16) go(linear_mid_kernel<1>, 16);
-    else if (a.n_tok <= 32) go(linear_mid_kernel<2>, 32);
-    else if (a.n_tok <= 48) go(linear_mid_kernel<3>, 48);
-    else go(linear_mid_kernel<4>, 64);
+    auto pick = [&](auto fin) {
+      constexpr bool FIN = decltype(fin)::value;
+      if (a.n_tok <= 16) go(linear_mid_kernel<1, FIN>, 16);
+      else if (a.n_tok <= 32) go(linear_mid_kernel<2, FIN>, 32);
+      else if (a.n_tok <= 48) go(linear_mid_kernel<3, FIN>, 48);
+      else go(linear_mid_kernel<4, FIN>, 64);
+    };
+    a.finish && splits == 1 ? pick(std::true_type{}) : pick(std::false_type{});      // (of several parts the join does it)
   }
   if (hipError_t e = hipGetLastError(); e != hipSuccess || splits == 1) return e;
   ProfScope ps("linear_join", stream, 4.0 * splits * (double)a.n_tok * (double)a.c_out);
-  linear_join_kernel<<<(unsigned)ceil_div(a.n_tok * ((a.c_out + 3) >> 2), 256), 256, 0, stream>>>(a, splits, partial);
+  const unsigned blocks = (unsigned)ceil_div(a.n_tok * ((a.c_out + 3) >> 2), 256);
+  if (a.finish) linear_join_kernel<true><<<blocks, 256, 0, stream>>>(a, splits, partial);
+  else linear_join_kernel<false><<<blocks, 256, 0, stream>>>(a, splits, partial);
   return hipGetLastError();
 }
 

@@ -55,7 +55,8 @@ __device__ __forceinline__ float half_head(float v, bool upper) {
 // - 351 under the profiler, 4.8 - 5.0 TB/s where a copy of as many bytes reaches 3.9 - 5.1; by latency for few tokens: 16 x 40
 // heads 5.0 us.
 enum { kHalfHead, kHalfRot, kNeighbours };
-template <typename T, int DH, int FORM>
+// AXES: a token has up to four positions and a frequency turns by that of its axis.
+template <typename T, int DH, int FORM, bool AXES>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkRopeArgs a, int wpt, bool nts) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int LPH = DH / 8, HPW = 64 / LPH;
@@ -67,8 +68,18 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkRopeArgs a, int wpt
   if (t >= a.n_tok) return;                       // (no barrier below)
   const int half = a.rot >> 1;
   {
-    const double p = (double)a.pos[t];
+    double p = 0.0;
+    int at[4];
+    if constexpr (!AXES) p = (double)a.pos[t];
+    else {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) at[x] = a.pos[(x < a.n_axes ? x : 0) * a.ld_pos + t];
+    }
     for (int i = lane; i < half; i += 64) {
+      if constexpr (AXES) {
+        const int x = a.axis[i];
+        p = (double)(x <= 0 ? at[0] : x == 1 || a.n_axes == 2 ? at[1] : x == 2 || a.n_axes == 3 ? at[2] : at[3]);
+      }
       double turns = p * a.inv_freq[i] * 0.15915494309189535;
       turns -= __builtin_rint(turns);
       float s, c;
@@ -188,9 +199,13 @@ hipError_t launch_qk_norm_rope(const QkRopeArgs& a, hipStream_t stream) {
   auto form = [&](auto t, auto dh) {
     using T = decltype(t);
     constexpr int DH = decltype(dh)::value;
-    if (a.interleaved) go(qk_norm_rope_kernel<T, DH, kNeighbours>);
-    else if (a.rot == DH) go(qk_norm_rope_kernel<T, DH, kHalfHead>);
-    else go(qk_norm_rope_kernel<T, DH, kHalfRot>);
+    auto axes = [&](auto many) {
+      constexpr bool AXES = decltype(many)::value;
+      if (a.interleaved) go(qk_norm_rope_kernel<T, DH, kNeighbours, AXES>);
+      else if (a.rot == DH) go(qk_norm_rope_kernel<T, DH, kHalfHead, AXES>);
+      else go(qk_norm_rope_kernel<T, DH, kHalfRot, AXES>);
+    };
+    a.axis && a.n_axes > 1 ? axes(std::true_type{}) : axes(std::false_type{});
   };
   auto width = [&](auto t) {
     if (a.head_dim == 64) form(t, std::integral_constant<int, 64>{});

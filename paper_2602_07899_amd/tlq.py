@@ -16,6 +16,7 @@ LIB_PATH = os.path.join(_HERE, "libtlq.so")
 
 OK, ERR_NULL, ERR_SHAPE, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_ALIGN, ERR_LAUNCH = range(7)
 F16, BF16, F32 = 0, 1, 2
+ACT_NONE, ACT_SILU, ACT_GELU_TANH, ACT_GELU_ERF = range(4)
 MAX_ALPHA = 64
 
 
@@ -42,6 +43,11 @@ class KvBatch(C.Structure):
                 ("max_len", C.c_int32), ("reserved", C.c_int32)]
 
 
+class Kv4Cache(C.Structure):
+    """tlq_kv4_cache; made by kv4_cache()."""
+    _fields_ = KvCache._fields_
+
+
 class TlqError(RuntimeError):
     def __init__(self, status, where):
         self.status = status
@@ -58,6 +64,7 @@ _PP = C.POINTER(Params)
 _F = C.c_float
 _PB = C.POINTER(KvBatch)
 _PC = C.POINTER(KvCache)
+_PC4 = C.POINTER(Kv4Cache)
 
 _SIGNATURES = {
     "tlq_status_string": (C.c_char_p, [C.c_int]),
@@ -103,6 +110,15 @@ _SIGNATURES = {
     "tlq_kv_append": (C.c_int, [_P, _I64, _P, _I64, _I64, _PB, _PC, _PP, _P]),
     "tlq_kv_attention_workspace_bytes": (_SZ, [_I64, _I32, _PB, _PC]),
     "tlq_kv_attention": (C.c_int, [_P, _I64, _I64, _I32, _F, _PB, _PC, _PP, _P, _I64, _P, _SZ, _P]),
+    "tlq_add_norm_codes": (C.c_int, [_P, _I64, _P, _I64, _I64, _I64, _P, _F, _I32, _PP, _P, _I64, _P, _I64, _P, _P]),
+    "tlq_linear_codes_workspace_bytes": (_SZ, [_I64, _I64]),
+    "tlq_linear_codes": (C.c_int, [_P, _I64, _P, _I64, _I64, _P, _I64, _I64, _P, _P, _I32, _P, _I64, _I32, _PP, _P, _I64, _P, _SZ, _P]),
+    "tlq_qk_norm_rope_axes": (C.c_int, [_P, _I64, _I32, _P, _I64, _I32, _I64, _I32, _I32, _I32, _I32, _F, _P, _P, _P, _I64, _I32, _P, _P,
+                                        _PP, _P, _I64, _P, _I64, _P]),
+    "tlq_kv4_append": (C.c_int, [_P, _I64, _P, _I64, _I64, _PB, _PC4, _PP, _P]),
+    "tlq_kv4_read": (C.c_int, [_PB, _PC4, _PP, _I64, _P, _I64, _P, _I64, _P]),
+    "tlq_kv4_attention_workspace_bytes": (_SZ, [_I64, _I32, _PB, _PC4]),
+    "tlq_kv4_attention": (C.c_int, [_P, _I64, _I64, _I32, _F, _PB, _PC4, _PP, _P, _I64, _P, _SZ, _P]),
     "tlq_selftest_tile_map": (C.c_int64, [_I64, _I64, _I64, _I32, C.POINTER(C.c_int64)]),
     "tlq_profile_enable": (C.c_int, [C.c_int]),
     "tlq_profile_enabled": (C.c_int, []),
@@ -573,6 +589,144 @@ def kv_attention(Q, n_heads, batch, cache, p, Out, scale=0.0, workspace=None):
     _shape(ws.get_device() == here, "workspace: not on the current device")
     _check(lib().tlq_kv_attention(Q.data_ptr(), _rows(Q, "Q"), n, n_heads, scale, C.byref(batch), C.byref(cache), C.byref(p),
                                   Out.data_ptr(), _rows(Out, "Out"), ws.data_ptr(), ws.numel(), _stream_of(here)), "tlq_kv_attention")
+    return Out
+
+
+# ------------------------------------------------------------------ the block's other calls in low bits, a cache in 4 bits
+def add_norm_codes(H, w, p, codes, steps, Z=None, H_out=None, eps=1e-6, bits=8):
+    """h = H + Z (into H_out if given), the rows of h normalised, times w (None: ones), as signed codes (int8 [n, >= c rounded up
+    to 128]) and steps (float [n])."""
+    ty, here = _types(), _current(H)
+    x = ty.of[p.x_dtype]
+    for t, want, name in ((H, x, "H"), (Z, x, "Z"), (H_out, x, "H_out"), (w, ty.f32, "w"), (codes, ty.i8, "codes"), (steps, ty.f32, "steps")):
+        if t is not None and (t.dtype is not want or t.get_device() != here):
+            _wrong(t, want, name, here)
+    n, c = _size(H, "H")
+    ldc = _rows(codes, "codes")
+    _shape((Z is None or Z.shape == (n, c)) and (H_out is None or H_out.shape == (n, c)), "H, Z and H_out: of one shape")
+    _shape(codes.size(0) == n and ldc >= codes.size(1) >= -(-c // 128) * 128, "codes: n rows, zeros behind c up to a multiple of 128")
+    _shape(steps.numel() == n and steps.is_contiguous(), "steps: one a row")
+    _shape(w is None or w.numel() == c and w.is_contiguous(), "w: one a channel")
+    _check(lib().tlq_add_norm_codes(H.data_ptr(), _rows(H, "H"), None if Z is None else Z.data_ptr(), 0 if Z is None else _rows(Z, "Z"), n, c,
+                                    None if w is None else w.data_ptr(), eps, bits, C.byref(p), None if H_out is None else H_out.data_ptr(),
+                                    0 if H_out is None else _rows(H_out, "H_out"), codes.data_ptr(), ldc, steps.data_ptr(),
+                                    _stream_of(here)), "tlq_add_norm_codes")
+
+
+def linear_codes_workspace_bytes(n_tok, c_in):
+    return int(lib().tlq_linear_codes_workspace_bytes(n_tok, c_in))
+
+
+def linear_codes(codes, steps, c_in, w_codes, w_steps, p, Y, bias=None, act=ACT_NONE, R=None, mul=False, workspace=None):
+    """Y = act(step_t * step_o * codes . w_codes^T + bias) + R, or * R with mul; codes and w_codes with zeros behind c_in up to a
+    multiple of 128."""
+    ty, here = _types(), _current(codes)
+    y = ty.of[p.yref_dtype]
+    for t, want, name in ((codes, ty.i8, "codes"), (steps, ty.f32, "steps"), (w_codes, ty.i8, "w_codes"), (w_steps, ty.f32, "w_steps"),
+                          (Y, y, "Y"), (bias, ty.f32, "bias"), (R, y, "R")):
+        if t is not None and (t.dtype is not want or t.get_device() != here):
+            _wrong(t, want, name, here)
+    (n, have), (co, wide) = _size(codes, "codes"), _size(w_codes, "w_codes")
+    _shape(have >= -(-c_in // 128) * 128 and wide >= -(-c_in // 128) * 128, "codes, w_codes: rows with zeros behind c_in up to a multiple of 128")
+    _shape(steps.numel() == n and steps.is_contiguous(), "steps: one a row")
+    _shape(w_steps.numel() == co and w_steps.is_contiguous(), "w_steps: one an output")
+    _shape(Y.shape == (n, co) and (R is None or R.shape == (n, co)), "Y, R: [n_tok, c_out]")
+    _shape(bias is None or bias.numel() == co and bias.is_contiguous(), "bias: one an output")
+    ws = workspace if workspace is not None else _ws(linear_codes_workspace_bytes(n, c_in), codes)
+    _shape(ws.get_device() == here, "workspace: not on the current device")
+    _check(lib().tlq_linear_codes(codes.data_ptr(), _rows(codes, "codes"), steps.data_ptr(), n, c_in, w_codes.data_ptr(), co,
+                                  _rows(w_codes, "w_codes"), w_steps.data_ptr(), None if bias is None else bias.data_ptr(), act,
+                                  None if R is None else R.data_ptr(), 0 if R is None else _rows(R, "R"), 1 if mul else 0, C.byref(p),
+                                  Y.data_ptr(), _rows(Y, "Y"), ws.data_ptr(), ws.numel(), _stream_of(here)), "tlq_linear_codes")
+    return Y
+
+
+def qk_norm_rope_axes(Q, K, head_dim, pos, axis, inv_freq, p, Q_out, K_out, wq=None, wk=None, eps=1e-6, norm=True, interleaved=False):
+    """qk_norm_rope with positions int32 [axes, n] and the axis of each frequency, int32 [len(inv_freq)]."""
+    ty, here = _types(), _current(Q)
+    x, f32 = ty.of[p.x_dtype], ty.f32
+    for t, want, name in ((Q, x, "Q"), (K, x, "K"), (Q_out, x, "Q_out"), (K_out, x, "K_out"), (pos, ty.i32, "pos"), (axis, ty.i32, "axis"),
+                          (inv_freq, ty.f64, "inv_freq"), (wq, f32, "wq"), (wk, f32, "wk")):
+        if t is not None and (t.dtype is not want or t.get_device() != here):
+            _wrong(t, want, name, here)
+    (n, nq), (rows, nk), (axes, each) = _size(Q, "Q"), _size(K, "K"), _size(pos, "pos")
+    _shape(rows == n and Q_out.shape == (n, nq) and K_out.shape == (n, nk), "outputs of the inputs' shapes")
+    _shape(head_dim > 0 and nq % head_dim == 0 and nk % head_dim == 0, "whole heads")
+    ld_pos = n if axes == 1 else pos.stride(0)
+    _shape(each == n and (n == 1 or pos.stride(1) == 1) and ld_pos >= n, "pos: a row an axis, a column a token")
+    _shape((axis is None) == (inv_freq is None) and (axis is None or axis.numel() == inv_freq.numel() and axis.is_contiguous()
+                                                     and inv_freq.is_contiguous()), "axis: one a frequency")
+    for w in (wq, wk):
+        _shape(w is None or w.numel() == head_dim and w.is_contiguous(), "one weight a channel of a head")
+    _check(lib().tlq_qk_norm_rope_axes(Q.data_ptr(), _rows(Q, "Q"), nq // head_dim, K.data_ptr(), _rows(K, "K"), nk // head_dim, n, head_dim,
+                                       0 if inv_freq is None else 2 * inv_freq.numel(), 1 if interleaved else 0, 1 if norm else 0, eps,
+                                       None if wq is None else wq.data_ptr(), None if wk is None else wk.data_ptr(), pos.data_ptr(), ld_pos,
+                                       axes, None if axis is None else axis.data_ptr(), None if inv_freq is None else inv_freq.data_ptr(),
+                                       C.byref(p), Q_out.data_ptr(), _rows(Q_out, "Q_out"), K_out.data_ptr(), _rows(K_out, "K_out"),
+                                       _stream_of(here)), "tlq_qk_norm_rope_axes")
+    return Q_out, K_out
+
+
+def kv4_cache(k, k_step, v, v_step):
+    """The cache made of words of eight codes, k int32 [n_pages, n_kv_heads, page, head_dim / 8] and v int32 [n_pages, n_kv_heads,
+    head_dim, page / 8], and their steps, half [n_pages, n_kv_heads, page, head_dim / 32] and [n_pages, n_kv_heads, head_dim / 32, page]."""
+    n, h, page, words = k.shape
+    dh = 8 * words
+    _shape(8 * v.size(-1) == page and tuple(v.shape[:3]) == (n, h, dh) and tuple(k_step.shape) == (n, h, page, dh // 32)
+           and tuple(v_step.shape) == (n, h, dh // 32, page), "the shapes of a cache's parts differ")
+    _shape(k.is_contiguous() and v.is_contiguous() and k_step.is_contiguous() and v_step.is_contiguous(), "a cache's parts are dense")
+    c = Kv4Cache(_KV_CACHE_BYTES, h, dh, page, n, k.data_ptr(), k_step.data_ptr(), v.data_ptr(), v_step.data_ptr())
+    c.parts = (k, v, k_step, v_step)       # (they live as long as the structure that points to them)
+    return c
+
+
+def _kv4_tensors(p, batch, cache, tensors):
+    ty, here = _types(), _current(cache.parts[0])
+    i32, f16, want_x = ty.i32, ty.of[F16], ty.of[p.x_dtype]
+    for t, name in tensors:
+        if t.dtype is not want_x or t.get_device() != here:
+            _wrong(t, want_x, name, here)
+    for t, want, name in (*zip(batch.parts, (i32, i32, i32), ("cu_new", "lens", "table")),
+                          *zip(cache.parts, (i32, i32, f16, f16), ("k", "v", "k_step", "v_step"))):
+        if t.dtype is not want or t.get_device() != here:
+            _wrong(t, want, name, here)
+    return here
+
+
+def kv4_append(K, V, batch, cache, p):
+    """New rows of keys and values [n_tok, n_kv_heads * head_dim] into the cache's pages."""
+    here = _kv4_tensors(p, batch, cache, ((K, "K"), (V, "V")))
+    n, width = _size(K, "K")
+    _shape(V.shape == (n, width) and width == cache.n_kv_heads * cache.head_dim, "K, V: [n_tok, n_kv_heads * head_dim]")
+    _check(lib().tlq_kv4_append(K.data_ptr(), _rows(K, "K"), V.data_ptr(), _rows(V, "V"), n, C.byref(batch), C.byref(cache), C.byref(p),
+                                _stream_of(here)), "tlq_kv4_append")
+
+
+def kv4_read(batch, cache, p, K_out=None, V_out=None):
+    """What the tokens of the batch's rows stand for, as rows [n_tok, n_kv_heads * head_dim]."""
+    outs = [(t, name) for t, name in ((K_out, "K_out"), (V_out, "V_out")) if t is not None]
+    _shape(bool(outs), "K_out, V_out: one of them at least")
+    here = _kv4_tensors(p, batch, cache, outs)
+    n, width = _size(*outs[0])
+    _shape(outs[-1][0].shape == (n, width) and width == cache.n_kv_heads * cache.head_dim, "K_out, V_out: [n_tok, n_kv_heads * head_dim]")
+    at = lambda t, name: (None, 0) if t is None else (t.data_ptr(), _rows(t, name))
+    _check(lib().tlq_kv4_read(C.byref(batch), C.byref(cache), C.byref(p), n, *at(K_out, "K_out"), *at(V_out, "V_out"), _stream_of(here)),
+           "tlq_kv4_read")
+
+
+def kv4_attention_workspace_bytes(n_tok, n_heads, batch, cache):
+    return int(lib().tlq_kv4_attention_workspace_bytes(n_tok, n_heads, C.byref(batch), C.byref(cache)))
+
+
+def kv4_attention(Q, n_heads, batch, cache, p, Out, scale=0.0, workspace=None):
+    """Causal attention of the new rows Q [n_tok, n_heads * head_dim] over the cache, their own tokens among it."""
+    here = _kv4_tensors(p, batch, cache, ((Q, "Q"), (Out, "Out")))
+    n, width = _size(Q, "Q")
+    _shape(Out.shape == (n, width) and width == n_heads * cache.head_dim, "Q, Out: [n_tok, n_heads * head_dim]")
+    ws = workspace if workspace is not None else _ws(kv4_attention_workspace_bytes(n, n_heads, batch, cache), Q)
+    _shape(ws.get_device() == here, "workspace: not on the current device")
+    _check(lib().tlq_kv4_attention(Q.data_ptr(), _rows(Q, "Q"), n, n_heads, scale, C.byref(batch), C.byref(cache), C.byref(p),
+                                   Out.data_ptr(), _rows(Out, "Out"), ws.data_ptr(), ws.numel(), _stream_of(here)), "tlq_kv4_attention")
     return Out
 
 
