@@ -3,10 +3,11 @@
 // Mathematics.  Key and value of token j are codes of four bits times steps of eight significant bits, one for each 32 channels:
 // products that halves hold exactly, so both matrix products run on fp16 matrix instructions with operands that are what the
 // cache stands for.  With z_j = scale * log2(e) * (q . key_j) and any reference m,  out = sum_j 2^(z_j - m) value_j / sum_j 2^(z_j - m).
-// m, the row's reference, is 7 below the largest z when it is set and is set again when a z lies 15 above it, so that weights
-// stay between 2^15 and, as normal halves, 2^-21 of the largest at least, and sums are rescaled a few times a row.  The weights are
-// rounded to halves for the second product, and the denominator sums what was rounded, in 32 bits: where one key has nearly
-// all of the weight its rounding cancels.  bf16 queries are multiplied with the power of two that brings the largest of the row to
+// m, the row's reference, is 7 below the largest z when it is set, and is set again where a lane's 8 or 16 weights come to 2^15, so that
+// weights stay below that and, as normal halves, go down to 2^-29 of it, and sums are rescaled a few times a row; no maximum is
+// looked for as long as the sum, which is needed anyhow, stays below (at first m is so low that every weight overflows).  The
+// weights are rounded to halves for the second product, and the denominator sums what was rounded, in 32 bits: where one key has
+// nearly all of the weight its rounding cancels.  bf16 queries are multiplied with the power of two that brings the largest of the row to
 // [2^14, 2^15).  The products are transposed, S^T = K Q^T and O^T = V^T P^T, so that a lane owns one query column and P stays in
 // registers; values are stored channel by channel so that V^T's rows are read as they lie.
 #include "kv4.h"
@@ -18,6 +19,9 @@ struct Kv4AttnDev : KvAttnDev { Kv4Dev d; };      // (of c the sizes)
 
 #if defined(__HIP_DEVICE_COMPILE__)
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+constexpr float kFull = 32768.0f;      // weights of a lane that call for another reference (the largest is 2^11 at least then)
+constexpr float kUnset = -1e30f;
+__device__ __forceinline__ float ref_of(float ref) { return ref < 0.5f * kUnset ? -INFINITY : ref; }      // for those who join
 __device__ __forceinline__ uint32_t twice(uint16_t h) { return (uint32_t)h | (uint32_t)h << 16; }
 // Of pair p of a lane's 16 keys, the halves of those below n
 __device__ __forceinline__ uint32_t keys_below(int p, int n) {
@@ -53,13 +57,16 @@ __global__ __launch_bounds__(256, 2) void kv4_few_kernel(Kv4AttnDev a) {
   const int k1 = end - k0 < a.chunk ? end : k0 + a.chunk;
 
   f16x8 qf[NS];
-  const float fac = a.scale2 * load_queries<T, NS, 8>(
-      a.Q + (q.row0 + qi) * a.ldq + ((int64_t)hk * a.group + g) * DH + fq * (DH / 4), qf, false);
+  float fac = fabsf(a.scale2) * load_queries<T, NS, 8>(
+      a.Q + (q.row0 + qi) * a.ldq + ((int64_t)hk * a.group + g) * DH + fq * (DH / 4), qf, a.scale2 < 0.0f);
+  fac = fmaxf(fac, 1e-37f);                 // (zero times a masked product would not be -inf)
 
   f32x4 acc[ND];
 #pragma unroll
   for (int d = 0; d < ND; ++d) acc[d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  float ref = -INFINITY, l_run = 0.0f;      // the row's reference, this lane's share of its sum
+  float ref = kUnset, l_run = 0.0f;         // the row's reference, this lane's share of its sum
+  const Kv4Bits bits = kv4_bits();
+  const int full = q.first + (int)a.by_group.of(first_row) + 1;      // keys that all rows of the tile see
 
   words kr[4];
   uint16_t ks[4];
@@ -114,37 +121,40 @@ __global__ __launch_bounds__(256, 2) void kv4_few_kernel(Kv4AttnDev a) {
       const uint32_t st = twice(ks[j]);
 #pragma unroll
       for (int i = 0; i < NS; ++i)
-        sc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, kv4_values(kr[j][i], st, st, st, st)), qf[i], sc[j], 0, 0, 0);
+        sc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, kv4_values(kr[j][i], bits, st, st, st, st)), qf[i], sc[j], 0, 0, 0);
     }
     if (unit + 256 < k1) load_k(unit + 256);
     // lane: keys unit + 16 fq + 4 j + r of its query
-    const int limit = seen ? (pos < k1 - 1 ? pos : k1 - 1) - (unit + fq * 16) : -1;    // last visible of the 16
-    float mx = -INFINITY;
+    const bool hidden = unit + 64 > k1 || __any(!seen);      // keys that no row of the tile sees
+    if (hidden || unit + 64 > full) {
+      const int limit = seen ? (pos < k1 - 1 ? pos : k1 - 1) - (unit + fq * 16) : -1;    // last visible of the 16
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+      for (int e = 0; e < 16; ++e) sc[e >> 2][e & 3] = e <= limit ? sc[e >> 2][e & 3] : -INFINITY;
+    }
+    f16x8 pf[2];
+    auto weigh = [&]() __attribute__((always_inline)) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float z = sc[j][r] * fac;
-        sc[j][r] = 4 * j + r <= limit ? z : -INFINITY;
-        mx = fmaxf(mx, sc[j][r]);
-      }
-    mx = column_max(mx);
-    if (__any(mx > ref + kRaise)) {
-      if (mx > ref + kRaise) {
+      for (int e = 0; e < 16; ++e) pf[e >> 3][e & 7] = (_Float16)exp2_of(__builtin_fmaf(sc[e >> 2][e & 3], fac, -ref));
+      return add_weights(pf[1], add_weights(pf[0], 0.0f));
+    };
+    float sum = weigh();
+    if (__any(!(sum < kFull))) {
+      float mx = sc[0][0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, sc[e >> 2][e & 3]);
+      mx = column_max(mx) * fac;
+      if (column_max(sum) >= kFull) {      // (the row's own sums: what the others hold has no part in it)
         const float next = mx - kTop, alpha = exp2_of(ref - next);       // (0 at the first visible key)
         l_run *= alpha;
         ref = next;
 #pragma unroll
         for (int d = 0; d < ND; ++d) acc[d] *= alpha;
       }
+      sum = weigh();
     }
-    const float from = ref == -INFINITY ? 0.0f : ref;
-    f16x8 pf[2];
-#pragma unroll
-    for (int e = 0; e < 16; ++e) pf[e >> 3][e & 7] = (_Float16)exp2_of(sc[e >> 2][e & 3] - from);
-    l_run += add_weights(pf[1], add_weights(pf[0], 0.0f));
+    l_run += sum;
     // (steps behind the last token, or of a page that is not this sequence's, may be anything)
-    if (unit + 64 > k1 || __any(!seen)) {
+    if (hidden) {
       const int n = seen ? k1 - (unit + fq * 16) : 0;
 #pragma unroll
       for (int i = 0; i < NG; ++i)
@@ -162,12 +172,13 @@ __global__ __launch_bounds__(256, 2) void kv4_few_kernel(Kv4AttnDev a) {
       for (int u = 0; u < 2; ++u) {
         const uint4 st = vs[d / 2][u];
         acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
-            __builtin_bit_cast(f16x8, kv4_values(u ? vr[d].y : vr[d].x, st.x, st.y, st.z, st.w)), pf[u], acc[d], 0, 0, 0);
+            __builtin_bit_cast(f16x8, kv4_values(u ? vr[d].y : vr[d].x, bits, st.x, st.y, st.z, st.w)), pf[u], acc[d], 0, 0, 0);
       }
     if (unit + 256 < k1) load_v(unit + 256);
   }
   l_run += __shfl_xor(l_run, 16, 64);
   l_run += __shfl_xor(l_run, 32, 64);
+  ref = ref_of(ref);
   if (fq == 0) ml[wave][l16] = make_float2(ref, l_run);
   __syncthreads();
   const float top = fmaxf(fmaxf(ml[0][l16].x, ml[1][l16].x), fmaxf(ml[2][l16].x, ml[3][l16].x));
@@ -277,7 +288,8 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kv4_prompt_kernel(Kv4At
   f32x4 acc[ND][2];
 #pragma unroll
   for (int d = 0; d < ND; ++d) acc[d][0] = acc[d][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  float ref[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.0f, 0.0f};
+  float ref[2] = {kUnset, kUnset}, l_run[2] = {0.0f, 0.0f};
+  const Kv4Bits bits = kv4_bits();
 
   // what a thread moves: K rows tid / (CPK / 2) and further ones, 16 codes of a group; V channels 16 wave + l16 and 64 further, the 16
   // keys that it has the scores of.
@@ -335,12 +347,12 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kv4_prompt_kernel(Kv4At
     if constexpr (I < 2 * LR) {
       const int row = krow + L * KSTEP;
       const uint32_t st = twice(ks[L]);
-      *reinterpret_cast<uint4*>(at + row * KB + ((kplace(kch + HALF) ^ kkey(row)) << 4)) = kv4_values(HALF ? kr[L].y : kr[L].x, st, st, st, st);
+      *reinterpret_cast<uint4*>(at + row * KB + ((kplace(kch + HALF) ^ kkey(row)) << 4)) = kv4_values(HALF ? kr[L].y : kr[L].x, bits, st, st, st, st);
     } else {
       const int row = vrow + L * 64;
       const uint4 st = vs[L][HALF];
       *reinterpret_cast<uint4*>(at + 64 * KB + row * VB + (((fq + 4 * HALF) ^ (row & 7)) << 4)) =
-          kv4_values(HALF ? vr[L].y : vr[L].x, st.x, st.y, st.z, st.w);
+          kv4_values(HALF ? vr[L].y : vr[L].x, bits, st.x, st.y, st.z, st.w);
     }
   };
   auto stage_all = [&](unsigned char* at) __attribute__((always_inline)) {
@@ -357,7 +369,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kv4_prompt_kernel(Kv4At
           const int row = vrow + i * 64;
           const uint4 st = vs[i][u];
           *reinterpret_cast<uint4*>(at + 64 * KB + row * VB + (((fq + 4 * u) ^ (row & 7)) << 4)) =
-              kv4_values(u ? vr[i].y : vr[i].x, st.x & keys_below(4 * u, n), st.y & keys_below(4 * u + 1, n),
+              kv4_values(u ? vr[i].y : vr[i].x, bits, st.x & keys_below(4 * u, n), st.y & keys_below(4 * u + 1, n),
                          st.z & keys_below(4 * u + 2, n), st.w & keys_below(4 * u + 3, n));
         }
     }
@@ -435,28 +447,6 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kv4_prompt_kernel(Kv4At
         for (int e = 0; e < 16; ++e) sc[e >> 2][n][e & 3] = e <= limit ? sc[e >> 2][n][e & 3] : -INFINITY;
       }
     }
-    float mx[2];
-#pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      mx[n] = sc[0][n][0];
-#pragma unroll
-      for (int e = 1; e < 16; ++e) mx[n] = fmaxf(mx[n], sc[e >> 2][n][e & 3]);
-      mx[n] = column_max(mx[n]) * fac[n];
-    }
-    if (__any(mx[0] > ref[0] + kRaise || mx[1] > ref[1] + kRaise)) {
-#pragma unroll
-      for (int n = 0; n < 2; ++n)
-        if (mx[n] > ref[n] + kRaise) {
-          const float next_ref = mx[n] - kTop, alpha = exp2_of(ref[n] - next_ref);
-          l_run[n] *= alpha;
-          ref[n] = next_ref;
-#pragma unroll
-          for (int d = 0; d < ND; ++d) acc[d][n] *= alpha;
-        }
-    }
-    float off[2];
-#pragma unroll
-    for (int n = 0; n < 2; ++n) off[n] = ref[n] != -INFINITY ? -ref[n] : 0.0f;
     // half of the keys after the other: the weights of the second half are formed between the products of the first
     f16x8 pf[2][2], vf[4];
     auto read_v = [&](int at) __attribute__((always_inline)) {
@@ -467,28 +457,63 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kv4_prompt_kernel(Kv4At
       constexpr int u = decltype(uc)::value, e = decltype(ec)::value;
 #pragma unroll
       for (int n = 0; n < 2; ++n)
-        pf[u][n][e] = (_Float16)exp2_of(__builtin_fmaf(sc[2 * u + (e >> 2)][n][e & 3], fac[n], off[n]));
+        pf[u][n][e] = (_Float16)exp2_of(__builtin_fmaf(sc[2 * u + (e >> 2)][n][e & 3], fac[n], -ref[n]));
     };
+    // the weights of a half into the sums, behind another reference if they call for it
+    auto take = [&](auto uc) __attribute__((always_inline)) {
+      constexpr int u = decltype(uc)::value;
+      float sum[2] = {add_weights(pf[u][0], 0.0f), add_weights(pf[u][1], 0.0f)};
+      if (__any(!(sum[0] < kFull && sum[1] < kFull))) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+          float mx = sc[2 * u][n][0];
+#pragma unroll
+          for (int e = 1; e < 8; ++e) mx = fmaxf(mx, sc[2 * u + (e >> 2)][n][e & 3]);
+          mx = column_max(mx) * fac[n];
+          if (column_max(sum[n]) >= kFull) {      // (the row's own sums: what the others hold has no part in it)
+            const float next_ref = mx - kTop, alpha = exp2_of(ref[n] - next_ref);
+            l_run[n] *= alpha;
+            ref[n] = next_ref;
+#pragma unroll
+            for (int d = 0; d < ND; ++d) acc[d][n] *= alpha;
+          }
+        }
+        static_for<0, 8>([&](auto ec) { weigh(uc, ec); });
+        sum[0] = add_weights(pf[u][0], 0.0f);
+        sum[1] = add_weights(pf[u][1], 0.0f);
+      }
+      l_run[0] += sum[0];
+      l_run[1] += sum[1];
+    };
+    using First = std::integral_constant<int, 0>;
+    using Second = std::integral_constant<int, 1>;
 #pragma unroll
     for (int at = 0; at < 4; ++at) read_v(at);
-    static_for<0, 8>([&](auto ec) { weigh(std::integral_constant<int, 0>{}, ec); });
-    static_for<0, 2 * ND>([&](auto ac) {
-      constexpr int at = decltype(ac)::value, d = at % ND, u = at / ND, E = 8 / ND;
-      acc[d][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[at & 3], pf[u][0], acc[d][0], 0, 0, 0);
-      acc[d][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[at & 3], pf[u][1], acc[d][1], 0, 0, 0);
-      if constexpr (at + 4 < 2 * ND) read_v(at + 4);
-      if constexpr (u == 0)
-        static_for<0, E>([&](auto ec) { weigh(std::integral_constant<int, 1>{}, std::integral_constant<int, d * E + decltype(ec)::value>{}); });
+    static_for<0, 8>([&](auto ec) { weigh(First{}, ec); });
+    take(First{});
+    static_for<0, ND>([&](auto dc) {
+      constexpr int d = decltype(dc)::value, E = 8 / ND;
+      acc[d][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[d & 3], pf[0][0], acc[d][0], 0, 0, 0);
+      acc[d][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[d & 3], pf[0][1], acc[d][1], 0, 0, 0);
+      read_v(d + 4);
+      static_for<0, E>([&](auto ec) { weigh(Second{}, std::integral_constant<int, d * E + decltype(ec)::value>{}); });
       __builtin_amdgcn_sched_barrier(0);
     });
-#pragma unroll
-    for (int n = 0; n < 2; ++n) l_run[n] += add_weights(pf[1][n], add_weights(pf[0][n], 0.0f));
+    take(Second{});
+    static_for<ND, 2 * ND>([&](auto ac) {
+      constexpr int at = decltype(ac)::value, d = at - ND;
+      acc[d][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[at & 3], pf[1][0], acc[d][0], 0, 0, 0);
+      acc[d][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[at & 3], pf[1][1], acc[d][1], 0, 0, 0);
+      if constexpr (at + 4 < 2 * ND) read_v(at + 4);
+      __builtin_amdgcn_sched_barrier(0);
+    });
   }
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
     float l = l_run[n];
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
+    ref[n] = ref_of(ref[n]);
     const uint32_t r = wrow + n * 16 + l16;
     if (r >= rows) continue;
     const uint32_t qi = a.by_group.of(r);
