@@ -22,6 +22,12 @@ __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2
 constexpr float kFull = 32768.0f;      // weights of a lane that call for another reference (the largest is 2^11 at least then)
 constexpr float kUnset = -1e30f;
 __device__ __forceinline__ float ref_of(float ref) { return ref < 0.5f * kUnset ? -INFINITY : ref; }      // for those who join
+// keeps what a wave's lanes write for each other in LDS in order
+__device__ __forceinline__ void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 __device__ __forceinline__ uint32_t twice(uint16_t h) { return (uint32_t)h | (uint32_t)h << 16; }
 // Of pair p of a lane's 16 keys, the halves of those below n
 __device__ __forceinline__ uint32_t keys_below(int p, int n) {
@@ -31,14 +37,18 @@ __device__ __forceinline__ uint32_t keys_below(int p, int n) {
 
 // The 16 rows of a tile (a query and head each: the heads that share a key head are rows side by side) against one split of
 // the keys.  Four waves take 64 keys each in turn and meet in LDS at the end; keys and values go from memory to registers,
-// where they are widened: no LDS, no barrier in the loop, the next 64 keys in flight while these are worked on.
+// where they are widened: no barrier in the loop, the next 64 keys in flight while these are worked on.  Only their steps pass
+// through the wave's own piece of LDS: a lane needs 16 of each group of channels, which sixteen lanes share; loaded by each they take
+// ten more loads and 36 registers (which cost the third wave a SIMD), us that way and this: 64 x 2000 keys x 32 heads 115 99, 64 x 4096 -
+// 8192 x 8 110 105, 131,072 x 4 29.3 27.8; heads of 64 64 67.
 template <typename T, int DH>
-__global__ __launch_bounds__(256, 2) void kv4_few_kernel(Kv4AttnDev a) {
+__global__ __launch_bounds__(256, 3) void kv4_few_kernel(Kv4AttnDev a) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int NS = DH / 32, ND = DH / 16, NG = DH / kKv4Group;      // k32 steps of a score = words of a lane's key, channel tiles, groups
   constexpr int RS = DH + 4;
   typedef uint32_t words __attribute__((ext_vector_type(NS)));
   __shared__ __attribute__((aligned(16))) float part[4][16][RS];
+  __shared__ __attribute__((aligned(16))) uint16_t steps[4][2][64 * NG];      // of a wave's 64 keys: [key][group], [16 keys][group][key]
   __shared__ float2 ml[4][16];
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, fq = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -68,10 +78,10 @@ __global__ __launch_bounds__(256, 2) void kv4_few_kernel(Kv4AttnDev a) {
   const Kv4Bits bits = kv4_bits();
   const int full = q.first + (int)a.by_group.of(first_row) + 1;      // keys that all rows of the tile see
 
+  typedef uint16_t halves __attribute__((ext_vector_type(NG)));
   words kr[4];
-  uint16_t ks[4];
   uint2 vr[ND];
-  uint4 vs[NG][2];
+  halves ksr, vsr;                      // steps of key fq * 16 + l16; of NG of the 16 keys, of one group
   bool seen = false;                    // this lane's 16 keys lie in a page that there is
   // The table's entries are fetched a turn before the pages they name (keys behind the last are never seen: any entry will
   // do); an entry outside the pool becomes the first page, in reach and never seen
@@ -83,12 +93,8 @@ __global__ __launch_bounds__(256, 2) void kv4_few_kernel(Kv4AttnDev a) {
   auto load_k = [&](int unit) {
     const int64_t token = ((int64_t)(kid < n_pages ? kid : 0) * a.c.n_kv_heads + hk) * a.c.page + ((unit + kgroup) & (a.c.page - 1)) + (l16 & 3);
     const uint32_t* p = a.d.k + token * (DH / 8) + fq * NS;
-    const uint16_t* st = a.d.k_step + token * NG + fq * NG / 4;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      kr[j] = *reinterpret_cast<const words*>(p + j * 4 * (DH / 8));
-      ks[j] = st[j * 4 * NG];
-    }
+    for (int j = 0; j < 4; ++j) kr[j] = *reinterpret_cast<const words*>(p + j * 4 * (DH / 8));
     kid = entry(unit + 256 + kgroup);
   };
   auto load_v = [&](int unit) {
@@ -96,13 +102,10 @@ __global__ __launch_bounds__(256, 2) void kv4_few_kernel(Kv4AttnDev a) {
     const int64_t slot = (int64_t)(seen ? vid : 0) * a.c.n_kv_heads + hk;
     const int at = (unit + vgroup) & (a.c.page - 1);
     const uint32_t* p = a.d.v + ((slot * DH + l16) * a.c.page + at) / 8;
-    const uint16_t* st = a.d.v_step + slot * NG * a.c.page + at;
+    ksr = *reinterpret_cast<const halves*>(a.d.k_step + (slot * a.c.page + at + l16) * NG);
+    vsr = *reinterpret_cast<const halves*>(a.d.v_step + (slot * NG + l16 / (16 / NG)) * a.c.page + at + l16 % (16 / NG) * NG);
 #pragma unroll
     for (int d = 0; d < ND; ++d) vr[d] = *reinterpret_cast<const uint2*>(p + d * 2 * a.c.page);
-#pragma unroll
-    for (int i = 0; i < NG; ++i)
-#pragma unroll
-      for (int u = 0; u < 2; ++u) vs[i][u] = *reinterpret_cast<const uint4*>(st + i * a.c.page + u * 8);
     vid = entry(unit + 256 + vgroup);
   };
 
@@ -113,7 +116,16 @@ __global__ __launch_bounds__(256, 2) void kv4_few_kernel(Kv4AttnDev a) {
     load_k(unit);
     load_v(unit);
   }
+  const uint16_t* my_ks = steps[wave][0] + (kgroup + (l16 & 3)) * NG + fq * NG / 4;
+  const uint16_t* my_vs = steps[wave][1] + fq * 16 * NG;
   for (; unit < k1; unit += 256) {
+    // the steps of the wave's keys pass through LDS, where each lane picks those of its own
+    *reinterpret_cast<halves*>(steps[wave][0] + lane * NG) = ksr;
+    *reinterpret_cast<halves*>(steps[wave][1] + lane * NG) = vsr;
+    wave_order();
+    uint16_t ks[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) ks[j] = my_ks[j * 4 * NG];
     f32x4 sc[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -153,6 +165,11 @@ __global__ __launch_bounds__(256, 2) void kv4_few_kernel(Kv4AttnDev a) {
       sum = weigh();
     }
     l_run += sum;
+    uint4 vs[NG][2];
+#pragma unroll
+    for (int i = 0; i < NG; ++i)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) vs[i][u] = *reinterpret_cast<const uint4*>(my_vs + i * 16 + u * 8);
     // (steps behind the last token, or of a page that is not this sequence's, may be anything)
     if (hidden) {
       const int n = seen ? k1 - (unit + fq * 16) : 0;
@@ -174,6 +191,7 @@ __global__ __launch_bounds__(256, 2) void kv4_few_kernel(Kv4AttnDev a) {
         acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
             __builtin_bit_cast(f16x8, kv4_values(u ? vr[d].y : vr[d].x, bits, st.x, st.y, st.z, st.w)), pf[u], acc[d], 0, 0, 0);
       }
+    wave_order();      // (before the next turn's steps overwrite these)
     if (unit + 256 < k1) load_v(unit + 256);
   }
   l_run += __shfl_xor(l_run, 16, 64);
