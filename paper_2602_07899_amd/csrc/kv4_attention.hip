@@ -318,15 +318,10 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kv4_prompt_kernel(Kv4At
   const uint32_t n_pages = (uint32_t)a.c.n_pages, in_page = (uint32_t)a.c.page - 1;
   const uint32_t *kp = a.d.k + (uint64_t)hk * head_words, *vp = a.d.v + (uint64_t)hk * head_words;
   const uint16_t *ksp = a.d.k_step + (uint64_t)hk * head_steps, *vsp = a.d.v_step + (uint64_t)hk * head_steps;
-  uint32_t koff[LR], ksoff[LR], voff[LR], vsoff[LR];
+  uint32_t koff[LR];                   // (a key's steps lie at a quarter of its words' offset)
 #pragma unroll
-  for (int i = 0; i < LR; ++i) {
-    const uint32_t token = (uint32_t)(krow + i * KSTEP) & in_page, at = (uint32_t)(fq * 16) & in_page, channel = vrow + i * 64;
-    koff[i] = token * (DH / 8) + kch;
-    ksoff[i] = token * NG + kch / 4;
-    voff[i] = (channel * a.c.page + at) / 8;
-    vsoff[i] = channel / kKv4Group * a.c.page + at;
-  }
+  for (int i = 0; i < LR; ++i) koff[i] = ((uint32_t)(krow + i * KSTEP) & in_page) * (DH / 8) + kch;
+  const uint32_t vat = (uint32_t)(fq * 16) & in_page, voff = (vrow * a.c.page + vat) / 8, vsoff = vrow / kKv4Group * a.c.page + vat;
   uint2 kr[LR], vr[LR];
   uint16_t ks[LR];
   uint4 vs[LR][2];
@@ -342,15 +337,15 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kv4_prompt_kernel(Kv4At
       uint32_t k = g == 0 ? ids[0] : g == 1 ? ids[1] : g == 2 ? ids[2] : ids[3];
       k = k < n_pages ? k : 0;
       kr[i] = *reinterpret_cast<const uint2*>(kp + ((uint64_t)k * page_stride + at * (DH / 8)) + koff[i]);
-      ks[i] = (ksp + ((uint64_t)k * page_steps + at * NG))[ksoff[i]];
+      ks[i] = (ksp + ((uint64_t)k * page_steps + at * NG))[koff[i] >> 2];
     }
     const uint32_t* p = vp + at / 8 + (uint64_t)id * page_stride;
     const uint16_t* st = vsp + at + (uint64_t)id * page_steps;
 #pragma unroll
     for (int i = 0; i < LR; ++i) {
-      vr[i] = *reinterpret_cast<const uint2*>(p + voff[i]);
-      vs[i][0] = *reinterpret_cast<const uint4*>(st + vsoff[i]);
-      vs[i][1] = *reinterpret_cast<const uint4*>(st + vsoff[i] + 8);
+      vr[i] = *reinterpret_cast<const uint2*>(p + i * 8 * a.c.page + voff);
+      vs[i][0] = *reinterpret_cast<const uint4*>(st + i * 2 * a.c.page + vsoff);
+      vs[i][1] = *reinterpret_cast<const uint4*>(st + i * 2 * a.c.page + vsoff + 8);
     }
     entries(unit + 64);
   };
