@@ -18,9 +18,10 @@ inline tlq_kv_cache kv4_sizes(const tlq_kv4_cache& c) {
   return s;
 }
 
+__host__ __device__ constexpr int kv4_shift(int e) { return 4 * (e >> 1) + 16 * (e & 1); }
+
 #if defined(__HIP_DEVICE_COMPILE__)
 typedef _Float16 kv4_f16x2 __attribute__((ext_vector_type(2)));
-__host__ __device__ constexpr int kv4_shift(int e) { return 4 * (e >> 1) + 16 * (e & 1); }
 // The bits of a pair of codes and what stands in front of them: four bits behind the exponent of 1024 are 1024 + n, four bits higher
 // up behind that of 64 are 64 + n.  In registers (as constants of an instruction each would need two of them).
 struct Kv4Bits { uint32_t low, high, k1024, k64; };

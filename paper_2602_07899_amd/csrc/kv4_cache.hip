@@ -1,9 +1,12 @@
 // New keys and values into the pages of a 4-bit cache, and what a cache holds as 16-bit rows.
+#include <type_traits>
+
 #include "kv4.h"
 
 namespace tlq {
 
 typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 
 struct Kv4CacheDev {
   const uint16_t *K, *V; uint16_t *Ko, *Vo; int64_t ldk, ldv, n_tok;      // rows in, or rows out
@@ -40,15 +43,31 @@ __device__ __forceinline__ bool kv4_piece(const Kv4CacheDev& a, Kv4Piece& p) {
   p.id = p.p0 >= 0 && p.p0 < p.q.len ? kv_page(a.b, a.c, s, (int)p.p0 / a.c.page) : -1;
   return true;
 }
-__device__ __forceinline__ float finite_abs(float x) { return __builtin_isfinite(x) ? fabsf(x) : 0.0f; }
-// code + 8 in the low bits.  x / step is k + 1/2 exactly or at least 2^-13 away from it: both have few bits (x at least 2^-6 steps: 11
-// and 8).  So the product with the reciprocal, off by 1.5 ulp, is brought to a multiple of 2^-16, which restores the ties
-// and crosses none, and rounded half to even by the addition.
+template <int CTRL>
+__device__ __forceinline__ uint32_t quad_max(uint32_t v) {      // with a lane of the same four
+  const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+  return o > v ? o : v;
+}
+template <typename T> struct Kv4Odd;      // magnitudes (their bits) from which on a group has a number that is not finite, or more than
+template <> struct Kv4Odd<F16> { static constexpr uint32_t bits = 0x7c00; };        // seven of the largest steps
+template <> struct Kv4Odd<BF16> { static constexpr uint32_t bits = 0x4780; };
+// The four bits of a code.  x / step is k + 1/2 exactly or at least 2^-13 away from it: both have few bits (x at least 2^-6 steps: 11
+// and 8).  So the product with the reciprocal, off by 1.5 ulp, is brought to a multiple of 2^-16 beside 192, which restores the
+// ties and crosses none, and rounded half to even beside 1.5 * 2^23, where the low bits are the code's + 8.
+constexpr float kBeside = 192.0f, kCodeAt = 12582920.0f - 192.0f;
+constexpr uint32_t kCodeBits = 0x4b400000u;      // what stands in front of them
 __device__ __forceinline__ uint32_t kv4_code(float x, float rd) {
-  float q = __builtin_fmaf(x, rd, 192.0f) - 192.0f;
-  q = __builtin_amdgcn_fmed3f(q, -kKv4Top, kKv4Top);
-  q = x != x ? 0.0f : q;
-  return __builtin_bit_cast(uint32_t, q + 12582920.0f) & 15u;      // 1.5 * 2^23 + 8
+  return __builtin_bit_cast(uint32_t, __builtin_fmaf(x, rd, kBeside) + kCodeAt);
+}
+__device__ __forceinline__ uint32_t kv4_code_any(float x, float rd) {      // also beyond the steps and of NaN
+  const float t = __builtin_amdgcn_fmed3f(__builtin_fmaf(x, rd, kBeside), kBeside - kKv4Top, kBeside + kKv4Top);
+  return __builtin_bit_cast(uint32_t, (x != x ? kBeside : t) + kCodeAt);
+}
+// what the fronts of eight codes come to when each is shifted to its place and all are added
+constexpr uint32_t kv4_fronts() {
+  uint32_t f = 0;
+  for (int e = 0; e < 8; ++e) f += kCodeBits << kv4_shift(e);
+  return f;
 }
 #endif
 
@@ -67,57 +86,86 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4CacheDev a) {
   const uint16_t* x = (val ? a.V : a.K) + (int64_t)p.h * DH + p.d8 * 8;
   const int64_t ld = val ? a.ldv : a.ldk;
   const int64_t slot = (int64_t)p.id * a.c.n_kv_heads + p.h;
-  u16x8 raw[8];
+  const bool whole = p.lo == 0 && p.hi == 8, first = (p.d8 & 3) == 0;
+  uint32_t* to = a.d.v + ((slot * DH + p.d8 * 8) * a.c.page + p.in_page) / 8;
+  uint16_t* at = a.d.v_step + (slot * NG + p.d8 / 4) * a.c.page + p.in_page;
+  uint4 raw[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    raw[e] = u16x8{0, 0, 0, 0, 0, 0, 0, 0};
-    if (e >= p.lo && e < p.hi) raw[e] = *reinterpret_cast<const u16x8*>(x + (p.row0 + e) * ld);
+  for (int e = 0; e < 8; ++e)
+    if (e >= p.lo && e < p.hi) raw[e] = *reinterpret_cast<const uint4*>(x + (p.row0 + e) * ld);
+  uint32_t old[8];
+  if (val && !whole) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) old[j] = to[(int64_t)j * (a.c.page / 8)];
   }
   uint32_t word[8];      // of K: a token's eight channels, of V: a channel's eight tokens
   uint16_t step[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) word[e] = 0;
+  for (int j = 0; j < 8; ++j) word[j] = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    float f[8], m = 0.0f;
+    if (e < p.lo || e >= p.hi) continue;
+    const uint32_t w[4] = {raw[e].x, raw[e].y, raw[e].z, raw[e].w};
+    u16x2 m2 = {0, 0};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      f[j] = T::to_float(raw[e][j]);
-      m = fmaxf(m, finite_abs(f[j]));
+    for (int j = 0; j < 4; ++j) m2 = __builtin_elementwise_max(m2, __builtin_bit_cast(u16x2, w[j] & 0x7fff7fffu));
+    uint32_t m = m2[0] > m2[1] ? m2[0] : m2[1];
+    m = quad_max<0x4E>(quad_max<0xB1>(m));
+    const bool odd = m >= Kv4Odd<T>::bits;
+    float f[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = T::to_float((uint16_t)(w[j >> 1] >> ((j & 1) * 16)));
+    if (__builtin_expect(__any(odd), 0)) {      // the largest finite one
+      m = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t b = (w[j >> 1] >> ((j & 1) * 16)) & 0x7fffu;
+        m = __builtin_isfinite(f[j]) && b > m ? b : m;
+      }
+      m = quad_max<0x4E>(quad_max<0xB1>(m));
     }
-    m = fmaxf(m, __shfl_xor(m, 1, 64));
-    m = fmaxf(m, __shfl_xor(m, 2, 64));
-    const float wide = BF16::to_float(BF16::from_float(fmaxf(m, kRangeFloor) / kKv4Top));
+    // a seventh: one correction step on the product with the reciprocal is the quotient (as in the weights' quantiser)
+    const float most = fmaxf(T::to_float((uint16_t)m), kRangeFloor), seventh = 1.0f / kKv4Top, q0 = most * seventh;
+    const float wide = BF16::to_float(BF16::from_float(__builtin_fmaf(__builtin_fmaf(-q0, kKv4Top, most), seventh, q0)));
     step[e] = F16::from_float(fminf(wide, kKv4Most));
     const float rd = __builtin_amdgcn_rcpf(F16::to_float(step[e]));
+    uint32_t n[8];
+    if (__builtin_expect(__any(odd), 0)) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) n[j] = kv4_code_any(f[j], rd);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) n[j] = kv4_code(f[j], rd);
+    }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const uint32_t n = kv4_code(f[j], rd);
-      if (val) word[j] |= n << kv4_shift(e);
-      else word[e] |= n << kv4_shift(j);
+      if (val) word[j] += n[j] << kv4_shift(e);
+      else word[e] += n[j] << kv4_shift(j);
     }
   }
-  const bool first = (p.d8 & 3) == 0;
   if (!val) {
     const int64_t token = slot * a.c.page + p.in_page;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       if (e < p.lo || e >= p.hi) continue;
-      a.d.k[(token + e) * (DH / 8) + p.d8] = word[e];
+      a.d.k[(token + e) * (DH / 8) + p.d8] = word[e] - kv4_fronts();
       if (first) a.d.k_step[(token + e) * NG + p.d8 / 4] = step[e];
     }
     return;
   }
-  uint32_t* to = a.d.v + ((slot * DH + p.d8 * 8) * a.c.page + p.in_page) / 8;
-  uint16_t* at = a.d.v_step + (slot * NG + p.d8 / 4) * a.c.page + p.in_page;
-  const bool whole = p.lo == 0 && p.hi == 8;
-  uint32_t mask = 0;
+  if (whole) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) mask |= e >= p.lo && e < p.hi ? 15u << kv4_shift(e) : 0u;
+    for (int j = 0; j < 8; ++j) to[(int64_t)j * (a.c.page / 8)] = word[j] - kv4_fronts();
+  } else {
+    uint32_t mask = 0, fronts = 0;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int64_t row = (int64_t)j * (a.c.page / 8);
-    to[row] = whole ? word[j] : (to[row] & ~mask) | (word[j] & mask);
+    for (int e = 0; e < 8; ++e)
+      if (e >= p.lo && e < p.hi) {
+        mask |= 15u << kv4_shift(e);
+        fronts += kCodeBits << kv4_shift(e);
+      }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) to[(int64_t)j * (a.c.page / 8)] = (old[j] & ~mask) | (word[j] - fronts);
   }
   if (first) {
     if (whole) {
@@ -143,35 +191,53 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4CacheDev a) {
   const int64_t ld = val ? a.ldv : a.ldk;
   const int64_t slot = (int64_t)(p.id < 0 ? 0 : p.id) * a.c.n_kv_heads + p.h;
   const int there = p.id < 0 ? 0 : p.q.len - p.p0 < 8 ? (int)(p.q.len - p.p0) : 8;      // tokens of the eight that there are
-  uint32_t word[8];
-  uint16_t step[8];
+  const Kv4Bits bits = kv4_bits();
+  uint4 half[8];      // of K: a token's eight channels, of V: a channel's eight tokens
   if (!val) {
     const int64_t token = slot * a.c.page + p.in_page;
+    uint32_t word[8], step[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      word[e] = a.d.k[(token + e) * (DH / 8) + p.d8];
-      step[e] = a.d.k_step[(token + e) * NG + p.d8 / 4];
-    }
+    for (int e = 0; e < 8; ++e)
+      if (e >= p.lo && e < p.hi) {
+        word[e] = a.d.k[(token + e) * (DH / 8) + p.d8];
+        step[e] = a.d.k_step[(token + e) * NG + p.d8 / 4];
+      }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e >= p.lo && e < p.hi) {
+        const uint32_t s = step[e] | step[e] << 16;
+        half[e] = kv4_values(word[e], bits, s, s, s, s);
+      }
   } else {
     const uint32_t* from = a.d.v + ((slot * DH + p.d8 * 8) * a.c.page + p.in_page) / 8;
-    const u16x8 s = *reinterpret_cast<const u16x8*>(a.d.v_step + (slot * NG + p.d8 / 4) * a.c.page + p.in_page);
+    const uint4 s = *reinterpret_cast<const uint4*>(a.d.v_step + (slot * NG + p.d8 / 4) * a.c.page + p.in_page);
+    uint32_t word[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      word[j] = from[(int64_t)j * (a.c.page / 8)];
-      step[j] = s[j];
-    }
+    for (int j = 0; j < 8; ++j) word[j] = from[(int64_t)j * (a.c.page / 8)];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) half[j] = kv4_values(word[j], bits, s.x, s.y, s.z, s.w);
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     if (e < p.lo || e >= p.hi) continue;
-    const float st = F16::to_float(step[e]);
-    uint16_t o[8];
+    uint32_t o[4];
+    if (!val) {
+      o[0] = half[e].x; o[1] = half[e].y; o[2] = half[e].z; o[3] = half[e].w;
+    } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t n = val ? word[j] >> kv4_shift(e) : word[e] >> kv4_shift(j);
-      o[j] = e < there ? T::from_float((float)((int)(n & 15u) - 8) * st) : 0;
+      for (int j = 0; j < 4; ++j) {
+        const uint4 &u = half[2 * j], &v = half[2 * j + 1];
+        const uint32_t c = e < 2 ? u.x : e < 4 ? u.y : e < 6 ? u.z : u.w, d = e < 2 ? v.x : e < 4 ? v.y : e < 6 ? v.z : v.w;
+        o[j] = __builtin_amdgcn_perm(d, c, e & 1 ? 0x07060302u : 0x05040100u);
+      }
     }
-    *reinterpret_cast<u16x8*>(x + (p.row0 + e) * ld) = u16x8{o[0], o[1], o[2], o[3], o[4], o[5], o[6], o[7]};
+    if constexpr (std::is_same<T, BF16>::value) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        o[j] = (uint32_t)BF16::from_float(F16::to_float((uint16_t)o[j])) | (uint32_t)BF16::from_float(F16::to_float((uint16_t)(o[j] >> 16))) << 16;
+    }
+    if (e >= there) o[0] = o[1] = o[2] = o[3] = 0;
+    *reinterpret_cast<uint4*>(x + (p.row0 + e) * ld) = make_uint4(o[0], o[1], o[2], o[3]);
   }
 #endif
 }
