@@ -198,7 +198,7 @@ struct FinalDev {
 struct GemmTile { bool small; int tok_blocks; };
 // S3+S4 / plain GEMM with store epilogue.
 // What follows a product's scaling (finish.h): y = act(y + bias[o]), then + or * R[t, o] of the output's type.  k1, k3: of the
-// logistic activations
+// logistic activations' exponent
 struct Finish { const float* bias; const void* R; int64_t ldr; int act, mul; float k1, k3; };
 struct GemmArgs : GemmTile {
   GemmTile& tile() { return *this; }

@@ -408,35 +408,24 @@ __device__ __forceinline__ void store_rows_lds(const GemmDev& a, void* Yout, con
 }
 
 #if defined(__HIP_DEVICE_COMPILE__)
-// The same with GemmDev::fin behind the scaling; the second matrix comes in whole lines through the same piece of LDS.
-template <typename YT, int CLASS, typename L, typename Acc>
-__device__ __forceinline__ void finish_rows_lds(const GemmDev& a, void* Yout, const Acc& acc, const float* tsc,
-                                                int64_t ow, int64_t tw, unsigned char* ylds) {
+// The same for accumulators that are outputs already, with the second matrix of GemmDev::fin, which comes in whole lines through
+// the same piece of LDS.
+template <typename YT, typename L, typename Acc>
+__device__ __forceinline__ void second_rows_lds(const GemmDev& a, void* Yout, const Acc& acc, int64_t ow, int64_t tw, unsigned char* ylds) {
   using S = Staged<L>;
-  const int lane = threadIdx.x & 63;
-  const Finish& f = a.fin;
+  const bool mul = a.fin.mul;
   static_for<0, S::GROUPS>([&](auto gc) {
     constexpr int G = decltype(gc)::value;
-    if (f.R) S::template fill<G>(f.R, f.ldr, ow, tw, ylds);
-    else if (G > 0) wave_lds_order();
+    S::template fill<G>(a.fin.R, a.fin.ldr, ow, tw, ylds);
 #pragma unroll
     for (int b = 0; b < S::template blocks<G>(); ++b) {
       const int tb = G * L::STG + b;
-      const float sg = tsc[tw + L::tok(tb, lane)];
 #pragma unroll
       for (int q = 0; q < L::NQ; ++q) {
         float y[4], r[4];
-        float4 bias = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (f.bias) bias = *reinterpret_cast<const float4*>(f.bias + ow + L::row(q, lane));
-        y[0] = act_of<CLASS>(__builtin_fmaf(sg, L::get(acc, q, tb, 0), bias.x), f);
-        y[1] = act_of<CLASS>(__builtin_fmaf(sg, L::get(acc, q, tb, 1), bias.y), f);
-        y[2] = act_of<CLASS>(__builtin_fmaf(sg, L::get(acc, q, tb, 2), bias.z), f);
-        y[3] = act_of<CLASS>(__builtin_fmaf(sg, L::get(acc, q, tb, 3), bias.w), f);
-        if (f.R) {
-          unpack4<YT>(*S::at4(ylds, b, q), r);
+        unpack4<YT>(*S::at4(ylds, b, q), r);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) y[e] = f.mul ? y[e] * r[e] : y[e] + r[e];
-        }
+        for (int e = 0; e < 4; ++e) y[e] = mul ? L::get(acc, q, tb, e) * r[e] : L::get(acc, q, tb, e) + r[e];
         *S::at4(ylds, b, q) = make_uint2((uint32_t)YT::from_float(y[0]) | (uint32_t)YT::from_float(y[1]) << 16,
                                          (uint32_t)YT::from_float(y[2]) | (uint32_t)YT::from_float(y[3]) << 16);
       }
@@ -445,35 +434,29 @@ __device__ __forceinline__ void finish_rows_lds(const GemmDev& a, void* Yout, co
     S::template drain<G>(Yout, a.ldo, ow, tw, ylds);
   });
 }
-// four neighbouring outputs of a token behind the scaling, stored
-template <typename Act>
-__device__ __forceinline__ void finish4(const Finish& f, void* Y, int ydt, int64_t ldy, int64_t t, int64_t o, int64_t c_out, float (&y)[4],
-                                        Act act) {
-  if (o + 3 < c_out) {
-    if (f.bias) {
-      const float4 b = *reinterpret_cast<const float4*>(f.bias + o);
-      y[0] += b.x; y[1] += b.y; y[2] += b.z; y[3] += b.w;
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = act(y[e]);
-    if (f.R) {
-      float r[4];
-      load_y4(f.R, ydt, t * f.ldr + o, r);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = f.mul ? y[e] * r[e] : y[e] + r[e];
-    }
-    store_y4(Y, ydt, t * ldy + o, y);
-    return;
+// Of four neighbouring outputs of a token what the epilogue reads, up to four floats (zeros where there are none)
+__device__ __forceinline__ void load4(const float* v, int64_t o, int64_t n, float (&x)[4]) {
+  x[0] = x[1] = x[2] = x[3] = 0.0f;
+  if (o + 3 < n) {
+    const float4 f = *reinterpret_cast<const float4*>(v + o);
+    x[0] = f.x; x[1] = f.y; x[2] = f.z; x[3] = f.w;
+  } else {
+    for (int e = 0; e < 3; ++e)
+      if (o + e < n) x[e] = v[o + e];
   }
-  for (int e = 0; e < 3; ++e) {
-    if (o + e >= c_out) return;
-    float v = act(f.bias ? y[e] + f.bias[o + e] : y[e]);
-    if (f.R) {
-      const float r = load_y(f.R, ydt, t * f.ldr + o + e);
-      v = f.mul ? v * r : v + r;
-    }
-    store_y1(Y, ydt, t * ldy + o + e, v);
-  }
+}
+__device__ __forceinline__ void load_second4(const Finish& f, int ydt, int64_t t, int64_t o, int64_t n, float (&x)[4]) {
+  x[0] = x[1] = x[2] = x[3] = 0.0f;
+  if (o + 3 < n) load_y4(f.R, ydt, t * f.ldr + o, x);
+  else
+    for (int e = 0; e < 3; ++e)
+      if (o + e < n) x[e] = load_y(f.R, ydt, t * f.ldr + o + e);
+}
+__device__ __forceinline__ void store_some4(void* Y, int ydt, int64_t ldy, int64_t t, int64_t o, int64_t n, const float (&y)[4]) {
+  if (o + 3 < n) store_y4(Y, ydt, t * ldy + o, y);
+  else
+    for (int e = 0; e < 3; ++e)
+      if (o + e < n) store_y1(Y, ydt, t * ldy + o + e, y[e]);
 }
 #endif
 
@@ -489,34 +472,41 @@ __device__ __forceinline__ void tile_epilogue(const GemmDev& a, const Acc& acc, 
   constexpr int WO = L::WO, WT = L::WT, NW = NWO * NWT, NT = NW * 64;
   constexpr int kStage = WO * L::STG * (WT / L::NTB) * 2;   // bytes of LDS per wave, see Staged
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const float* tsc = a.tok_scale ? a.tok_scale + (int64_t)cand * a.n_tok : nullptr;
+  [[maybe_unused]] const float* tsc = a.tok_scale ? a.tok_scale + (int64_t)cand * a.n_tok : nullptr;
 #if defined(__HIP_DEVICE_COMPILE__)
-  if constexpr (EPI >= EPI_FINISH) {      // (one candidate, tokens' steps)
-    constexpr int CLASS = EPI - EPI_FINISH;
-    if constexpr (YLDS) {
-      if (a.odt != TLQ_F32 && (o0 + NWO * WO <= a.c_out) && (t0 + BT <= a.n_tok)) {
-        unsigned char* ylds = reinterpret_cast<unsigned char*>(rows) + wave * kStage;
-        if (a.odt == TLQ_F16) finish_rows_lds<F16, CLASS, L>(a, a.Yout, acc, tsc, o0 + wo * WO, t0 + wt * WT, ylds);
-        else finish_rows_lds<BF16, CLASS, L>(a, a.Yout, acc, tsc, o0 + wo * WO, t0 + wt * WT, ylds);
-        return;
+  if constexpr (EPI >= EPI_FINISH) {
+    // (the accumulators are outputs but for the second matrix)
+    if (a.fin.R) {
+      if constexpr (YLDS) {
+        if (a.odt != TLQ_F32 && (o0 + NWO * WO <= a.c_out) && (t0 + BT <= a.n_tok)) {
+          unsigned char* ylds = reinterpret_cast<unsigned char*>(rows) + wave * kStage;
+          if (a.odt == TLQ_F16) second_rows_lds<F16, L>(a, a.Yout, acc, o0 + wo * WO, t0 + wt * WT, ylds);
+          else second_rows_lds<BF16, L>(a, a.Yout, acc, o0 + wo * WO, t0 + wt * WT, ylds);
+          return;
+        }
       }
-    }
-    static_for<0, L::NTB>([&](auto tbc) {
-      constexpr int tb = decltype(tbc)::value;
-      const int64_t t = t0 + wt * WT + L::tok(tb, lane);
-      if (t >= a.n_tok) return;
-      const float sg = tsc[t];
+      const bool mul = a.fin.mul;
+      static_for<0, L::NTB>([&](auto tbc) {
+        constexpr int tb = decltype(tbc)::value;
+        const int64_t t = t0 + wt * WT + L::tok(tb, lane);
+        if (t >= a.n_tok) return;
+        float r[L::NQ][4];      // (all of a token's loads at once)
 #pragma unroll
-      for (int q = 0; q < L::NQ; ++q) {
-        float y[4] = {sg * L::get(acc, q, tb, 0), sg * L::get(acc, q, tb, 1), sg * L::get(acc, q, tb, 2), sg * L::get(acc, q, tb, 3)};
-        const int64_t o = o0 + wo * WO + L::row(q, lane);
-        if (o < a.c_out) finish4(a.fin, a.Yout, a.odt, a.ldo, t, o, a.c_out, y, [&](float v) { return act_of<CLASS>(v, a.fin); });
-      }
-    });
-    return;
+        for (int q = 0; q < L::NQ; ++q) load_second4(a.fin, a.odt, t, o0 + wo * WO + L::row(q, lane), a.c_out, r[q]);
+#pragma unroll
+        for (int q = 0; q < L::NQ; ++q) {
+          float y[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = mul ? L::get(acc, q, tb, e) * r[q][e] : L::get(acc, q, tb, e) + r[q][e];
+          store_some4(a.Yout, a.odt, a.ldo, t, o0 + wo * WO + L::row(q, lane), a.c_out, y);
+        }
+      });
+      return;
+    }
+    tsc = nullptr;
   }
 #endif
-  if (EPI == EPI_STORE) {
+  if (EPI == EPI_STORE || EPI >= EPI_FINISH) {
     void* Yo = (unsigned char*)a.Yout + (int64_t)cand * a.o_cand_stride * (a.odt == TLQ_F32 ? 4 : 2);
     if constexpr (YLDS) {
       if (a.odt != TLQ_F32 && (o0 + NWO * WO <= a.c_out) && (t0 + BT <= a.n_tok) && (a.ldo % 8) == 0 &&
@@ -1027,6 +1017,38 @@ __device__ __forceinline__ void gemm_dma_body(const GemmDev& a) {
 
   if constexpr (std::is_same<T, Int8>::value) {   // sums of codes -> multiples of the output rows' steps
     const float* rsc = a.row_scale + (int64_t)cand * a.row_scale_stride;
+    if constexpr (EPI >= EPI_FINISH) {      // ... and outputs: the tokens' steps, the bias, the activation
+      float sg[JB];
+#pragma unroll
+      for (int j = 0; j < JB; ++j) {
+        const int64_t t = t0 + wt * WT + j * 16 + frow;
+        sg[j] = a.tok_scale[t < a.n_tok ? t : a.n_tok - 1];
+      }
+      // (rows' steps and biases four blocks of rows ahead: all of them at once need more registers than there are)
+      constexpr int AHEAD = IA < 4 ? IA : 4;
+      float r[AHEAD][4], bias[AHEAD][4];
+      auto fetch = [&](auto ic) __attribute__((always_inline)) {
+        constexpr int i = decltype(ic)::value, at = i % AHEAD;
+        const int64_t o = o0 + wo * WO + i * 16 + fq * 4;
+        load4(rsc, o, a.c_out, r[at]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bias[at][e] = 0.0f;
+        if (a.fin.bias) load4(a.fin.bias, o, a.c_out, bias[at]);
+      };
+      static_for<0, AHEAD>(fetch);
+      static_for<0, IA>([&](auto ic) __attribute__((always_inline)) {
+        constexpr int i = decltype(ic)::value, at = i % AHEAD;
+#pragma unroll
+        for (int j = 0; j < JB; ++j) {
+          const i32x4 v = __builtin_bit_cast(i32x4, acc[i][j]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            acc[i][j][e] = act_of<EPI - EPI_FINISH>(__builtin_fmaf(sg[j], r[at][e] * (float)v[e], bias[at][e]), a.fin);
+          if ((j & 1) || j == JB - 1) __builtin_amdgcn_sched_barrier(0);      // (eight at a time)
+        }
+        if constexpr (i + AHEAD < IA) fetch(std::integral_constant<int, i + AHEAD>{});
+      });
+    } else {
 #pragma unroll
     for (int i = 0; i < IA; ++i) {
       const int64_t o = o0 + wo * WO + i * 16 + fq * 4;
@@ -1045,6 +1067,7 @@ __device__ __forceinline__ void gemm_dma_body(const GemmDev& a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[i][j][e] = r[e] * (float)v[e];
       }
+    }
     }
   }
   // every LDS-DMA write has landed and every wave is past its last fragment read:

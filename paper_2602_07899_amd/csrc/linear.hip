@@ -7,19 +7,35 @@ namespace tlq {
 
 #if defined(__HIP_DEVICE_COMPILE__)
 // four neighbouring outputs of a token
-template <bool FIN>
 __device__ __forceinline__ void write4(const LinearI8Args& a, int64_t t, int64_t o, float st, const i32x4& s) {
   float y[4];
 #pragma unroll
   for (int r = 0; r < 4; ++r) y[r] = o + r < a.c_out ? st * (a.ws[o + r] * (float)s[r]) : 0.0f;
-  if constexpr (FIN) {
-    if (o < a.c_out) finish4(a.fin, a.Y, a.ydt, a.ldy, t, o, a.c_out, y, [&](float v) { return act_of(v, a.fin); });
-    return;
+  store_some4(a.Y, a.ydt, a.ldy, t, o, a.c_out, y);
+}
+// The same with LinearI8Args::fin behind it: what it reads is loaded before the sums are there, `is` where there are such outputs.
+struct Tail4 { float st, ws[4], bias[4], second[4]; };
+__device__ __forceinline__ void load_tail4(const LinearI8Args& a, int64_t t, int64_t o, bool is, Tail4& f) {
+  f.st = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) f.ws[e] = f.bias[e] = f.second[e] = 0.0f;
+  if (!is) return;
+  f.st = a.xs[t];
+  load4(a.ws, o, a.c_out, f.ws);
+  if (a.fin.bias) load4(a.fin.bias, o, a.c_out, f.bias);
+  if (a.fin.R) load_second4(a.fin, a.ydt, t, o, a.c_out, f.second);
+}
+__device__ __forceinline__ void finish4(const LinearI8Args& a, int64_t t, int64_t o, const Tail4& f, const i32x4& s) {
+  float y[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = __builtin_fmaf(f.st, f.ws[e] * (float)s[e], f.bias[e]);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = act_of(y[e], a.fin);
+  if (a.fin.R) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = a.fin.mul ? y[e] * f.second[e] : y[e] + f.second[e];
   }
-  if (o + 3 < a.c_out) store_y4(a.Y, a.ydt, t * a.ldy + o, y);
-  else
-    for (int r = 0; r < 3; ++r)
-      if (o + r < a.c_out) store_y1(a.Y, a.ydt, t * a.ldy + o + r, y[r]);
+  store_some4(a.Y, a.ydt, a.ldy, t, o, a.c_out, y);
 }
 #endif
 
@@ -46,6 +62,9 @@ __global__ __launch_bounds__(NW * 64) void linear_few_kernel(LinearI8Args a) {
     const int64_t t = t0 + n * 16 + l16 < a.n_tok ? t0 + n * 16 + l16 : a.n_tok - 1;
     x[n] = a.xc + t * a.ldx + fq * 32;
   }
+  const int64_t t = t0 + (wave < NT ? wave : 0) * 16 + l16;      // of the outputs that this lane writes, if its wave does
+  Tail4 tail;
+  if constexpr (FIN) load_tail4(a, t, o0 + fq * 4, wave < NT && t < a.n_tok && o0 + fq * 4 < a.c_out, tail);
   i32x4 acc[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) acc[n] = i32x4{0, 0, 0, 0};
@@ -77,8 +96,11 @@ __global__ __launch_bounds__(NW * 64) void linear_few_kernel(LinearI8Args a) {
   i32x4 s = red[0][wave][lane];
 #pragma unroll
   for (int v = 1; v < NW; ++v) s += red[v][wave][lane];
-  const int64_t t = t0 + wave * 16 + l16;
-  if (t < a.n_tok) write4<FIN>(a, t, o0 + fq * 4, a.xs[t], s);
+  if constexpr (FIN) {
+    if (t < a.n_tok && o0 + fq * 4 < a.c_out) finish4(a, t, o0 + fq * 4, tail, s);
+  } else if (t < a.n_tok) {
+    write4(a, t, o0 + fq * 4, a.xs[t], s);
+  }
 #endif
 }
 
@@ -207,7 +229,14 @@ __global__ __launch_bounds__(512) void linear_mid_kernel(LinearI8Args a, int spl
         if (o < a.c_out) *reinterpret_cast<i32x4*>(partial + ((int64_t)part * a.n_tok + t) * ((a.c_out + 3) & ~(int64_t)3) + o) = s;
         continue;
       }
-      write4<FIN>(a, t, o, a.xs[t], s);
+      if constexpr (FIN) {
+        if (o >= a.c_out) continue;
+        Tail4 tail;
+        load_tail4(a, t, o, true, tail);
+        finish4(a, t, o, tail, s);
+      } else {
+        write4(a, t, o, a.xs[t], s);
+      }
     }
   }
 #endif
@@ -219,10 +248,13 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinearI8Args a, int sp
   const int64_t quads = (a.c_out + 3) >> 2, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= a.n_tok * quads) return;
   const int64_t t = i / quads;
+  Tail4 tail;
+  if constexpr (FIN) load_tail4(a, t, (i - t * quads) * 4, true, tail);
   i32x4 s = *reinterpret_cast<const i32x4*>(partial + i * 4);
 #pragma unroll 8
   for (int p = 1; p < splits; ++p) s += *reinterpret_cast<const i32x4*>(partial + ((int64_t)p * a.n_tok * quads + i) * 4);
-  write4<FIN>(a, t, (i - t * quads) * 4, a.xs[t], s);
+  if constexpr (FIN) finish4(a, t, (i - t * quads) * 4, tail, s);
+  else write4(a, t, (i - t * quads) * 4, a.xs[t], s);
 #endif
 }
 

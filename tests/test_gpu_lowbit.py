@@ -183,16 +183,22 @@ def _padded(c, gpu, extra=0):
     return t
 
 
-def _linear_bound(p, v, a, y, kind, r, mul, od):
-    """The sum as a float and its two products (3 roundings), the bias (1); the activation's derivative is 1.13 at most, its own error: an
-    exponential whose argument is off by 3 roundings of itself and 8 further ones, for the normal distribution 20; what is below
-    1e-36 may be zero; the second matrix (1); the output."""
+def _linear_bound(p, v, a, y, kind, r, mul, od, x=None):
+    """The sum as a float and its two products (3 roundings), the bias (1); the activation's derivative is 1.13 at most.  Its own error:
+    logistic, an exponential whose argument x is off by 4 roundings of itself (two constants, a product, a sum with one of equal
+    sign, a product) and 8 further ones; normal distribution, 20, and 3 of v^2 / 2 (a constant, two products), in the tail that
+    is taken from v above zero; what is below 1e-36 may be zero; the second matrix (1); the output."""
     dv = np.abs(p) * 3.1 * U + np.abs(v) * 1.1 * U
+    x = v if x is None else x
     if kind == 0:
         da = dv
+    elif kind == 3:
+        tail = np.where(x >= 0, np.abs(x - a), np.abs(a))
+        da = 1.13 * dv + (tail * (20 + 1.5 * np.minimum(x * x, 1e4)) + np.abs(a)) * U + 1e-36
     else:
-        x = np.abs(v if kind == 1 else 1.6 * (v + 0.0447 * v ** 3))
-        da = 1.13 * dv + np.abs(a) * ((3 * x + 8) * U if kind != 3 else 20 * U) + 1e-36
+        arg = np.minimum(np.abs(x if kind == 1 else 1.6 * (x + 0.0447 * np.clip(x, -1e3, 1e3) ** 3)), 1e4)
+        tail = np.where(x >= 0, np.abs(x - a), np.abs(a))
+        da = 1.13 * dv + (tail * 4 * arg + np.abs(a) * 8) * U + 1e-36
     if r is not None:
         da = (da * np.abs(r) if mul else da) + np.abs(y) * U
     return da * 1.01 + (np.abs(y) + da) * HALF[od] + TINY[od] * 1.01
@@ -286,8 +292,7 @@ def test_activations_over_their_range(gpu, kind, n):
     tlq.linear_codes(_padded(codes, gpu), dev(np.ones(n, np.float32), gpu), ci, _padded(w, gpu), dev(v, gpu), tlq.params(yref_dtype=tlq.F32), y, act=kind)
     v = v.astype(np.float64)
     a = lo.act(v, kind)
-    within(host(y), np.broadcast_to(a, (n, co)), _linear_bound(0 * v, 0 * v, a, a, kind, None, False, "f32") +
-           (np.abs(a) * 3 * np.abs(v if kind == 1 else np.clip(1.6 * (v + 0.0447 * v ** 3), -100, 100)) * U if kind != 3 else 0.0))
+    within(host(y), np.broadcast_to(a, (n, co)), _linear_bound(0 * v, 0 * v, a, a, kind, None, False, "f32", v))
 
 
 def test_linear_codes_extreme_sums(gpu):
