@@ -488,8 +488,8 @@ typedef struct tlq_kv4_cache {
  *   step = max(max |x|, 1e-5) / 7 rounded to bf16 and then to half (its 8 significant bits keep code * step exact), 9344 at most;
  *   code = clip(rint(x / step), -7, 7).
  * Infinities count as +-7 and NaN as 0, neither has a part in the step.  Everything that is not a new token's stays as it was.
- * K, V and pages that are shared as in tlq_kv_append; n_seq (n_kv_heads head_dim (max_new / 8 + 2) / 2048 + 1) below 2^23, here and in
- * tlq_kv4_read (max_new at most n_tok there). */
+ * K, V and pages that are shared as in tlq_kv_append.  Here and in tlq_kv4_read, with e = (min(max_new, n_tok) + 14) / 8 rounded down
+ * and both quotients rounded up, n_seq (n_kv_heads (e head_dim / 512) / 4) is below 2^23. */
 tlq_status tlq_kv4_append(const void* K, int64_t ldk, const void* V, int64_t ldv, int64_t n_tok, const tlq_kv_batch* b,
                           const tlq_kv4_cache* c, const tlq_params* p, void* stream);
 /* tlq_kv4_read: what the tokens of a batch's rows stand for: row r of K_out and V_out [n_tok, n_kv_heads * head_dim] x_dtype, 16-byte aligned, strides

@@ -1083,10 +1083,9 @@ static tlq_status check_kv4(const tlq_kv_batch* b, const tlq_kv4_cache* c) {
     return TLQ_ERR_ALIGN;
   return TLQ_OK;
 }
-// blocks of 256 threads, each with eight tokens of eight channels, for K and for V: fewer than 2^32 threads a launch
+// blocks of 256 threads, for K and for V: fewer than 2^32 threads a launch
 static bool kv4_rows_fit(int64_t n_tok, const tlq_kv_batch& b, const tlq_kv4_cache& c) {
-  const int64_t most = b.max_new < n_tok ? b.max_new : n_tok;
-  return ((int64_t)c.n_kv_heads * c.head_dim * (most / 8 + 2) / 2048 + 1) * b.n_seq < (1LL << 23);
+  return kv4_cache_blocks(n_tok, b, c) * b.n_seq < (1LL << 23);
 }
 
 tlq_status tlq_kv4_append(const void* K, int64_t ldk, const void* V, int64_t ldv, int64_t n_tok, const tlq_kv_batch* b,

@@ -301,6 +301,7 @@ hipError_t launch_kv_attention(const void* Q, int64_t ldq, int64_t n_tok, int n_
                                const tlq_kv_cache& c, bool bf16, void* Out, int64_t ldo, void* workspace, hipStream_t stream);
 
 // the 4-bit cache (kv4_cache.hip, kv4_attention.hip)
+int64_t kv4_cache_blocks(int64_t n_tok, const tlq_kv_batch& b, const tlq_kv4_cache& c);      // of a launch, for a sequence
 hipError_t launch_kv4_append(const void* K, int64_t ldk, const void* V, int64_t ldv, int64_t n_tok, const tlq_kv_batch& b,
                              const tlq_kv4_cache& c, bool bf16, hipStream_t stream);
 hipError_t launch_kv4_read(void* K, int64_t ldk, void* V, int64_t ldv, int64_t n_tok, const tlq_kv_batch& b,

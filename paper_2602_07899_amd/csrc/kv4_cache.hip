@@ -12,7 +12,6 @@ typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 struct Kv4CacheDev {
   const uint16_t *K, *V; uint16_t *Ko, *Vo; int64_t ldk, ldv, n_tok;      // rows in, or rows out
   tlq_kv_batch b; tlq_kv_cache c; Kv4Dev d;      // (c: sizes)
-  int groups;                                     // eights of tokens that a sequence's new ones can lie in
 };
 
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -260,12 +259,10 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4CacheDev a) {
   else kv4_read_piece<T, DH, false>(a);
 }
 
-static dim3 kv4_cache_grid(const Kv4CacheDev& a, unsigned z) {
-  return dim3((unsigned)ceil_div((int64_t)a.c.n_kv_heads * ceil_div(a.groups, 512 / a.c.head_dim), 4), (unsigned)a.b.n_seq, z);
-}
-int64_t kv4_cache_groups(int64_t n_tok, const tlq_kv_batch& b) {
-  const int64_t most = b.max_new < n_tok ? b.max_new : n_tok;
-  return (most - 1 + 7) / 8 + 1;
+// eights of tokens that a sequence's new ones can lie in, wherever they begin; a wave has 512 / head_dim of them for a head
+int64_t kv4_cache_blocks(int64_t n_tok, const tlq_kv_batch& b, const tlq_kv4_cache& c) {
+  const int64_t eights = ((b.max_new < n_tok ? b.max_new : n_tok) + 14) / 8;
+  return ceil_div(c.n_kv_heads * ceil_div(eights, 512 / c.head_dim), 4);
 }
 
 hipError_t launch_kv4_append(const void* K, int64_t ldk, const void* V, int64_t ldv, int64_t n_tok, const tlq_kv_batch& b,
@@ -274,8 +271,7 @@ hipError_t launch_kv4_append(const void* K, int64_t ldk, const void* V, int64_t 
   Kv4CacheDev a{};
   a.K = (const uint16_t*)K; a.V = (const uint16_t*)V; a.ldk = ldk; a.ldv = ldv; a.n_tok = n_tok;
   a.b = b; a.c = kv4_sizes(c); a.d = {c.k, c.k_step, c.v, c.v_step};
-  a.groups = (int)kv4_cache_groups(n_tok, b);
-  const dim3 grid = kv4_cache_grid(a, 2);
+  const dim3 grid((unsigned)kv4_cache_blocks(n_tok, b, c), (unsigned)b.n_seq, 2);
   auto pick = [&](auto t) {
     using T = decltype(t);
     if (c.head_dim == 128) kv4_append_kernel<T, 128><<<grid, 256, 0, stream>>>(a);
@@ -291,8 +287,7 @@ hipError_t launch_kv4_read(void* K, int64_t ldk, void* V, int64_t ldv, int64_t n
   Kv4CacheDev a{};
   a.Ko = (uint16_t*)K; a.Vo = (uint16_t*)V; a.ldk = ldk; a.ldv = ldv; a.n_tok = n_tok;
   a.b = b; a.c = kv4_sizes(c); a.d = {c.k, c.k_step, c.v, c.v_step};
-  a.groups = (int)kv4_cache_groups(n_tok, b);
-  const dim3 grid = kv4_cache_grid(a, K && V ? 2 : 1);
+  const dim3 grid((unsigned)kv4_cache_blocks(n_tok, b, c), (unsigned)b.n_seq, K && V ? 2 : 1);
   auto pick = [&](auto t) {
     using T = decltype(t);
     if (c.head_dim == 128) kv4_read_kernel<T, 128><<<grid, 256, 0, stream>>>(a);

@@ -119,9 +119,17 @@ def test_cache_refusals():
         assert call(ldk=248) == call(ldv=128) == tlq.ERR_SHAPE
         assert call(K=ODD) == call(V=ODD) == call(ldk=260) == call(ldv=260) == tlq.ERR_ALIGN
         # more threads than a launch can have, and the last that fits (found behind: the address)
-        big = dict(n=1 << 20, n_seq=32767, max_new=4064, max_len=4064)       # 2 x 128 x (508 + 2) / 2048 + 1 = 64 blocks a sequence
+        big = dict(n=1 << 20, n_seq=32767, max_new=4064, max_len=4064)       # 2 x ceil(509 / 4) / 4 = 64 blocks a sequence
         assert call(**{**big, "max_new": 4096 * 4, "max_len": 1 << 20, "n_seq": 65535}) == tlq.ERR_SHAPE
         assert call(K=ODD, **big) == tlq.ERR_ALIGN
+        # one token of many heads: a wave each.  128 x 65535 blocks are fewer than 2^23, 129 are not
+        one = dict(n=1 << 20, n_seq=65535, max_new=1, max_len=1, n_kv_heads=512, ldk=513 * 128, ldv=513 * 128)
+        assert call(K=ODD, **one) == tlq.ERR_ALIGN
+        assert call(**{**one, "n_kv_heads": 513}) == tlq.ERR_SHAPE
+        # 57 tokens lie in eight eights at most, a wave's of 64 channels; 58 can lie in nine
+        most = dict(n=1 << 20, n_seq=65535, max_new=57, max_len=58, n_kv_heads=512, head_dim=64, ldk=512 * 64, ldv=512 * 64)
+        assert call(K=ODD, **most) == tlq.ERR_ALIGN
+        assert call(**{**most, "max_new": 58}) == tlq.ERR_SHAPE
     assert append(K=None) == append(V=None) == tlq.ERR_NULL
     assert read(K=None, ldk=0, V=ODD) == read(V=None, ldv=0, K=ODD) == tlq.ERR_ALIGN
     assert attend(Q=None) == attend(Out=None) == tlq.ERR_NULL
