@@ -502,6 +502,16 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kv4_prompt_kernel(Kv4At
     using Second = std::integral_constant<int, 1>;
 #pragma unroll
     for (int at = 0; at < 4; ++at) read_v(at);
+    if (unit == k0) {      // the first reference, if there is a key (356 -> 353 us; the weights need no second go for it)
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        float mx = sc[0][n][0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) mx = fmaxf(mx, sc[e >> 2][n][e & 3]);
+        mx = column_max(mx) * fac[n];
+        ref[n] = mx > kUnset ? mx - kTop : kUnset;
+      }
+    }
     static_for<0, 8>([&](auto ec) { weigh(First{}, ec); });
     take(First{});
     static_for<0, ND>([&](auto dc) {
