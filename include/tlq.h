@@ -434,8 +434,8 @@ tlq_status tlq_kv_attention(const void* Q, int64_t ldq, int64_t n_tok, int32_t n
  * norm's weight and the searched scales' reciprocals are one factor w: float [c], 16-byte aligned, or NULL (ones).
  * H, Z, H_out [n, c] x_dtype, 16-byte aligned, strides multiples of 8; H_out may be NULL (not wanted), or H or Z with the same
  * stride; no other overlap.  c a multiple of 8, at most 65536; bits 2..8; eps >= 0 (with 0 a row of zeros gives NaN).  codes, ldc and steps as
- * in tlq_row_codes.  A row with h that is not finite, or whose mean with eps is 0, has a NaN step (and with it every product of the row)
- * and undefined codes.  n at most 2^21. */
+ * in tlq_row_codes.  A row with h or r that is not finite (a mean and eps of 0, or near it) has a NaN step (and with it every
+ * product of the row) and undefined codes.  n at most 2^21. */
 tlq_status tlq_add_norm_codes(const void* H, int64_t ldh, const void* Z, int64_t ldz, int64_t n, int64_t c, const float* w,
                               float eps, int32_t bits, const tlq_params* p, void* H_out, int64_t ldho, int8_t* codes,
                               int64_t ldc, float* steps, void* stream);
@@ -445,7 +445,7 @@ tlq_status tlq_add_norm_codes(const void* H, int64_t ldh, const void* Z, int64_t
  * codes int8 [n_tok, ldx] and w_codes with zeros behind c_in up to the next multiple of 128, 16-byte aligned, strides (bytes)
  * multiples of 16 and below 2^22; steps float [n_tok].  bias: float [c_out], 16-byte aligned, or NULL.  act: one of tlq_act.
  * R [n_tok, c_out] yref_dtype, aligned as Y, or NULL (mul has to be 0 then); Y may be R with the same stride; no other
- * overlap.  Float arithmetic, one rounding to yref_dtype at the end.  c_in, c_out, w_steps, Y as in tlq_linear_i8; of p the
+ * overlap.  Float arithmetic, one rounding to yref_dtype at the end; NaN and +infinity pass an activation, -infinity may give NaN.  c_in, c_out, w_steps, Y as in tlq_linear_i8; of p the
  * type of Y is read.  Workspace from the query. */
 typedef enum {
   TLQ_ACT_NONE = 0,

@@ -295,6 +295,29 @@ def test_activations_over_their_range(gpu, kind, n):
     within(host(y), np.broadcast_to(a, (n, co)), _linear_bound(0 * v, 0 * v, a, a, kind, None, False, "f32", v))
 
 
+@pytest.mark.parametrize("kind", [0, 1, 2, 3])
+@pytest.mark.parametrize("n,ci,co", [(3, 264, 50), (40, 2568, 13000), (64, 8200, 2203), (300, 4104, 263), (2501, 136, 2050)])
+def test_linear_codes_of_numbers_that_are_not_finite(gpu, kind, n, ci, co):
+    """Infinities and NaN in a bias, a row whose step is NaN (as the norm marks it): they stay in their outputs and rows."""
+    import torch
+    g = np.random.default_rng([79, n])
+    codes, steps, w, ws = _linear_case(g, n, ci, co)
+    bias = g.standard_normal(co).astype(np.float32)
+    X, W, WS, p = _padded(codes, gpu), _padded(w, gpu), dev(ws, gpu), tlq.params()
+    clean, odd = (torch.empty((n, -(-co // 8) * 8), dtype=torch.float16, device=gpu)[:, :co] for _ in range(2))
+    tlq.linear_codes(X, dev(steps, gpu), ci, W, WS, p, clean, bias=dev(bias, gpu), act=kind)
+    steps[n // 2], bias[5], bias[co - 1], bias[17] = np.nan, np.inf, np.nan, -np.inf
+    tlq.linear_codes(X, dev(steps, gpu), ci, W, WS, p, odd, bias=dev(bias, gpu), act=kind)
+    rest = torch.ones((n, co), dtype=torch.bool, device=gpu)
+    rest[n // 2] = rest[:, 5] = rest[:, co - 1] = rest[:, 17] = False
+    assert torch.equal(odd[rest], clean[rest])
+    assert bool(odd[n // 2].isnan().all()) and bool(odd[:, co - 1].isnan().all())
+    there = [t for t in range(n) if t != n // 2]
+    assert bool((odd[there, 5] == float("inf")).all())
+    low = odd[there, 17]
+    assert bool({0: low == float("-inf"), 3: low == 0}.get(kind, low.isnan()).all())
+
+
 def test_linear_codes_extreme_sums(gpu):
     """The largest sums that the codes allow, 2^30, with a bias that nearly cancels them."""
     import torch
