@@ -1062,7 +1062,7 @@ tlq_status tlq_linear_codes(const int8_t* codes, int64_t ldx, const float* steps
   const Finish fin{bias, R, ldr, act, mul, tanh_form ? -2.30220820f : -1.44269504f, tanh_form ? -0.102943240f : 0.0f};      // (finish.h)
   const bool finish = bias || R || act != TLQ_ACT_NONE;
   const LinearI8Args l{codes, n_tok, ldx, steps, w_codes, c_out, ldw, k, w_steps, Y, ldy, p->yref_dtype, finish, fin};
-  const LinearKind kind = linear_kind(n_tok, c_out, k);
+  const LinearKind kind = linear_codes_kind(n_tok, c_out, k);
   if (kind == kLinearFew) return hip_status(launch_linear_few(l, st));
   if (kind == kLinearMid) return hip_status(launch_linear_mid(l, linear_mid_splits(n_tok, c_out, k), (int*)workspace, st));
   GemmArgs g{};
@@ -1070,9 +1070,9 @@ tlq_status tlq_linear_codes(const int8_t* codes, int64_t ldx, const float* steps
   g.i8_k = c_in; g.c_in = k / 2; g.ldx = ldx / 2; g.ldw = ldw / 2;      // (in units of 16 bits)
   g.Yout = Y; g.ldo = ldy; g.yout_dtype = p->yref_dtype;
   g.wide_patch = true;
-  g.tile() = gemm_tile(g, kTileAll, INT64_MAX);
+  g.tile() = gemm_tile(g, kTileAll | kTileHalf, INT64_MAX);
   g.fin = fin;
-  return hip_status(finish ? launch_gemm_finish(g, st) : launch_gemm_store(g, st));
+  return hip_status(finish || (g.small && g.tok_blocks == 2) ? launch_gemm_finish(g, st) : launch_gemm_store(g, st));
 }
 
 static tlq_status check_kv4(const tlq_kv_batch* b, const tlq_kv4_cache* c) {

@@ -192,7 +192,7 @@ struct FinalDev {
 };
 
 // Output tile of the pipelined contraction: 256 rows x 64 tok_blocks tokens (3, 4 or 5 blocks of 16 tokens a wave; 0 = 4),
-// or small: 128 rows x 32 tok_blocks (0 = 4, or 2: 128 x 64, not of integer codes), for stores (with tri only 128 x 128) and fp16 losses
+// or small: 128 rows x 32 tok_blocks (0 = 4, or 2: 128 x 64, of integer codes only with launch_gemm_finish), for stores (with tri only 128 x 128) and fp16 losses
 // (128 x 128 with tok_partial: tok_blocks has to say 4).
 // gemm_tile says which is the fastest.
 struct GemmTile { bool small; int tok_blocks; };
@@ -276,6 +276,7 @@ struct LinearI8Args {
 enum LinearKind { kLinearFew, kLinearMid, kLinearTiles };
 constexpr int64_t kLinearMidTokens = 256;
 LinearKind linear_kind(int64_t n_tok, int64_t c_out, int64_t K);
+LinearKind linear_codes_kind(int64_t n_tok, int64_t c_out, int64_t K);
 hipError_t launch_linear_few(const LinearI8Args& a, hipStream_t stream);
 // for more tokens; partial: scratch of kLinearMidInts ints for each token of the first 64, not used with one split
 constexpr int64_t kLinearMidInts = 256 * 128;      // (splits times blocks of 128 outputs and 64 tokens are at most 256)

@@ -430,8 +430,8 @@ hipError_t launch_gemm_store(const GemmArgs& g, hipStream_t stream) {
   return g.bf16 ? launch_gemm<BF16, EPI_STORE>(g, name, stream) : launch_gemm<F16, EPI_STORE>(g, name, stream);
 }
 hipError_t launch_gemm_finish(const GemmArgs& g, hipStream_t stream) {
-  if (!g.i8_k || g.n_cand != 1 || g.tri || g.bf16 || !g.tok_scale || g.Yref || (g.small && g.tok_blocks != 0 && g.tok_blocks != 4) || !pipelined_ok(g) ||
-      !g.row_scale || (g.c_in % kDmaBK) != 0)
+  if (!g.i8_k || g.n_cand != 1 || g.tri || g.bf16 || !g.tok_scale || g.Yref || (g.small && g.tok_blocks != 0 && g.tok_blocks != 2 && g.tok_blocks != 4) ||
+      !pipelined_ok(g) || !g.row_scale || (g.c_in % kDmaBK) != 0)
     return hipErrorInvalidValue;
   const GemmDev d = make_dev(g);
   const int64_t blocks = dev_blocks(d);

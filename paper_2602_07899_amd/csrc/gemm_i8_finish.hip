@@ -1,6 +1,11 @@
 // Products of activation codes with weight codes on int8 MFMA with a bias, an activation and a second matrix behind them: the
 // tiles of gemm_i8.hip with another epilogue.  The classes of activations are kernels of their own: an activation is written out for
-// each of a lane's 64 to 160 outputs, and code that a tile runs once is fetched cold.
+// each of a lane's 32 to 160 outputs, and code that a tile runs once is fetched cold.  Bound by the matrix instructions and the
+// LDS reads that feed them, as without an epilogue: 10,240 x 5120 x 13824 with SiLU and a second matrix 647 us behind other work, 2.24
+// POP/s (a large library product of codes reaches 2.01; the second matrix adds 283 MB).  By latency where
+// tiles are few; then they are 128 x 64, one a CU, as in gemm_half.hip: 128 x 128 and these, us, tokens x channels x outputs:
+// 613 x 1096 x 1399 14.4 9.7, 512 x 1024 x 1024 10.8 7.7, 300 x 4096 x 2048 26.6 16.9, 8000 x 1096 x 250 19.1 12.3; 288 of
+// them would be a second round, 1100 x 1000 x 2000 stays 15.5.
 #include "contraction.h"
 
 namespace tlq {
@@ -15,6 +20,7 @@ static hipError_t launch(const GemmDev& d, GemmTile tile, unsigned blocks, hipSt
   if (!tile.small && tile.tok_blocks == 3) gemm_i8_finish_kernel<2, CLASS, 2, 3><<<blocks, 512, 0, stream>>>(d);
   else if (!tile.small && tile.tok_blocks == 5) gemm_i8_finish_kernel<2, CLASS, 2, 5><<<blocks, 512, 0, stream>>>(d);
   else if (!tile.small) gemm_i8_finish_kernel<2, CLASS, 2, 4><<<blocks, 512, 0, stream>>>(d);
+  else if (tile.tok_blocks == 2) gemm_i8_finish_kernel<4, CLASS, 1, 2><<<blocks, 256, 0, stream>>>(d);
   else if ((int64_t)d.tiles_o * d.tiles_t <= 256) gemm_i8_finish_kernel<4, CLASS, 1, 4><<<blocks, 256, 0, stream>>>(d);
   else gemm_i8_finish_kernel<2, CLASS, 1, 4><<<blocks, 256, 0, stream>>>(d);
   return hipGetLastError();

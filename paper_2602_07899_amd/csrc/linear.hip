@@ -280,6 +280,24 @@ LinearKind linear_kind(int64_t n_tok, int64_t c_out, int64_t K) {
   return n_tok <= kLinearMidTokens && ceil_div(n_tok, 128) * ceil_div(c_out, 128) <= 64 && K >= 2048 ? kLinearMid : kLinearTiles;
 }
 
+// Codes that are there already have tiles of 128 x 64 too (gemm_i8_finish.hip), up to one a CU.  Kernels of products with bias and an
+// activation, us, the rule above and those tiles (their number), tokens x channels x outputs:
+//   few:  1 x 4096 x 14336 (112) 15.5 16.6     16 x 2048 x 14336 (112) 12.7 12.1     32 x 1024 x 14336 (112) 12.4 11.2
+//         1 x 2048 x 28672 (224) 18.2 15.5     16 x 512 x 28672 (224) 11.7 8.8       32 x 512 x 14336 (112)   8.4  9.5
+//        48 x 1024 x 9216 (72)   12.1 10.7     64 x 256 x 9216 (72)    8.8 6.7       64 x 1024 x 14336 (112) 18.2  8.6
+//   mid: 16 x 4096 x 14336 (112) 20.1 15.9     64 x 4096 x 11008 (86) 19.1 15.7     128 x 4096 x 4096 (64)   15.0 15.6
+//        32 x 4096 x 11008 (86)  16.7 16.2     64 x 8192 x 14336 (112) 33.7 29.3    256 x 4096 x 2560 (80)   17.1 15.6
+//       128 x 8192 x 6144 (96)   28.4 26.4    256 x 8192 x 4096 (128) 28.9 24.8     256 x 8192 x 1024 (32)   17.0 24.0
+//        64 x 11008 x 14336 (112) 50.0 58.7    64 x 11008 x 16640 (130) 80.1 65.0   128 x 16384 x 8448 (132) 84.2 62.5
+// (the mid kernel splits the channels of up to 128 tiles).
+LinearKind linear_codes_kind(int64_t n_tok, int64_t c_out, int64_t K) {
+  const LinearKind kind = linear_kind(n_tok, c_out, K);
+  const int64_t tiles = ceil_div(n_tok, 64) * ceil_div(c_out, 128);
+  if (tiles > 256) return kind;
+  if (kind == kLinearMid) return tiles > 128 || (tiles >= 80 && K <= 8192) ? kLinearTiles : kind;
+  return kind == kLinearFew && n_tok <= 64 && (ceil_div(n_tok, 16) + 1) * tiles >= 320 ? kLinearTiles : kind;
+}
+
 int linear_mid_splits(int64_t n_tok, int64_t c_out, int64_t K) {
   const int64_t blocks = ceil_div(c_out, 128) * ceil_div(n_tok, 64), most = ceil_div(K, kMidStage);
   int64_t s = 256 / blocks;

@@ -211,9 +211,11 @@ EPILOGUES = [(1, 3, "mul"), (1, 0, "add"), (0, 1, "mul"), (1, 2, ""), (0, 3, "")
 @pytest.mark.parametrize("out", ["f16", "bf16", "f32"])
 @pytest.mark.parametrize("n,ci,co,kernels", [
     (1, 8, 1, FEW), (1, 4096, 16, FEW), (2, 72, 3, FEW), (17, 136, 31, FEW), (33, 2056, 50, FEW), (64, 384, 130, FEW), (300, 1096, 263, FEW),
-    (16, 8200, 9001, MID), (40, 2568, 13000, MID), (64, 8200, 2203, MID), (200, 4104, 1003, MID), (33, 512, 70001, ONE),
-    # tiles of 128 x 128, at most one a CU and more; of 256 outputs x 192, 256 and 320 tokens; ragged and whole
-    (300, 4104, 263, TILES), (1000, 264, 2051, TILES), (1024, 256, 2048, TILES), (2501, 136, 2050, TILES), (6391, 136, 2557, TILES),
+    (16, 8200, 9001, MID), (40, 8200, 8001, MID), (64, 8200, 2203, MID), (200, 4104, 1003, MID), (33, 512, 70001, ONE),
+    # tiles of 128 outputs x 64 tokens, where they are one a CU at most; of 128 x 128, as many and more; of 256 outputs x 192,
+    # 256 and 320 tokens; ragged and whole
+    (1, 136, 20481, TILES), (16, 264, 32768, TILES), (40, 2568, 13000, TILES), (64, 128, 8192, TILES), (130, 2184, 3401, TILES), (300, 4104, 263, TILES),
+    (1152, 256, 2048, TILES), (1000, 264, 2051, TILES), (1024, 256, 2048, TILES), (2501, 136, 2050, TILES), (6391, 136, 2557, TILES),
     (2496, 128, 4096, TILES), (4001, 136, 2051, TILES), (4000, 128, 4002, TILES), (4096, 128, 4096, TILES), (4800, 128, 4096, TILES), (8001, 136, 2051, TILES)])
 def test_linear_codes(gpu, out, n, ci, co, kernels):
     """Every kernel of the product, each named, with every activation, a bias, a second matrix added and multiplied."""
