@@ -240,7 +240,15 @@ __global__ __launch_bounds__(256, 3) void kv4_few_kernel(Kv4AttnDev a) {
 // 128 rows of a sequence and key head against one split of the keys, 32 rows a wave, 64 keys a step.  The keys and values of
 // a step are widened once for the block on their way into LDS: what comes from memory during one step is written during
 // the next into the stage that nobody reads (one barrier a step).  All row tiles of a sequence and key head run on one XCD, the
-// longest first, as far as the pairs can be dealt out evenly.
+// longest first, as far as the pairs can be dealt out evenly.  Tiles are counted from the last row, so that the one that is not
+// full is the one with the fewest keys: 16 x 1200 tokens x 40 heads 366 -> 354 us, 1000 behind 1000 others x 32 433 -> 414, 4 x 2400
+// 254 -> 251, 16 x 200 40 -> 42.
+//   Bound by the waits of two waves a SIMD for each other, for LDS and at the barrier.  9600 tokens x 40 heads 1038 us, 910
+// TFLOP/s where a large library product of halves reaches 1180; 16 x 1200 x 40 353, 670 TFLOP/s, since a block has 10 steps on average
+// there, the diagonal's half of them idle for half of its waves, and begins and ends with a chain of loads and stores.  Of a wave's time
+// 29 % issues vector instructions, of the SIMDs' 26 % is matrix products.  Left out for measurement: widening 42 us, exponentials 32.
+// Not better, us for 16 x 1200 x 40: a step in four phases that interleave two of them 469 against 371, values staged in the
+// second product 5 % slower, 16 rows a wave and four waves a SIMD 493 against 359 (LDS is read twice as often).
 template <typename T, int DH>
 __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kv4_prompt_kernel(Kv4AttnDev a) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -273,7 +281,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kv4_prompt_kernel(Kv4At
     if (sh >= a.n_pairs) return;
   }
   const uint32_t turn = a.n_splits == 1 ? which : which / (uint32_t)a.n_splits;
-  const int tile = a.tiles - 1 - (int)turn, split = (int)(which - turn * a.n_splits);
+  const int split = (int)(which - turn * a.n_splits);
   const int s = (int)a.by_heads.of(sh), hk = (int)(sh - s * a.by_heads.d);
   const int k0 = split * a.chunk;
   // Table entries are the same for the whole block (scalar loads, a step before the pages they name are loaded, the first beside the
@@ -290,18 +298,18 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kv4_prompt_kernel(Kv4At
   };
   entries(k0);
   const KvSeq q = kv_sequence(a.b, a.c.page, a.n_tok, s);
-  const uint32_t rows = (uint32_t)q.n_new * a.group, first_row = (uint32_t)tile * 128;
-  if (first_row >= rows) return;
-  auto last_key = [&](uint32_t r) {      // number of keys that rows up to r see
-    const int p = q.first + (int)a.by_group.of(r < rows - 1 ? r : rows - 1);
+  const int rows = q.n_new * a.group, first_row = rows - ((int)turn + 1) * 128;      // (rows below 0: there are none)
+  if (first_row <= -128) return;
+  auto last_key = [&](int r) {      // number of keys that rows up to r see
+    const int p = q.first + (int)a.by_group.of(r > 0 ? (uint32_t)r : 0);
     return p + 1 < q.len ? p + 1 : q.len;
   };
   const int end = last_key(first_row + 127);
   if (k0 >= end && a.n_splits > 1) return;
   const int k1 = end - k0 < a.chunk ? end : k0 + a.chunk;
-  const uint32_t wrow = first_row + wave * 32;
-  const int wend = wrow < rows ? (last_key(wrow + 31) < k1 ? last_key(wrow + 31) : k1) : 0;    // keys of this wave
-  const int wfull = wrow < rows ? last_key(wrow) : 0;                                          // keys that all of its rows see
+  const int wrow = first_row + wave * 32;
+  const int wend = wrow > -32 ? (last_key(wrow + 31) < k1 ? last_key(wrow + 31) : k1) : 0;     // keys of this wave
+  const int wfull = wrow > -32 ? last_key(wrow) : 0;                                           // keys that all of its rows see
 
   f32x4 acc[ND][2];
 #pragma unroll
@@ -397,7 +405,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kv4_prompt_kernel(Kv4At
   int pos[2];
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
-    const uint32_t r = wrow + n * 16 + l16 < rows ? wrow + n * 16 + l16 : rows - 1;
+    const uint32_t r = wrow + n * 16 + l16 > 0 ? (uint32_t)(wrow + n * 16 + l16) : 0;
     const int qi = (int)a.by_group.of(r), g = (int)(r - qi * a.group);
     pos[n] = q.first + qi;
     const uint16_t* p = a.Q + (q.row0 + qi) * a.ldq + ((int64_t)hk * a.group + g) * DH + fq * 8;
@@ -537,8 +545,8 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kv4_prompt_kernel(Kv4At
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
     ref[n] = ref_of(ref[n]);
-    const uint32_t r = wrow + n * 16 + l16;
-    if (r >= rows) continue;
+    if (wrow + n * 16 + l16 < 0) continue;
+    const uint32_t r = (uint32_t)(wrow + n * 16 + l16);
     const uint32_t qi = a.by_group.of(r);
     const int64_t token = q.row0 + qi, head = (int64_t)hk * a.group + (r - qi * a.group);
     if (a.n_splits > 1) {
@@ -587,7 +595,7 @@ hipError_t launch_kv4_attention(const void* Q, int64_t ldq, int64_t n_tok, int n
     else bf16 ? pick(BF16{}, W64{}) : pick(F16{}, W64{});
   }
   if (hipError_t e = hipGetLastError(); e != hipSuccess || p.n_splits == 1) return e;
-  return launch_kv_join(p, a, bf16, stream);
+  return launch_kv_join(p, a, p.prompt, bf16, stream);
 }
 
 }  // namespace tlq

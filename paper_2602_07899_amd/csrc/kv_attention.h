@@ -37,7 +37,7 @@ struct KvPlan { bool prompt; int rows, tiles, n_splits, chunk; size_t acc_at, by
 KvPlan kv_plan(int64_t n_tok, int n_heads, const tlq_kv_batch& b, const tlq_kv_cache& c);      // (sizes are read, no pointer)
 KvAttnDev kv_attn_dev(const KvPlan& p, const void* Q, int64_t ldq, int64_t n_tok, int n_heads, float scale, const tlq_kv_batch& b,
                       const tlq_kv_cache& c, void* Out, int64_t ldo, void* workspace, dim3* grid);
-hipError_t launch_kv_join(const KvPlan& p, const KvAttnDev& a, bool bf16, hipStream_t stream);
+hipError_t launch_kv_join(const KvPlan& p, const KvAttnDev& a, bool from_last, bool bf16, hipStream_t stream);
 
 template <int I, int N, typename Fn>
 __device__ __forceinline__ void static_for(Fn&& f) {

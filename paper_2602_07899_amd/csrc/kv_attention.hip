@@ -529,10 +529,10 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kv_prompt_kernel(KvAttn
 #endif
 }
 
-// Number of splits that the tile of a row has written (see the kernels).
-__device__ __forceinline__ int written_splits(const KvAttnDev& a, const KvSeq& q, int qi, int head, uint32_t tile_rows) {
-  const uint32_t rows = (uint32_t)q.n_new * a.group;
-  uint32_t last_row = ((uint32_t)qi * a.group + (uint32_t)head % (uint32_t)a.group) / tile_rows * tile_rows + tile_rows - 1;
+// Number of splits that the tile of a row has written (see the kernels).  Tiles are counted from the first row, or from the last.
+__device__ __forceinline__ int written_splits(const KvAttnDev& a, const KvSeq& q, int qi, int head, uint32_t tile_rows, bool from_last) {
+  const uint32_t rows = (uint32_t)q.n_new * a.group, row = (uint32_t)qi * a.group + (uint32_t)head % (uint32_t)a.group;
+  uint32_t last_row = from_last ? rows - 1 - (rows - 1 - row) / tile_rows * tile_rows : row / tile_rows * tile_rows + tile_rows - 1;
   if (last_row > rows - 1) last_row = rows - 1;
   const int last = q.first + (int)a.by_group.of(last_row);
   const int end = last + 1 < q.len ? last + 1 : q.len;
@@ -542,14 +542,14 @@ __device__ __forceinline__ int written_splits(const KvAttnDev& a, const KvSeq& q
 // The splits of a row, up to 64 of them: sums joined with the largest of their references, a wave a row.  Bound by latency: 5
 // splits of 32 rows 3.8 us.
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void kv_join_few_kernel(KvAttnDev a, uint32_t tile_rows) {
+__global__ __launch_bounds__(256) void kv_join_few_kernel(KvAttnDev a, uint32_t tile_rows, bool from_last) {
 #if defined(__HIP_DEVICE_COMPILE__)
   typedef float vec __attribute__((ext_vector_type(DH / 64)));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int s = blockIdx.z, head = blockIdx.y * 4 + wave, qi = blockIdx.x;
   const KvSeq q = kv_sequence(a.b, a.c.page, a.n_tok, s);
   if (qi >= q.n_new || head >= a.n_heads) return;
-  const int n = written_splits(a, q, qi, head, tile_rows);
+  const int n = written_splits(a, q, qi, head, tile_rows, from_last);
   const int64_t at = ((q.row0 + qi) * a.n_heads + head) * a.n_splits;
   const float2 p = lane < n ? a.ml[at + lane] : make_float2(-INFINITY, 0.0f);
   float m = p.x;
@@ -579,7 +579,7 @@ __global__ __launch_bounds__(256) void kv_join_few_kernel(KvAttnDev a, uint32_t 
 // splits of 28 rows of 128 4.8 us (a wave a row, as above, 30 for 256 splits).
 [[maybe_unused]] constexpr int kMaxSplits = 1024;
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void kv_join_kernel(KvAttnDev a, uint32_t tile_rows) {
+__global__ __launch_bounds__(256) void kv_join_kernel(KvAttnDev a, uint32_t tile_rows, bool from_last) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int LPR = DH / 4, SIDE = 256 / LPR;
   __shared__ __attribute__((aligned(16))) float4 sum[SIDE][LPR];
@@ -588,7 +588,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnDev a, uint32_t tile
   const int s = blockIdx.z, head = blockIdx.y, qi = blockIdx.x;
   const KvSeq q = kv_sequence(a.b, a.c.page, a.n_tok, s);
   if (qi >= q.n_new) return;
-  const int n = written_splits(a, q, qi, head, tile_rows);
+  const int n = written_splits(a, q, qi, head, tile_rows, from_last);
   const int64_t at = ((q.row0 + qi) * a.n_heads + head) * a.n_splits;
   float2 p[kMaxSplits / 256];
   float m = -INFINITY, l = 0.0f;
@@ -717,15 +717,15 @@ KvAttnDev kv_attn_dev(const KvPlan& p, const void* Q, int64_t ldq, int64_t n_tok
 }
 
 // The joining of a launch's splits into Out.
-hipError_t launch_kv_join(const KvPlan& p, const KvAttnDev& a, bool bf16, hipStream_t stream) {
+hipError_t launch_kv_join(const KvPlan& p, const KvAttnDev& a, bool from_last, bool bf16, hipStream_t stream) {
   const int64_t most = a.b.max_new < a.n_tok ? a.b.max_new : a.n_tok;
   ProfScope ps("kv_join", stream, 4.0 * (double)a.n_tok * a.n_heads * p.n_splits * a.c.head_dim);
   auto pick = [&](auto t, auto dh) {
     using T = decltype(t);
     constexpr int DH = decltype(dh)::value;
     if (p.n_splits <= 64)
-      kv_join_few_kernel<T, DH><<<dim3((unsigned)most, (unsigned)ceil_div(a.n_heads, 4), (unsigned)a.b.n_seq), 256, 0, stream>>>(a, (uint32_t)p.rows);
-    else kv_join_kernel<T, DH><<<dim3((unsigned)most, (unsigned)a.n_heads, (unsigned)a.b.n_seq), 256, 0, stream>>>(a, (uint32_t)p.rows);
+      kv_join_few_kernel<T, DH><<<dim3((unsigned)most, (unsigned)ceil_div(a.n_heads, 4), (unsigned)a.b.n_seq), 256, 0, stream>>>(a, (uint32_t)p.rows, from_last);
+    else kv_join_kernel<T, DH><<<dim3((unsigned)most, (unsigned)a.n_heads, (unsigned)a.b.n_seq), 256, 0, stream>>>(a, (uint32_t)p.rows, from_last);
     return hipGetLastError();
   };
   using W128 = std::integral_constant<int, 128>;
@@ -748,7 +748,7 @@ hipError_t launch_kv_attention(const void* Q, int64_t ldq, int64_t n_tok, int n_
       else kv_few_kernel<T, DH><<<grid, 256, 0, stream>>>(a);
     }
     if (hipError_t e = hipGetLastError(); e != hipSuccess || p.n_splits == 1) return e;
-    return launch_kv_join(p, a, bf16, stream);
+    return launch_kv_join(p, a, false, bf16, stream);
   };
   using W128 = std::integral_constant<int, 128>;
   using W64 = std::integral_constant<int, 64>;
