@@ -40,7 +40,9 @@ __device__ __forceinline__ uint32_t keys_below(int p, int n) {
 // where they are widened: no barrier in the loop, the next 64 keys in flight while these are worked on.  Only their steps pass
 // through the wave's own piece of LDS: a lane needs 16 of each group of channels, which sixteen lanes share; loaded by each they take
 // ten more loads and 36 registers (which cost the third wave a SIMD), us that way and this: 64 x 2000 keys x 32 heads 115 99, 64 x 4096 -
-// 8192 x 8 110 105, 131,072 x 4 29.3 27.8; heads of 64 64 67.
+// 8192 x 8 110 105, 131,072 x 4 29.3 27.8; heads of 64 64 67.  Bound by the bytes of the cache where there are many, 64 x 4096 - 8192 x 8
+// 104 us, 4.4 TB/s (a copy reaches 4.8), by latency else, 1200 x 32 6.2 and 3.6 for joining five splits.  Not better: keys and values
+// both two turns ahead (109 -> 121), up to 767, 1023 or 2100 blocks in place of 511.
 template <typename T, int DH>
 __global__ __launch_bounds__(256, 3) void kv4_few_kernel(Kv4AttnDev a) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -570,13 +572,13 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kv4_prompt_kernel(Kv4At
 }
 
 size_t kv4_attention_workspace(int64_t n_tok, int n_heads, const tlq_kv_batch& b, const tlq_kv4_cache& c) {
-  return kv_plan(n_tok, n_heads, b, kv4_sizes(c)).bytes;
+  return kv_plan(n_tok, n_heads, b, kv4_sizes(c), true).bytes;
 }
 
 hipError_t launch_kv4_attention(const void* Q, int64_t ldq, int64_t n_tok, int n_heads, float scale, const tlq_kv_batch& b,
                                 const tlq_kv4_cache& c, bool bf16, void* Out, int64_t ldo, void* workspace, hipStream_t stream) {
   const tlq_kv_cache sizes = kv4_sizes(c);
-  const KvPlan p = kv_plan(n_tok, n_heads, b, sizes);
+  const KvPlan p = kv_plan(n_tok, n_heads, b, sizes, true);
   dim3 grid;
   Kv4AttnDev a;
   static_cast<KvAttnDev&>(a) = kv_attn_dev(p, Q, ldq, n_tok, n_heads, scale, b, sizes, Out, ldo, workspace, &grid);

@@ -34,7 +34,7 @@ struct KvAttnDev {
 
 // How a call is launched: prompts' tiles of 128 rows or few tiles of 16, splits of the keys, room in the workspace
 struct KvPlan { bool prompt; int rows, tiles, n_splits, chunk; size_t acc_at, bytes; };
-KvPlan kv_plan(int64_t n_tok, int n_heads, const tlq_kv_batch& b, const tlq_kv_cache& c);      // (sizes are read, no pointer)
+KvPlan kv_plan(int64_t n_tok, int n_heads, const tlq_kv_batch& b, const tlq_kv_cache& c, bool bits4);      // (sizes are read, no pointer)
 KvAttnDev kv_attn_dev(const KvPlan& p, const void* Q, int64_t ldq, int64_t n_tok, int n_heads, float scale, const tlq_kv_batch& b,
                       const tlq_kv_cache& c, void* Out, int64_t ldo, void* workspace, dim3* grid);
 hipError_t launch_kv_join(const KvPlan& p, const KvAttnDev& a, bool from_last, bool bf16, hipStream_t stream);

@@ -644,13 +644,21 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnDev a, uint32_t tile
 // 22 30, x 64 x 500 (2048) 22 20; whole prompts 300 x 8 pairs (304) 13.1 13.4, 600 x 4 (456) 14 21, 1000 x 1 (252) 11 30, 2400 x 1 (1500) 24
 // 30, 100 x 32 with four rows a token (800) 11.9 11.0.
 constexpr int64_t kFewWork = 1536;
+// Over a cache in 4 bits reading the keys again costs less: few and prompt there, 20 rows x 512 pairs x 8192 (32768) 178 235, 32 x 128 x
+// 16,000 (16128) 128 160, 48 x 256 x 4000 (12288) 64 109, x 512 x 2000 (12288) 69 73, x 512 x 600 (4608) 30 30, x 2048 x 48 (6144) 47 37;
+// 56 x 64 x 2000 (2048) 20 26, x 16 x 16,000 (4032) 37 39; 64 x 128 x 4000 (8192) 46 66, x 32 x 16,000 (8064) 70 60, x 512 x 1000 (8192) 52 45;
+// 128 x 64 x 1000 (2048) 20 25, x 16 x 5000 (2560) 31 28, x 32 x 4000 (4096) 35 31; 200 x 32 x 1000 (1664) 17 25, x 32 x 2000 (3328) 28 31;
+// whole prompts 300 x 64 (2432) 20 18, 400 x 64 (3200) 24 21, 1000 x 8 (2016) 18 26, x 16 (4032) 28 35.  Heads of 64: 48 x 512 x 2000
+// (12288) 43 50, 96 x 64 x 4000 (6144) 32 31.
+constexpr int64_t kFewWork4 = 3328, kFewRows4 = 48;
 
-KvPlan kv_plan(int64_t n_tok, int n_heads, const tlq_kv_batch& b, const tlq_kv_cache& c) {
+KvPlan kv_plan(int64_t n_tok, int n_heads, const tlq_kv_batch& b, const tlq_kv_cache& c, bool bits4) {
   KvPlan p;
   const int group = n_heads / c.n_kv_heads;
   const int64_t most = b.max_new < n_tok ? b.max_new : n_tok;
   const int64_t room = (int64_t)b.max_pages * c.page, keys = b.max_len < room ? b.max_len : room;
-  p.prompt = most * group > 16 && ceil_div(most * group, 16) * c.n_kv_heads * b.n_seq * ceil_div(keys, 256) > kFewWork;
+  p.prompt = most * group > (bits4 && keys > 256 ? kFewRows4 : 16) &&
+             ceil_div(most * group, 16) * c.n_kv_heads * b.n_seq * ceil_div(keys, 256) > (bits4 ? kFewWork4 : kFewWork);
   p.rows = p.prompt ? 128 : 16;
   p.tiles = (int)ceil_div(most * group, p.rows);
   const int64_t base = (int64_t)p.tiles * c.n_kv_heads * b.n_seq;
@@ -684,7 +692,7 @@ KvPlan kv_plan(int64_t n_tok, int n_heads, const tlq_kv_batch& b, const tlq_kv_c
 }
 
 size_t kv_attention_workspace(int64_t n_tok, int n_heads, const tlq_kv_batch& b, const tlq_kv_cache& c) {
-  return kv_plan(n_tok, n_heads, b, c).bytes;
+  return kv_plan(n_tok, n_heads, b, c, false).bytes;
 }
 
 // What a launch's kernels read besides the cache's codes (c: its sizes are), and its grid.
@@ -736,7 +744,7 @@ hipError_t launch_kv_join(const KvPlan& p, const KvAttnDev& a, bool from_last, b
 
 hipError_t launch_kv_attention(const void* Q, int64_t ldq, int64_t n_tok, int n_heads, float scale, const tlq_kv_batch& b,
                                const tlq_kv_cache& c, bool bf16, void* Out, int64_t ldo, void* workspace, hipStream_t stream) {
-  const KvPlan p = kv_plan(n_tok, n_heads, b, c);
+  const KvPlan p = kv_plan(n_tok, n_heads, b, c, false);
   dim3 grid;
   const KvAttnDev a = kv_attn_dev(p, Q, ldq, n_tok, n_heads, scale, b, c, Out, ldo, workspace, &grid);
   auto pick = [&](auto t, auto dh) {

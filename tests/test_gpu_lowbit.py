@@ -549,14 +549,14 @@ def _attend(gpu, c, heads, dt, q, scale=0.0):
 
 def _bounds(c, heads, q, kind):
     """Host's bounds under which the tiles of 128 rows are taken (they need work for many blocks): rows behind the last sequence
-    ("tiles"), or, for more than 16 rows, longer sequences than there are ("parts": many parts, most of them empty)."""
+    ("tiles"), or, for more than 48 rows, longer sequences than there are ("parts": many parts, most of them empty)."""
     group, pairs = heads // c.kv, len(c.lens) * c.kv
     if kind == "tiles":
-        q = np.concatenate([q, np.full((1540 * 16 // (group * pairs) + 16, q.shape[1]), np.nan)])
+        q = np.concatenate([q, np.full((3340 * 16 // (group * pairs) + 16, q.shape[1]), np.nan)])
         c.max_new = q.shape[0]
         c.max_len = max(c.max_len, c.max_new)
     if kind == "parts":
-        units = 1540 // (max(-(-c.max_new * group // 16), 1) * pairs) + 1
+        units = 3340 // (max(-(-c.max_new * group // 16), 1) * pairs) + 1
         c.max_len = max(c.max_len, units * 256)
         c.table = np.concatenate([c.table, np.full((len(c.lens), max(0, -(-c.max_len // c.page) - c.table.shape[1])), -1, np.int32)], 1)
     return q
