@@ -1058,8 +1058,7 @@ tlq_status tlq_linear_codes(const int8_t* codes, int64_t ldx, const float* steps
   TLQ_TRY(check_ws(workspace, workspace_bytes, tlq_linear_codes_workspace_bytes(n_tok, c_in)));
   hipStream_t st = (hipStream_t)stream;
   const int64_t k = int8_row(c_in);
-  const bool tanh_form = act == TLQ_ACT_GELU_TANH;
-  const Finish fin{bias, R, ldr, act, mul, tanh_form ? -2.30220820f : -1.44269504f, tanh_form ? -0.102943240f : 0.0f};      // (finish.h)
+  const Finish fin{bias, R, ldr, act, mul};
   const bool finish = bias || R || act != TLQ_ACT_NONE;
   const LinearI8Args l{codes, n_tok, ldx, steps, w_codes, c_out, ldw, k, w_steps, Y, ldy, p->yref_dtype, finish, fin};
   const LinearKind kind = linear_codes_kind(n_tok, c_out, k);

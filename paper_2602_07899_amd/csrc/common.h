@@ -196,10 +196,9 @@ struct FinalDev {
 // (128 x 128 with tok_partial: tok_blocks has to say 4).
 // gemm_tile says which is the fastest.
 struct GemmTile { bool small; int tok_blocks; };
+// What follows a product's scaling (finish.h): y = act(y + bias[o]), then + or * R[t, o] of the output's type.
+struct Finish { const float* bias; const void* R; int64_t ldr; int act, mul; };
 // S3+S4 / plain GEMM with store epilogue.
-// What follows a product's scaling (finish.h): y = act(y + bias[o]), then + or * R[t, o] of the output's type.  k1, k3: of the
-// logistic activations' exponent
-struct Finish { const float* bias; const void* R; int64_t ldr; int act, mul; float k1, k3; };
 struct GemmArgs : GemmTile {
   GemmTile& tile() { return *this; }
   const void* X; int64_t n_tok, c_in, ldx;     // tokens  [n_tok, c_in]

@@ -125,7 +125,7 @@ template <int IA, int JB> struct Acc16 {   // acc[IA][JB] of f32x4 (16x16x32)
 
 // EPI_DOT: partial = sum over the tile of acc * Y (Y read like Y_ref, one matrix per candidate, no
 // token weights): the quadratic form of the second-moment search.
-// EPI_FINISH + an activation's class (finish.h): a store with GemmDev::fin behind the scaling.
+// EPI_FINISH + an activation (finish.h): a store with GemmDev::fin behind the scaling.
 enum { EPI_LOSS = 0, EPI_LOSS_TOK = 1, EPI_STORE = 2, EPI_DOT = 3, EPI_FINISH = 4 };
 constexpr int BK = 64;        // halves per k-tile
 constexpr int ROWB = BK * 2;  // bytes per LDS row
@@ -1043,7 +1043,7 @@ __device__ __forceinline__ void gemm_dma_body(const GemmDev& a) {
           const i32x4 v = __builtin_bit_cast(i32x4, acc[i][j]);
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            acc[i][j][e] = act_of<EPI - EPI_FINISH>(__builtin_fmaf(sg[j], r[at][e] * (float)v[e], bias[at][e]), a.fin);
+            acc[i][j][e] = act_of<EPI - EPI_FINISH>(__builtin_fmaf(sg[j], r[at][e] * (float)v[e], bias[at][e]));
           if ((j & 1) || j == JB - 1) __builtin_amdgcn_sched_barrier(0);      // (eight at a time)
         }
         if constexpr (i + AHEAD < IA) fetch(std::integral_constant<int, i + AHEAD>{});

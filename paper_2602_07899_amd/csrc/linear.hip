@@ -30,7 +30,7 @@ __device__ __forceinline__ void finish4(const LinearI8Args& a, int64_t t, int64_
 #pragma unroll
   for (int e = 0; e < 4; ++e) y[e] = __builtin_fmaf(f.st, f.ws[e] * (float)s[e], f.bias[e]);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) y[e] = act_of(y[e], a.fin);
+  for (int e = 0; e < 4; ++e) y[e] = act_of(y[e], a.fin.act);
   if (a.fin.R) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) y[e] = a.fin.mul ? y[e] * f.second[e] : y[e] + f.second[e];
