@@ -55,7 +55,8 @@ __device__ __forceinline__ float half_head(float v, bool upper) {
 // - 351 under the profiler, 4.8 - 5.0 TB/s where a copy of as many bytes reaches 3.9 - 5.1; by latency for few tokens: 16 x 40
 // heads 5.0 us.
 enum { kHalfHead, kHalfRot, kNeighbours };
-// AXES: a token has up to four positions and a frequency turns by that of its axis.
+// AXES: a token has up to four positions and a frequency turns by that of its axis.  The positions are one load more before the
+// angles, beside which the frequencies' axes come: 16 x 40 heads 5.4 us, with one axis 5.1; 40,800 x 80 heads 343 and 345.
 template <typename T, int DH, int FORM, bool AXES>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkRopeArgs a, int wpt, bool nts) {
 #if defined(__HIP_DEVICE_COMPILE__)
