@@ -246,7 +246,7 @@ __global__ __launch_bounds__(256, 3) void kv4_few_kernel(Kv4AttnDev a) {
 // full is the one with the fewest keys: 16 x 1200 tokens x 40 heads 366 -> 354 us, 1000 behind 1000 others x 32 433 -> 414, 4 x 2400
 // 254 -> 251, 16 x 200 40 -> 42.
 //   Bound by the waits of two waves a SIMD for each other, for LDS and at the barrier.  9600 tokens x 40 heads 1038 us, 910
-// TFLOP/s where a large library product of halves reaches 1180; 16 x 1200 x 40 353, 670 TFLOP/s, since a block has 10 steps on average
+// TFLOP/s where a large library product of halves reaches 1180; 16 x up to 1200 x 40 346, 620 TFLOP/s, since a block has 10 steps on average
 // there, the diagonal's half of them idle for half of its waves, and begins and ends with a chain of loads and stores.  Of a wave's time
 // 29 % issues vector instructions, of the SIMDs' 26 % is matrix products.  Left out for measurement: widening 42 us, exponentials 32.
 // Not better, us for 16 x 1200 x 40: a step in four phases that interleave two of them 469 against 371, values staged in the
