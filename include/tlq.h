@@ -500,7 +500,8 @@ tlq_status tlq_kv4_read(const tlq_kv_batch* b, const tlq_kv4_cache* c, const tlq
                         void* V_out, int64_t ldv, void* stream);
 /* tlq_kv4_attention: tlq_kv_attention over a cache in 4 bits: the same rows, masks, limits and workspace rules.  Keys and values
  * enter the matrix products exactly, queries as there, and softmax weights rounded to halves, which the softmax's sum takes as well; scores,
- * softmax and sums are float.  Steps have to be finite in tokens that a row sees; others may hold anything. */
+ * softmax and sums are float.  Scores may have any size here: beyond 2^24 they are rounded to floats before the exponential, and where
+ * floats end the largest takes all of the weight.  Steps have to be finite in tokens that a row sees; others may hold anything. */
 size_t tlq_kv4_attention_workspace_bytes(int64_t n_tok, int32_t n_heads, const tlq_kv_batch* b, const tlq_kv4_cache* c);
 tlq_status tlq_kv4_attention(const void* Q, int64_t ldq, int64_t n_tok, int32_t n_heads, float scale, const tlq_kv_batch* b,
                              const tlq_kv4_cache* c, const tlq_params* p, void* Out, int64_t ldo, void* workspace,

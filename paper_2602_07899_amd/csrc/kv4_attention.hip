@@ -5,7 +5,10 @@
 // cache stands for.  With z_j = scale * log2(e) * (q . key_j) and any reference m,  out = sum_j 2^(z_j - m) value_j / sum_j 2^(z_j - m).
 // m, the row's reference, is 7 below the largest z when it is set, and is set again where a lane's 8 or 16 weights come to 2^15, so that
 // weights stay below that and, as normal halves, go down to 2^-29 of it, and sums are rescaled a few times a row; no maximum is
-// looked for as long as the sum, which is needed anyhow, stays below (at first m is so low that every weight overflows).  The
+// looked for as long as the sum, which is needed anyhow, stays below (a row without a reference has one so low that every weight
+// overflows; prompts set the first from their first 64 scores).  2^(z - m) is one fused product and an exponential, exact where m is
+// not, so that m's rounding cancels as long as it is small.  From |m| = 2^24 on it is not, neighbouring floats being whole binary
+// orders apart: such a row's scores are rounded to floats first (kFar), and the largest has the weight that m gives it.  The
 // weights are rounded to halves for the second product, and the denominator sums what was rounded, in 32 bits: where one key has
 // nearly all of the weight its rounding cancels.  bf16 queries are multiplied with the power of two that brings the largest of the row to
 // [2^14, 2^15).  The products are transposed, S^T = K Q^T and O^T = V^T P^T, so that a lane owns one query column and P stays in
@@ -20,8 +23,19 @@ struct Kv4AttnDev : KvAttnDev { Kv4Dev d; };      // (of c the sizes)
 #if defined(__HIP_DEVICE_COMPILE__)
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 constexpr float kFull = 32768.0f;      // weights of a lane that call for another reference (the largest is 2^11 at least then)
-constexpr float kUnset = -1e30f;
-__device__ __forceinline__ float ref_of(float ref) { return ref < 0.5f * kUnset ? -INFINITY : ref; }      // for those who join
+constexpr float kUnset = -3.40282347e38f;      // (no score is as low, see score_factor)
+__device__ __forceinline__ float ref_of(float ref) { return ref == kUnset ? -INFINITY : ref; }      // for those who join
+constexpr float kFar = 16777216.0f;
+// What a row's products are multiplied with.  Not zero: zero times a masked product would not be -inf.  A product of queries (2^16)
+// and keys (2^16) is below 2^39, so that with 2^88 at most every score is a float.  That changes no result: two products that differ at
+// all lie 2^-48 apart at least, times 2^88 all of the weight either way.
+__device__ __forceinline__ float score_factor(float f) { return __builtin_amdgcn_fmed3f(f, 1e-37f, 0x1p88f); }
+// The reference that a row's largest product gives; from kFar on that of the score as a float (fused, it could come out a float below)
+__device__ __forceinline__ float reference(float product, float fac) {
+#pragma clang fp contract(off)
+  const float ref = __builtin_fmaf(product, fac, -kTop), score = product * fac;
+  return fabsf(ref) >= kFar ? score - kTop : ref;
+}
 // keeps what a wave's lanes write for each other in LDS in order
 __device__ __forceinline__ void wave_order() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -52,6 +66,7 @@ __global__ __launch_bounds__(256, 3) void kv4_few_kernel(Kv4AttnDev a) {
   __shared__ __attribute__((aligned(16))) float part[4][16][RS];
   __shared__ __attribute__((aligned(16))) uint16_t steps[4][2][64 * NG];      // of a wave's 64 keys: [key][group], [16 keys][group][key]
   __shared__ float2 ml[4][16];
+  __shared__ float far_fac[4][16];      // 1, or of rows from kFar on the factor that their scores have before the exponent's product
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, fq = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int s = blockIdx.z, hk = blockIdx.y;
@@ -71,7 +86,9 @@ __global__ __launch_bounds__(256, 3) void kv4_few_kernel(Kv4AttnDev a) {
   f16x8 qf[NS];
   float fac = fabsf(a.scale2) * load_queries<T, NS, 8>(
       a.Q + (q.row0 + qi) * a.ldq + ((int64_t)hk * a.group + g) * DH + fq * (DH / 4), qf, a.scale2 < 0.0f);
-  fac = fmaxf(fac, 1e-37f);                 // (zero times a masked product would not be -inf)
+  fac = score_factor(fac);
+  far_fac[wave][l16] = 1.0f;
+  bool far = false;                         // whether a row of the wave has such scores
 
   f32x4 acc[ND];
 #pragma unroll
@@ -145,6 +162,11 @@ __global__ __launch_bounds__(256, 3) void kv4_few_kernel(Kv4AttnDev a) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) sc[e >> 2][e & 3] = e <= limit ? sc[e >> 2][e & 3] : -INFINITY;
     }
+    if (__builtin_expect(far, 0)) {
+      const float f = far_fac[wave][l16];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sc[j] *= f;
+    }
     f16x8 pf[2];
     auto weigh = [&]() __attribute__((always_inline)) {
 #pragma unroll
@@ -156,13 +178,24 @@ __global__ __launch_bounds__(256, 3) void kv4_few_kernel(Kv4AttnDev a) {
       float mx = sc[0][0];
 #pragma unroll
       for (int e = 1; e < 16; ++e) mx = fmaxf(mx, sc[e >> 2][e & 3]);
-      mx = column_max(mx) * fac;
+      mx = column_max(mx);
+      bool far_now = false;
       if (column_max(sum) >= kFull) {      // (the row's own sums: what the others hold has no part in it)
-        const float next = mx - kTop, alpha = exp2_of(ref - next);       // (0 at the first visible key)
+        const float next = reference(mx, fac), alpha = exp2_of(ref - next);       // (0 at the first visible key)
         l_run *= alpha;
         ref = next;
 #pragma unroll
         for (int d = 0; d < ND; ++d) acc[d] *= alpha;
+        far_now = fabsf(next) >= kFar;
+      }
+      if (__any(far_now)) {
+        const float f = far_now ? fac : 1.0f;      // (one in a row that has been far before)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sc[j] *= f;
+        far_fac[wave][l16] *= f;
+        wave_order();
+        fac = far_now ? 1.0f : fac;
+        far = true;
       }
       sum = weigh();
     }
@@ -258,6 +291,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kv4_prompt_kernel(Kv4At
   constexpr int KB = DH * 2, VB = 128;                      // bytes of a row of K, of V^T in LDS
   constexpr int STAGE = 64 * KB + DH * VB, LR = DH / 64;    // LR: 8-byte loads of a thread for K, and for V
   __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * STAGE];
+  __shared__ float far_fac[4][2][16];                       // as in kv4_few_kernel
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, fq = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // block 8 j + x runs on XCD x.  It has pair x of each eight: 2^together_bits such pairs at a time, then those that are left of
@@ -412,8 +446,10 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kv4_prompt_kernel(Kv4At
     pos[n] = q.first + qi;
     const uint16_t* p = a.Q + (q.row0 + qi) * a.ldq + ((int64_t)hk * a.group + g) * DH + fq * 8;
     fac[n] = fabsf(a.scale2) * load_queries<T, NS, 32>(p, qf[n], a.scale2 < 0.0f);
-    fac[n] = fmaxf(fac[n], 1e-37f);       // (zero times a masked product would not be -inf)
+    fac[n] = score_factor(fac[n]);
+    far_fac[wave][n][l16] = 1.0f;
   }
+  bool far = false;                         // whether a row of the wave has scores from kFar on
   if (k0 < k1) {
     stage_all(lds);
     stage_tail(lds, k0);
@@ -470,6 +506,14 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kv4_prompt_kernel(Kv4At
         for (int e = 0; e < 16; ++e) sc[e >> 2][n][e & 3] = e <= limit ? sc[e >> 2][n][e & 3] : -INFINITY;
       }
     }
+    if (__builtin_expect(far, 0)) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const float f = far_fac[wave][n][l16];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sc[j][n] *= f;
+      }
+    }
     // half of the keys after the other: the weights of the second half are formed between the products of the first
     f16x8 pf[2][2], vf[4];
     auto read_v = [&](int at) __attribute__((always_inline)) {
@@ -487,19 +531,33 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kv4_prompt_kernel(Kv4At
       constexpr int u = decltype(uc)::value;
       float sum[2] = {add_weights(pf[u][0], 0.0f), add_weights(pf[u][1], 0.0f)};
       if (__any(!(sum[0] < kFull && sum[1] < kFull))) {
+        bool far_now[2] = {false, false};
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
           float mx = sc[2 * u][n][0];
 #pragma unroll
           for (int e = 1; e < 8; ++e) mx = fmaxf(mx, sc[2 * u + (e >> 2)][n][e & 3]);
-          mx = column_max(mx) * fac[n];
+          mx = column_max(mx);
           if (column_max(sum[n]) >= kFull) {      // (the row's own sums: what the others hold has no part in it)
-            const float next_ref = mx - kTop, alpha = exp2_of(ref[n] - next_ref);
+            const float next_ref = reference(mx, fac[n]), alpha = exp2_of(ref[n] - next_ref);
             l_run[n] *= alpha;
             ref[n] = next_ref;
 #pragma unroll
             for (int d = 0; d < ND; ++d) acc[d][n] *= alpha;
+            far_now[n] = fabsf(next_ref) >= kFar;
           }
+        }
+        if (__any(far_now[0] || far_now[1])) {
+#pragma unroll
+          for (int n = 0; n < 2; ++n) {
+            const float f = far_now[n] ? fac[n] : 1.0f;      // (one in a row that has been far before)
+#pragma unroll
+            for (int j = 2 * u; j < 4; ++j) sc[j][n] *= f;
+            far_fac[wave][n][l16] *= f;
+            fac[n] = far_now[n] ? 1.0f : fac[n];
+          }
+          wave_order();
+          far = true;
         }
         static_for<0, 8>([&](auto ec) { weigh(uc, ec); });
         sum[0] = add_weights(pf[u][0], 0.0f);
@@ -512,14 +570,14 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kv4_prompt_kernel(Kv4At
     using Second = std::integral_constant<int, 1>;
 #pragma unroll
     for (int at = 0; at < 4; ++at) read_v(at);
-    if (unit == k0) {      // the first reference, if there is a key (356 -> 353 us; the weights need no second go for it)
+    if (unit == k0) {      // the first reference, if there is a key that is not far (356 -> 353 us; the weights need no second go for it)
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
         float mx = sc[0][n][0];
 #pragma unroll
         for (int e = 1; e < 16; ++e) mx = fmaxf(mx, sc[e >> 2][n][e & 3]);
         mx = column_max(mx) * fac[n];
-        ref[n] = mx > kUnset ? mx - kTop : kUnset;
+        ref[n] = fabsf(mx) < kFar ? mx - kTop : kUnset;
       }
     }
     static_for<0, 8>([&](auto ec) { weigh(First{}, ec); });
@@ -541,14 +599,16 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kv4_prompt_kernel(Kv4At
       __builtin_amdgcn_sched_barrier(0);
     });
   }
+  int column = l16;      // (rows are worked out again, not held in registers through the loop)
+  asm volatile("" : "+v"(column));
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
     float l = l_run[n];
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
     ref[n] = ref_of(ref[n]);
-    if (wrow + n * 16 + l16 < 0) continue;
-    const uint32_t r = (uint32_t)(wrow + n * 16 + l16);
+    if (wrow + n * 16 + column < 0) continue;
+    const uint32_t r = (uint32_t)(wrow + n * 16 + column);
     const uint32_t qi = a.by_group.of(r);
     const int64_t token = q.row0 + qi, head = (int64_t)hk * a.group + (r - qi * a.group);
     if (a.n_splits > 1) {

@@ -820,6 +820,60 @@ def test_kv4_attention_of_queries_near_the_types_largest(gpu):
     _check_attention(gpu, c, 2, "bf16", rnd(big.astype(np.float64) * 2.0 ** -255, "bf16"))
 
 
+def _winners(c, heads, q, scale):
+    """(out, ok): the mean of the values of each row's largest score, ties among equal keys; ok where every other score lies further
+    below it than floats can take (products of dh terms in 32 bits, and 64 binary orders)."""
+    k, v = c.values()
+    out, ok = np.zeros((c.rows, heads * c.dh)), np.zeros((c.rows, heads), bool)
+    scale = scale or c.dh ** -0.5
+    for s, n in enumerate(c.lens):
+        ids = c.table[s, :-(-n // c.page)]
+        for h in range(heads):
+            keys = k[ids, h * c.kv // heads].reshape(-1, c.dh)[:n]
+            vals = v[ids, h * c.kv // heads].transpose(0, 2, 1).reshape(-1, c.dh)[:n]
+            for r in range(c.cu[s], c.cu[s + 1]):
+                m = n - (c.cu[s + 1] - r) + 1
+                terms = scale * keys[:m] * q[r, h * c.dh:(h + 1) * c.dh].astype(np.float64)
+                z, sens = terms.sum(1), np.abs(terms).sum(1).max()
+                top = z == z.max()
+                out[r, h * c.dh:(h + 1) * c.dh] = vals[:m][top].mean(0)
+                ok[r, h] = top.all() or z.max() - z[~top].max() > 64 + 4 * (c.dh + 8) * U * sens
+    return out, np.repeat(ok, c.dh, 1)
+
+
+@pytest.mark.parametrize("kind", ["", "tiles", "parts"])
+@pytest.mark.parametrize("dt,size,scale,dh", [
+    ("f16", 6e4, 0.0, 128), ("f16", 6e4, -3e4, 128), ("bf16", 2.0 ** 28, 0.0, 128), ("bf16", 2.0 ** 60, 0.0, 128), ("bf16", 2.0 ** 101, 0.0, 128),
+    ("bf16", 2.0 ** 126, 0.0, 128), ("bf16", 2.0 ** 126, -2.0 ** 60, 128), ("f16", 6e4, 0.0, 64), ("bf16", 2.0 ** 101, 0.0, 64)])
+def test_kv4_attention_of_scores_of_any_size(gpu, kind, dt, size, scale, dh):
+    """Scores (2^28 to 2^192) whose neighbours as floats lie many binary orders on, or that no float is, of both signs or all below
+    zero: the largest takes all of the weight, keys that are equal share it.  Rows with ordinary scores beside them keep their bits."""
+    g = np.random.default_rng(101)
+    c = Pool(g, gpu, [700, 300, 3], [5, 40, 3], 2, dh, 16, dt)
+    for s, n in enumerate(c.lens):                             # the second half of a sequence has the keys of the first again
+        for t in range(n // 2):
+            a, b = (c.table[s, t // 16], slice(None), t % 16), (c.table[s, (t + n // 2) // 16], slice(None), (t + n // 2) % 16)
+            c.kc[b], c.ks[b] = c.kc[a], c.ks[a]
+    c.kc[:, 0] = -np.abs(c.kc[:, 0])
+    if dt == "f16":
+        c.ks[:] = np.minimum(c.ks.astype(np.float32) * 2.0 ** 14, 8160.0).astype(np.float16)      # (eight times 8192 is no half)
+    q = g.standard_normal((c.rows, 4 * dh))
+    q[::4, :2 * dh] = np.abs(q[::4, :2 * dh]) + 0.1                  # (with the keys of head 0: no score above zero)
+    plain = rnd(q * (1e-4 if dt == "f16" else 1.0), dt)
+    loud = rnd(q / np.abs(q).max(axis=1, keepdims=True) * size, dt)
+    loud[1::2] = plain[1::2]
+    far = np.arange(c.rows) % 2 == 0
+    want, ok = _winners(c, 4, loud, scale)
+    assert ok[far].mean() > 0.9
+    got = _attend(gpu, c, 4, dt, _bounds(c, 4, loud, kind), scale)[:c.rows]
+    assert np.isfinite(got[far]).all()
+    # (of one weight, or a few that are equal: sums and quotient in 32 bits, the output)
+    within(got[ok & far[:, None]], want[ok & far[:, None]], (np.abs(want) * (HALF[dt] * 1.001 + 8 * U) + TINY[dt] * 1.01)[ok & far[:, None]])
+    if scale == 0.0:
+        quiet = _attend(gpu, c, 4, dt, _bounds(c, 4, plain, kind), scale)[:c.rows]
+        assert np.isfinite(quiet).all() and np.array_equal(got[~far], quiet[~far])
+
+
 @pytest.mark.parametrize("dt", ["f16", "bf16"])
 @pytest.mark.parametrize("new,kind", [(1, ""), (20, ""), (20, "tiles"), (20, "parts"), (150, ""), (150, "tiles"), (150, "parts")])
 def test_kv4_attention_of_queries_that_are_not_finite(gpu, dt, new, kind):
