@@ -280,7 +280,8 @@ __global__ __launch_bounds__(256, 3) void kv4_few_kernel(Kv4AttnDev a) {
 // 254 -> 251, 16 x 200 40 -> 42.
 //   Bound by the waits of two waves a SIMD for each other, for LDS and at the barrier.  9600 tokens x 40 heads 1038 us, 910
 // TFLOP/s where a large library product of halves reaches 1180; 16 x up to 1200 x 40 346, 620 TFLOP/s, since a block has 10 steps on average
-// there, the diagonal's half of them idle for half of its waves, and begins and ends with a chain of loads and stores.  Of a wave's time
+// there, the diagonal's half of them idle for half of its waves, and begins and ends with a chain of loads and stores.  Rows of far scores cost the
+// others 0.5 % (346 -> 348, with heads of 64 1.5 %).  Of a wave's time
 // 29 % issues vector instructions, of the SIMDs' 26 % is matrix products.  Left out for measurement: widening 42 us, exponentials 32.
 // Not better, us for 16 x 1200 x 40: a step in four phases that interleave two of them 469 against 371, values staged in the
 // second product 5 % slower, 16 rows a wave and four waves a SIMD 493 against 359 (LDS is read twice as often).
@@ -644,7 +645,7 @@ hipError_t launch_kv4_attention(const void* Q, int64_t ldq, int64_t n_tok, int n
   static_cast<KvAttnDev&>(a) = kv_attn_dev(p, Q, ldq, n_tok, n_heads, scale, b, sizes, Out, ldo, workspace, &grid);
   a.d = {c.k, c.k_step, c.v, c.v_step};
   {
-    ProfScope ps("kv4_attention", stream, 4.0 * (double)n_tok * n_heads * c.head_dim * (double)b.max_len);
+    ProfScope ps(p.prompt ? "kv4_prompt" : "kv4_few", stream, 4.0 * (double)n_tok * n_heads * c.head_dim * (double)b.max_len);
     auto pick = [&](auto t, auto dh) {
       using T = decltype(t);
       constexpr int DH = decltype(dh)::value;

@@ -609,6 +609,20 @@ def test_kv4_attention(gpu, dt, kind, lens, new, kv, group, dh, page):
 
 
 @pytest.mark.parametrize("kind", ["", "tiles", "parts"])
+@pytest.mark.parametrize("lens,new,kv,group,dh,page", ATTENTION)
+def test_kv4_attention_runs_the_kernel_that_its_bounds_are_for(gpu, kind, lens, new, kv, group, dh, page):
+    """Tiles of 16 rows by the batches' own bounds; by those of `_bounds` tiles of 128, for more than 48 rows where only the length grows."""
+    g = np.random.default_rng(102)
+    c = Pool(g, gpu, lens, new, kv, dh, page, "f16")
+    q = _bounds(c, kv * group, np.zeros((c.rows, kv * group * dh), np.float32), kind)
+    want = "kv4_prompt" if kind == "tiles" or (kind == "parts" and max(new) * group > 48) else "kv4_few"
+    b, cache = c.load()
+    Q = dev(np.nan_to_num(q), gpu, "f16")
+    names = _kernels(lambda: tlq.kv4_attention(Q, kv * group, b, cache, tlq.params(), Q.clone()))
+    assert want in names and names <= {want, "kv_join"}
+
+
+@pytest.mark.parametrize("kind", ["", "tiles", "parts"])
 @pytest.mark.parametrize("dt", ["f16", "bf16"])
 def test_kv4_attention_of_wild_steps_and_loud_queries(gpu, dt, kind):
     """Steps from the smallest to the largest, subnormal halves among them; queries of very different size, zeros among them; scores
