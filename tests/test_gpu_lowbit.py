@@ -130,6 +130,22 @@ def test_add_norm_codes_are_those_of_the_calls_apart(gpu):
     assert torch.equal(a, b) and torch.equal(sa, sb)
 
 
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("n,c", [(5, 136), (3, 1096), (3, 5120), (2, 13824), (2, 20008), (2, 40008)])
+def test_add_norm_codes_onto_the_second_matrix(gpu, dt, n, c):
+    """H_out may be Z; H and Z may be the same."""
+    import torch
+    g = np.random.default_rng([103, n, c])
+    h, z = (rnd(g.standard_normal((n, c)), dt) for _ in range(2))
+    H, Z = dev(h, gpu, dt), dev(z, gpu, dt)
+    codes, steps = torch.empty((n, -(-c // 128) * 128), dtype=torch.int8, device=gpu), torch.empty(n, device=gpu)
+    p = tlq.params(x_dtype=CODE[dt])
+    for a, b, second in ((H, Z, z), (H, H, h)):
+        tlq.add_norm_codes(a, None, p, codes, steps, Z=b, H_out=b, eps=1e-5)
+        want = lo.add_norm_codes(h, second, None, 1e-5, 8, dt == "bf16")
+        assert np.array_equal(host(b), want[0]) and np.array_equal(codes.cpu().numpy()[:, :c], want[1]) and np.array_equal(steps.cpu().numpy(), want[2])
+
+
 @pytest.mark.parametrize("dt,c", [("f16", 264), ("bf16", 5120)])
 def test_add_norm_codes_of_rows_that_are_not_finite(gpu, dt, c):
     """Such a row has a NaN step, and its products are NaN; the others do not see it.  Zeros without eps likewise."""
