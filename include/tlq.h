@@ -430,7 +430,8 @@ tlq_status tlq_kv_attention(const void* Q, int64_t ldq, int64_t n_tok, int32_t n
  * tlq_add_norm_codes: the residual's addition, a root-mean-square norm and the codes of the normalised rows in one pass:
  *   h = round16(H + Z) (Z NULL: h = H);  r = float(1 / sqrt(mean_c h^2 + eps)) with the mean and the root in double;
  *   u = (h * r) * w[c];  step = max(max_c |u|, 1e-5) / (2^(bits-1) - 1);  code = clip(rint(u / step), -2^(bits-1), 2^(bits-1) - 1)
- * (float arithmetic, one rounding an operation, half to even; the double sum makes r the same in any order of its terms).  The
+ * (float arithmetic, one rounding an operation, half to even; the double sum is off by 2^-46 at most, so that r is this float but in a row
+ * of some millions, whose r may be its neighbour).  The
  * norm's weight and the searched scales' reciprocals are one factor w: float [c], 16-byte aligned, or NULL (ones).
  * H, Z, H_out [n, c] x_dtype, 16-byte aligned, strides multiples of 8; H_out may be NULL (not wanted), or H or Z with the same
  * stride; no other overlap.  c a multiple of 8, at most 65536; bits 2..8; eps >= 0 (with 0 a row of zeros gives NaN).  codes, ldc and steps as

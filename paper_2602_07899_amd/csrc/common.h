@@ -237,7 +237,7 @@ int64_t gemm_blocks(const GemmArgs& g);   // workgroups of the launch (sizes, ti
 int64_t tile_map_defects(int64_t n_tok, int64_t c_in, int64_t c_out, int n_cand);
 hipError_t launch_gemm_loss(const GemmArgs& a, hipStream_t stream);
 hipError_t launch_gemm_store(const GemmArgs& a, hipStream_t stream);
-// the store of one product of integer codes with g.fin behind it (any tile but 128 x 64)
+// the store of one product of integer codes with g.fin behind it (any tile; the one way to tiles of 128 x 64)
 hipError_t launch_gemm_finish(const GemmArgs& a, hipStream_t stream);
 // partial[k, tile] = sum over the tile of (X_k Wh^T)[t,o] * Y_k[t,o]  (no token weights), fp16, for a symmetric
 // Wh (sym_k): about half the flops, same partial sums

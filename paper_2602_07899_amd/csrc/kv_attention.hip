@@ -649,7 +649,9 @@ constexpr int64_t kFewWork = 1536;
 // 56 x 64 x 2000 (2048) 20 26, x 16 x 16,000 (4032) 37 39; 64 x 128 x 4000 (8192) 46 66, x 32 x 16,000 (8064) 70 60, x 512 x 1000 (8192) 52 45;
 // 128 x 64 x 1000 (2048) 20 25, x 16 x 5000 (2560) 31 28, x 32 x 4000 (4096) 35 31; 200 x 32 x 1000 (1664) 17 25, x 32 x 2000 (3328) 28 31;
 // whole prompts 300 x 64 (2432) 20 18, 400 x 64 (3200) 24 21, 1000 x 8 (2016) 18 26, x 16 (4032) 28 35.  Heads of 64: 48 x 512 x 2000
-// (12288) 43 50, 96 x 64 x 4000 (6144) 32 31.
+// (12288) 43 50, 96 x 64 x 4000 (6144) 32 31.  Two limits on a count of tiles of 16 rows are coarse (64 rows are half of a tile of 128,
+// and half of a prompt's tiles have few keys): they keep the slower kernel at 64 x 128 x 4000 (43 %), prompts of 1000 x 16 (25 %), 400 x 64
+// (14 %) and 300 x 64, 128 x 16 x 5000 (11 %).
 constexpr int64_t kFewWork4 = 3328, kFewRows4 = 48;
 
 KvPlan kv_plan(int64_t n_tok, int n_heads, const tlq_kv_batch& b, const tlq_kv_cache& c, bool bits4) {

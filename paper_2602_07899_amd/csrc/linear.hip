@@ -285,11 +285,14 @@ LinearKind linear_kind(int64_t n_tok, int64_t c_out, int64_t K) {
 //   few:  1 x 4096 x 14336 (112) 15.5 16.6     16 x 2048 x 14336 (112) 12.7 12.1     32 x 1024 x 14336 (112) 12.4 11.2
 //         1 x 2048 x 28672 (224) 18.2 15.5     16 x 512 x 28672 (224) 11.7 8.8       32 x 512 x 14336 (112)   8.4  9.5
 //        48 x 1024 x 9216 (72)   12.1 10.7     64 x 256 x 9216 (72)    8.8 6.7       64 x 1024 x 14336 (112) 18.2  8.6
-//   mid: 16 x 4096 x 14336 (112) 20.1 15.9     64 x 4096 x 11008 (86) 19.1 15.7     128 x 4096 x 4096 (64)   15.0 15.6
-//        32 x 4096 x 11008 (86)  16.7 16.2     64 x 8192 x 14336 (112) 33.7 29.3    256 x 4096 x 2560 (80)   17.1 15.6
-//       128 x 8192 x 6144 (96)   28.4 26.4    256 x 8192 x 4096 (128) 28.9 24.8     256 x 8192 x 1024 (32)   17.0 24.0
-//        64 x 11008 x 14336 (112) 50.0 58.7    64 x 11008 x 16640 (130) 80.1 65.0   128 x 16384 x 8448 (132) 84.2 62.5
-// (the mid kernel splits the channels of up to 128 tiles).
+//        16 x 4096 x 14336 (112) 20.1 15.9
+//   mid: 64 x 4096 x 11008 (86)  19.1 15.7     32 x 4096 x 11008 (86)  16.7 16.2    128 x 4096 x 4096 (64)   15.0 15.6
+//        64 x 8192 x 14336 (112) 33.7 29.3    256 x 4096 x 2560 (80)   17.1 15.6    128 x 8192 x 6144 (96)   28.4 26.4
+//       256 x 8192 x 4096 (128)  28.9 24.8    256 x 8192 x 1024 (32)   17.0 24.0     64 x 11008 x 14336 (112) 50.0 58.7
+//        64 x 11008 x 16640 (130) 80.1 65.0 (the mid kernel splits the channels of up to 128 tiles)
+//   tiles of 128 x 128: 128 x 16384 x 8448 (132) 84.2 62.5
+// The rule for few tokens counts neither the channels nor what a token's bytes cost that each 16 outputs read again: it keeps the
+// slower kernel at 16 x 4096 x 14336 (26 %), 48 x 1024 x 9216 and 32 x 512 x 14336 (13 %), 16 x 2048 x 14336 (5 %).
 LinearKind linear_codes_kind(int64_t n_tok, int64_t c_out, int64_t K) {
   const LinearKind kind = linear_kind(n_tok, c_out, K);
   const int64_t tiles = ceil_div(n_tok, 64) * ceil_div(c_out, 128);

@@ -16,10 +16,13 @@ struct NormCodesDev {
 
 // h = round16(H + Z); u = (h * r) * w with r = 1 / sqrt(mean h^2 + eps); code = rint(u / step), step = max |u| / qa.
 // W waves have a row, P passes of 512 W channels, which stay in registers from the sum through the maximum to the codes, so that
-// H and Z are read once.  The squares of 16-bit numbers are exact in double and their sum is off by 2^-50 of itself at
-// most, whatever the order, so that r is the same float in any order (but where 1 / sqrt lies that near between two).  With one wave a row
+// H and Z are read once.  The squares of 16-bit numbers are exact in double and their sum is off by 2^-46 of itself at
+// most (85 additions one behind the other for 65,536 channels), so that r is the float that the definition gives, but where 1 / sqrt lies
+// that near between two (a row in some millions).  With one wave a row
 // a block has four rows.  Bound by bytes: 10,240 x 5120 with the residual 77 us, 4.8 TB/s of seven bytes an element (a copy reaches
-// 4.8), x 4096 60, x 8192 112, 4000 x 13824 86; by latency for few rows, 1 x 4096 3.6.
+// 4.8), x 4096 60, x 8192 112, 4000 x 13824 86, 2000 x 32,768 107; by latency for few rows, 1 x 4096 3.6.  Beyond 32,768 channels
+// the eight passes do not all fit into the 128 registers of a block of 16 waves, 30 are kept in scratch: 2000 x 32,776 206 us, x
+// 40,000 233 (2.4 TB/s), x 65,536 322 (2.8 TB/s).
 template <typename T, int W, int P>
 __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void add_norm_codes_kernel(NormCodesDev a) {
   __shared__ double sums[W];
